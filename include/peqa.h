@@ -379,6 +379,110 @@ typedef struct {
 peqa_status peqa_scale_update_multi(int32_t n, const peqa_update_item *items, const peqa_adamw *opt,
                                     void *stream);
 
+/*
+ * Decoding over a paged key-value cache.  What a decoder layer does between the query, key and value projections and
+ * the output projection when it answers one token at a time (Sec. 3.1's deployment): the new tokens' queries and keys are
+ * rotated by their positions, their keys and values stored, and every new query attends over its sequence's cache.
+ *
+ * The cache is two pools of pages, one of keys and one of values.  A page holds page_size consecutive positions of one
+ * sequence for all kv_heads heads; the page of positions [b page_size, (b+1) page_size) of sequence s is table[s][b].
+ * Element d of head h at position p lies at
+ *   page * page_stride + h * head_stride + (p % page_size) * slot_stride + d      (elements, in both pools)
+ * so pools of any order of heads and slots, and pools that hold keys and values side by side, can be described.
+ *   dtype PEQA_CACHE_BF16: bf16.  PEQA_CACHE_FP8: 8-bit floats with 4 exponent and 3 mantissa bits, no infinities, largest
+ *   finite value 448 ("e4m3fn"); a stored value stands for itself times k_scale[h] or v_scale[h] (fp32, device; NULL = 1).
+ *   k, v and the strides are multiples of 16 bytes (PEQA_ERR_ALIGN); page_size is a power of two, 8 .. 1024; head_dim is
+ *   64, 128 or 256.  A table entry outside [0, n_pages) stands for a page that is not there: nothing is stored to it and
+ *   its positions are not attended to.
+ * The struct is a HOST descriptor, read during the call; the table and the pools are read when the work runs.
+ */
+typedef enum { PEQA_CACHE_BF16 = 0, PEQA_CACHE_FP8 = 1 } peqa_cache_dtype;
+typedef struct {
+    void *k, *v;                                      /* pools                                         */
+    const int32_t *table;                             /* [n_seqs, n_blocks], rows table_stride apart   */
+    const float *k_scale, *v_scale;                   /* [kv_heads] or NULL; PEQA_CACHE_FP8 only       */
+    int64_t page_stride, head_stride, slot_stride;    /* in elements                                   */
+    int64_t table_stride;                             /* in entries                                    */
+    int32_t n_pages, page_size, kv_heads, head_dim;
+    int32_t n_seqs, n_blocks;
+    int32_t dtype;                                    /* peqa_cache_dtype                              */
+    int32_t reserved;                                 /* 0 */
+} peqa_kv_cache;
+
+/* PEQA_OK, or what is wrong with the descriptor (host-only). */
+peqa_status peqa_check_cache(const peqa_kv_cache *C);
+
+/*
+ * Rotates and stores T new tokens.  Token t is position pos[t] of sequence seq[t] (seq NULL: of sequence t).
+ *   q_out[t, h] = R(pos[t]) q[t, h];   cache[seq[t], pos[t], h] = R(pos[t]) k[t, h],  v[t, h]
+ * R turns pair i of the first `rot` elements of a head, (x[i], x[i + rot/2]), or (x[2i], x[2i+1]) where `interleaved`, by
+ * the angle whose cosine and sine are cos_table[pos, i] and sin_table[pos, i] (fp32 [n_pos, rot/2]); the other elements
+ * stay.  rot is a multiple of 16, at most head_dim; rot = 0 (tables NULL, n_pos not read): no rotation.
+ *   q [T, heads, head_dim] bf16, rows q_stride elements apart, or NULL (with q_out): keys and values only
+ *   k, v [T, kv_heads, head_dim] bf16, rows k_stride, v_stride apart;  q_out as q (may be q itself), rows q_out_stride apart
+ *   pointers and row strides multiples of 16 bytes: the members of a stacked query/key/value output can be passed as they lie
+ * The rotation is fp32 and rounds once to what is stored (nearest even; 8-bit: of x / scale, values past 448 become 448).
+ * A token with pos < 0, pos >= n_pos (where rotated), seq outside [0, n_seqs), a position past the table or a page that
+ * is not there is skipped: its row of q_out is zeros and nothing is stored.  Of tokens with the same sequence and position
+ * one is stored.
+ */
+peqa_status peqa_rope_append(const peqa_kv_cache *C, int32_t T, const int32_t *pos, const int32_t *seq,
+                             const float *cos_table, const float *sin_table, int32_t n_pos, int32_t rot,
+                             int32_t interleaved, int32_t heads, const uint16_t *q, int64_t q_stride, const uint16_t *k,
+                             int64_t k_stride, const uint16_t *v, int64_t v_stride, uint16_t *q_out,
+                             int64_t q_out_stride, void *stream);
+
+/*
+ * Attention of one query token per row over its sequence's cache: for row r (sequence seq[r]; NULL: r), head h and
+ * its key head h / (heads / kv_heads), over the positions j in [max(0, len - window), len), len = lens[r] (window 0: all)
+ *   x_j = scale * <q[r,h], k_j>;   out[r,h] = sum_j exp(x_j) v_j / sum_j exp(x_j);   lse[r,h] = log sum_j exp(x_j)
+ * A row with no position (len <= 0, seq outside [0, n_seqs), no page there) gives zeros and lse = -inf.  Positions outside
+ * the range may hold anything, NaN included.  Several new tokens of one sequence are rows with the same seq.
+ *   q, out [rows, heads, head_dim] bf16, rows q_stride, out_stride elements apart (multiples of 8, pointers 16-byte aligned)
+ *   lens [rows] int32;  lse [rows, heads] fp32 or NULL
+ *   max_len: the host's bound of lens, at most n_blocks * page_size (PEQA_ERR_SHAPE); longer rows are cut to it.  The work
+ *            is split for it, so a tight bound is faster.  heads: a multiple of kv_heads.
+ *   workspace: peqa_paged_attention_workspace_bytes(C, rows, heads, max_len, window).
+ * Products and sums are fp32.  The softmax weights are rounded for the matrix instructions: against bf16 values in two
+ * bf16 parts (16 bits), against 8-bit values to fp16 (11 bits).
+ */
+size_t peqa_paged_attention_workspace_bytes(const peqa_kv_cache *C, int32_t rows, int32_t heads, int32_t max_len,
+                                            int32_t window);
+peqa_status peqa_paged_attention(const peqa_kv_cache *C, int32_t rows, int32_t heads, const uint16_t *q, int64_t q_stride,
+                                 const int32_t *lens, const int32_t *seq, int32_t max_len, int32_t window, float scale,
+                                 uint16_t *out, int64_t out_stride, float *lse, void *workspace, size_t workspace_bytes,
+                                 void *stream);
+
+/*
+ * Log probabilities.  Of every row x = logits[t, 0 .. vocab-1] (bf16 or fp32, rows `stride` elements apart), in fp32:
+ *   lse[t] = log sum_j exp(x_j);  logp[t] = x[targets[t]] - lse[t];  entropy[t] = -sum_j p_j log p_j,  p_j = exp(x_j - lse[t])
+ *   top_ids[t, i], top_logp[t, i], i < top: the `top` largest x_j in falling order (equal ones: the lowest index first) and
+ *   their log probabilities
+ * A target outside [0, vocab) is ignored: logp = 0.  Words may be masked with -inf or the type's lowest value; a row of -inf
+ * only has lse = logp = top_logp = -inf and entropy 0.  A row with a NaN, or with +inf, gives NaN for all but the ids.
+ *   logits: rows at any element (16-byte aligned rows are faster), stride >= vocab;  targets [T] int32 or NULL (with logp NULL)
+ *   logp, entropy, lse [T] fp32, each or NULL;  top 0 .. PEQA_MAX_TOP, at most vocab;  top_logp, top_ids [T, top] (NULL if top = 0)
+ *   workspace: peqa_token_logprobs_workspace_bytes(T, vocab, top).
+ */
+#define PEQA_MAX_TOP 32
+typedef enum { PEQA_LOGITS_BF16 = 0, PEQA_LOGITS_F32 = 1 } peqa_logits_dtype;
+size_t peqa_token_logprobs_workspace_bytes(int32_t T, int32_t vocab, int32_t top);
+peqa_status peqa_token_logprobs(const void *logits, int32_t dtype, int32_t T, int32_t vocab, int64_t stride,
+                                const int32_t *targets, int32_t top, float *logp, float *entropy, float *lse,
+                                float *top_logp, int32_t *top_ids, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * The gradient of sum_t d_logp[t] logp[t] + d_entropy[t] entropy[t] with respect to the logits, in the logits' type:
+ *   d_logits[t, j] = d_logp[t] ([j = targets[t]] - p_j) - d_entropy[t] p_j (log p_j + entropy[t]),   p_j = exp(x_j - lse[t])
+ * (an ignored target: without the first term; p_j = 0 has no second).  The mean cross entropy of n tokens is d_logp = -1/n.
+ *   lse, and entropy where d_entropy is given, as peqa_token_logprobs left them;  d_logp or d_entropy may be NULL (= 0)
+ *   d_logits: rows d_stride elements apart, may be logits itself with the same stride; only the first `vocab` elements of
+ *   a row are written.  Rows whose two factors are 0 (logits not read), or whose lse is -inf, are zeros.
+ */
+peqa_status peqa_token_logprobs_bwd(const void *logits, int32_t dtype, int32_t T, int32_t vocab, int64_t stride,
+                                    const int32_t *targets, const float *lse, const float *entropy, const float *d_logp,
+                                    const float *d_entropy, void *d_logits, int64_t d_stride, void *stream);
+
 /* Compute units and peak engine clock (kHz) of the current device, as the HIP runtime reports them
  * (for benchmark reports: the denominators of roofline fractions). */
 peqa_status peqa_device_info(int32_t *compute_units, int32_t *clock_khz);

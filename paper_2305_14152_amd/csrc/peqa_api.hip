@@ -1035,7 +1035,8 @@ char g_trace_prefix[32] = "";     // only kernels whose name starts with this ar
 const char *const kKernelNames[peqa::KID_COUNT] = {
     "quantize", "rowsum", "gemm_y", "gemm_dds", "gemm_dx", "scale_dy", "reduce_partials", "adamw", "gemv",
     "gemv_finish", "group_table", "dds_kept", "dz_partial", "dz_finish", "transpose_pad", "gemm_dw", "gemm_bwd", "gemm_multi_y",
-    "gemm_multi_dds", "gemm_multi_dx", "gemm_finish"};
+    "gemm_multi_dds", "gemm_multi_dx", "gemm_finish", "rope_append", "attend", "attend_join", "logprobs", "logprobs_join",
+    "logprobs_bwd"};
 
 }  // namespace
 namespace {

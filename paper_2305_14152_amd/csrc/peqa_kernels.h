@@ -386,6 +386,7 @@ enum {
     KID_QUANTIZE = 0, KID_ROWSUM, KID_GEMM_Y, KID_GEMM_DDS, KID_GEMM_DX, KID_SCALE_DY,
     KID_REDUCE, KID_ADAMW, KID_GEMV, KID_GEMV_FINISH, KID_GROUP_TABLE, KID_DDS_KEPT, KID_DZ_PARTIAL, KID_DZ_FINISH,
     KID_TRANSPOSE, KID_GEMM_DW, KID_GEMM_BWD, KID_GEMM_MULTI_Y, KID_GEMM_MULTI_DDS, KID_GEMM_MULTI_DX, KID_GEMM_FINISH,
+    KID_ROPE_APPEND, KID_ATTEND, KID_ATTEND_JOIN, KID_LOGPROBS, KID_LOGPROBS_JOIN, KID_LOGPROBS_BWD,
     KID_COUNT
 };
 

@@ -1,0 +1,530 @@
+// Log probabilities of given words, entropy and the largest alternatives (peqa_token_logprobs), and the gradient of the
+// first two with respect to the logits (peqa_token_logprobs_bwd).
+//
+// With m the largest of a row, s = sum e^(x - m) and u = sum e^(x - m) (x - m):
+//   lse = m + log s,   logp = (x_target - m) - log s,   entropy = log s - u / s
+// m, s and u are kept per thread over one pass; when a larger m' is met, s and u are carried over to it:
+//   u' = e^(m - m') (u + s (m - m')),  s' = e^(m - m') s.
+// Alternatives: see take_top.
+#include "peqa_device.h"
+#include "peqa_host.h"
+
+using namespace peqa::host;
+
+namespace peqa {
+
+namespace {
+
+constexpr float LOG2E = 1.44269504088896341f;
+constexpr float LOWEST = -3.402823466e38f;   // the lowest finite float: the maximum of a row without a finite logit
+constexpr float FAR = -1e4f;                 // e^FAR is 0; products with differences are kept finite by it
+constexpr int CANDIDATES = 1024;             // alternatives that are gathered before their order is found
+
+struct LogprobArgs {
+    const void *logits;
+    const int32_t *targets;
+    float *logp, *entropy, *lse, *top_logp;
+    int32_t *top_ids;
+    float *part;                // [T, slices, 4] m, s, u of the slices of a row
+    unsigned long long *part_keys;   // [T, slices, top]
+    long long stride;
+    int T, V, top;
+    int slices, slice;          // slices of a row, and vectors of eight logits in one
+};
+
+struct GradArgs {
+    const void *logits;
+    const int32_t *targets;
+    const float *lse, *entropy, *d_logp, *d_entropy;
+    void *d_logits;
+    long long stride, d_stride;
+    int T, V, blocks;           // workgroups per row
+};
+
+__device__ __forceinline__ float exp_of(float y) { return __builtin_amdgcn_exp2f(y * LOG2E); }
+
+// A row as vectors of eight elements from the 16-byte boundary at or before its start on: `off` elements of the first vector
+// are not the row's.
+template <bool F32> struct Row {
+    typedef typename std::conditional<F32, float, uint16_t>::type T;
+    const T *base;
+    int off;
+    __device__ __forceinline__ Row(const void *logits, long long row, long long stride)
+    {
+        const T *p = static_cast<const T *>(logits) + row * stride;
+        off = (int)((reinterpret_cast<uintptr_t>(p) & 15u) / sizeof(T));
+        base = p - off;
+    }
+    __device__ __forceinline__ float one(int j) const
+    {
+        if constexpr (F32) return base[off + j];
+        else return __uint_as_float((uint32_t)base[off + j] << 16);
+    }
+    __device__ __forceinline__ int vectors(int V) const { return (V + off + 7) >> 3; }
+    __device__ __forceinline__ bool edge(int v, int V) const { return 8 * v < off || 8 * v + 8 > V + off; }
+};
+
+struct Raw {
+    u32x4 a, b;     // b: fp32 only
+};
+template <bool F32> __device__ __forceinline__ Raw load_vector(const Row<F32> &r, int v)
+{
+    Raw w;
+    const u32x4 *p = reinterpret_cast<const u32x4 *>(r.base + 8ll * v);
+    w.a = p[0];
+    if constexpr (F32) w.b = p[1];
+    return w;
+}
+template <bool F32> __device__ __forceinline__ void floats(const Raw &w, float x[8])
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if constexpr (F32) {
+            x[i] = __uint_as_float(w.a[i]);
+            x[4 + i] = __uint_as_float(w.b[i]);
+        } else {
+            x[2 * i] = bf16_lo(w.a[i]);
+            x[2 * i + 1] = bf16_hi(w.a[i]);
+        }
+    }
+}
+// Any vector of a row, what is not the row's as -inf; whole vectors by 16-byte loads.
+template <bool F32> __device__ __forceinline__ void read_vector(const Row<F32> &r, int v, int V, float x[8])
+{
+    if (!r.edge(v, V)) {
+        floats<F32>(load_vector<F32>(r, v), x);
+        return;
+    }
+    for (int i = 0; i < 8; ++i) {
+        const int j = 8 * v + i - r.off;
+        x[i] = j >= 0 && j < V ? r.one(j) : -__builtin_inff();
+    }
+}
+
+// Order of the alternatives as unsigned numbers: by logit, then the lower index first.  -0 counts as 0, NaN as -inf.
+__device__ __forceinline__ uint32_t order_of(float x)
+{
+    const uint32_t b = __float_as_uint(x != x ? -__builtin_inff() : x + 0.f);
+    return b & 0x80000000u ? ~b : b | 0x80000000u;
+}
+__device__ __forceinline__ unsigned long long key_of(float x, int j)
+{
+    return (unsigned long long)order_of(x) << 32 | (uint32_t)~j;
+}
+__device__ __forceinline__ int key_index(unsigned long long key) { return (int)~(uint32_t)key; }
+__device__ __forceinline__ float key_logit(unsigned long long key)
+{
+    const uint32_t b = (uint32_t)(key >> 32);
+    return __uint_as_float(b & 0x80000000u ? b & 0x7FFFFFFFu : ~b);
+}
+
+struct Stats {
+    float m, s, u;
+    // the state as seen from a maximum that is no smaller
+    __device__ __forceinline__ void move_to(float to)
+    {
+        const float d = fmaxf(m - to, FAR), f = exp_of(d);
+        u = f * (u + s * d);
+        s *= f;
+        m = to;
+    }
+};
+
+__device__ __forceinline__ float wave_sum(float v)
+{
+#pragma unroll
+    for (int o = 32; o >= 1; o >>= 1) v += __shfl_xor(v, o);
+    return v;
+}
+
+struct Answer {
+    float logp, entropy, lse, log_s, m;
+};
+__device__ __forceinline__ Answer answer_of(float m, float s, float u)
+{
+    Answer r;
+    r.m = m;
+    r.log_s = logf(s);
+    const bool none = s == 0.f;              // a row without a finite logit
+    r.lse = none ? -__builtin_inff() : m + r.log_s;
+    r.entropy = none ? 0.f : r.log_s - u / s;
+    return r;
+}
+__device__ __forceinline__ float logp_of(const Answer &r, float x) { return r.lse == -__builtin_inff() ? r.lse : (x - r.m) - r.log_s; }
+
+template <bool F32>
+__device__ __forceinline__ void write_row(const LogprobArgs &a, int row, const Row<F32> &r, const Answer &n)
+{
+    if (a.logp) {
+        const int t = a.targets[row];
+        a.logp[row] = t >= 0 && t < a.V ? logp_of(n, r.one(t)) : 0.f;
+    }
+    if (a.entropy) a.entropy[row] = n.entropy;
+    if (a.lse) a.lse[row] = n.lse;
+}
+
+// The `top` largest of `count` different keys in LDS, by counting for every key how many are larger.
+template <int NT, typename Out> __device__ __forceinline__ void rank_keys(const unsigned long long *keys, int count, int top, Out out)
+{
+    for (int i = threadIdx.x; i < count; i += NT) {
+        const unsigned long long key = keys[i];
+        int rank = 0;
+        for (int j = 0; j < count; ++j) rank += keys[j] > key;
+        if (rank < top) out(rank, key);
+    }
+}
+
+// One workgroup of NT threads per slice of a row.
+template <bool F32, int NT>
+__global__ __launch_bounds__(NT) void logprobs_kernel(LogprobArgs a)
+{
+    constexpr int WAVES = NT / 64;
+    __shared__ float wave_m[WAVES], wave_s[WAVES], wave_u[WAVES];
+    __shared__ unsigned long long best[NT], list[CANDIDATES], bound;
+    __shared__ int gathered;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int row = (int)(blockIdx.x / (unsigned)a.slices), slice = (int)(blockIdx.x - (unsigned)row * (unsigned)a.slices);
+    const Row<F32> r(a.logits, row, a.stride);
+    const int all = r.vectors(a.V);
+    const int v0 = slice * a.slice < all ? slice * a.slice : all, v1 = slice + 1 < a.slices && v0 + a.slice < all ? v0 + a.slice : all;
+
+    Stats st{LOWEST, 0.f, 0.f};
+    float most = -__builtin_inff();
+    int at = v0 + tid < v1 ? v0 + tid : -1;                // the vector with the first of this thread's largest
+    for (int v = v0 + tid; v < v1; v += NT) {
+        float x[8];
+        read_vector<F32>(r, v, a.V, x);
+        float vm = x[0];
+#pragma unroll
+        for (int i = 1; i < 8; ++i) vm = fmaxf(vm, x[i]);
+        if (vm > most) { most = vm; at = v; }
+        st.move_to(fmaxf(st.m, vm));
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float y = x[i] - st.m, e = exp_of(y);
+            st.s += e;
+            st.u += e * fmaxf(y, FAR);
+        }
+    }
+
+    unsigned long long mine = 0;
+    if (a.top > 0) {
+        if (at >= 0) {
+            float x[8];
+            read_vector<F32>(r, at, a.V, x);
+            for (int i = 7; i >= 0; --i) {
+                const int j = 8 * at + i - r.off;
+                if (j < 0 || j >= a.V) continue;
+                const unsigned long long key = key_of(x[i], j);
+                mine = key > mine ? key : mine;
+            }
+        }
+        best[tid] = mine;
+        if (tid == 0) { gathered = 0; bound = 0; }
+    }
+    float m = st.m;
+#pragma unroll
+    for (int o = 32; o >= 1; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
+    if (lane == 0) wave_m[wave] = m;
+    __syncthreads();
+    m = wave_m[0];
+#pragma unroll
+    for (int w = 1; w < WAVES; ++w) m = fmaxf(m, wave_m[w]);
+    st.move_to(m);
+    st.s = wave_sum(st.s);
+    st.u = wave_sum(st.u);
+    if (lane == 0) { wave_s[wave] = st.s; wave_u[wave] = st.u; }
+    if (a.top > 0) {
+        // The threads with the same lane are a group.  At least `top` groups have an element no smaller than the top-th
+        // largest of the 64 groups' best ones: all that is larger than or equal to this bound, a few more than `top` if the
+        // large logits lie anywhere, contains the answer.  Every wave looks at some of the groups' best.
+        unsigned long long column = 0;
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) column = best[w * 64 + lane] > column ? best[w * 64 + lane] : column;
+#pragma unroll
+        for (int i = 0; i < 64 / WAVES; ++i) {
+            const int l = wave * (64 / WAVES) + i;
+            const unsigned long long key = __shfl(column, l);
+            if (key != 0 && __popcll(__ballot(column > key)) == a.top - 1 && lane == 0) bound = key;
+        }
+    }
+    __syncthreads();
+    float s = 0.f, u = 0.f;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) { s += wave_s[w]; u += wave_u[w]; }
+    const Answer n = answer_of(m, s, u);
+    if (a.slices == 1) {
+        if (tid == 0) write_row<F32>(a, row, r, n);
+    } else if (tid == 0) {
+        float *p = a.part + 4 * ((size_t)row * a.slices + slice);
+        p[0] = m;
+        p[1] = s;
+        p[2] = u;
+    }
+    if (a.top == 0) return;
+
+    const unsigned long long least = bound;                // 0: fewer than `top` groups have elements
+    if (mine != 0 && mine >= least) {
+        for (int v = v0 + tid; v < v1; v += NT) {
+            float x[8];
+            read_vector<F32>(r, v, a.V, x);
+            for (int i = 0; i < 8; ++i) {
+                const int j = 8 * v + i - r.off;
+                if (j < 0 || j >= a.V) continue;
+                const unsigned long long key = key_of(x[i], j);
+                if (key < least) continue;
+                const int place = atomicAdd(&gathered, 1);
+                if (place < CANDIDATES) list[place] = key;
+            }
+        }
+    }
+    __syncthreads();
+    int count = gathered;
+    if (count > CANDIDATES) {
+        // Many large logits in few groups: the answer one by one, the largest key below the last one found.
+        unsigned long long below = ~0ull;
+        for (int k = 0; k < a.top; ++k) {
+            unsigned long long top = 0;
+            for (int v = v0 + tid; v < v1; v += NT) {
+                float x[8];
+                read_vector<F32>(r, v, a.V, x);
+                for (int i = 0; i < 8; ++i) {
+                    const int j = 8 * v + i - r.off;
+                    if (j < 0 || j >= a.V) continue;
+                    const unsigned long long key = key_of(x[i], j);
+                    if (key < below && key > top) top = key;
+                }
+            }
+#pragma unroll
+            for (int o = 32; o >= 1; o >>= 1) {
+                const unsigned long long other = __shfl_xor(top, o);
+                top = other > top ? other : top;
+            }
+            __syncthreads();
+            if (lane == 0) best[wave] = top;
+            __syncthreads();
+            below = best[0];
+#pragma unroll
+            for (int w = 1; w < WAVES; ++w) below = best[w] > below ? best[w] : below;
+            if (tid == 0) list[k] = below;
+        }
+        count = a.top;
+        __syncthreads();
+    }
+    if (a.slices == 1) {
+        rank_keys<NT>(list, count, a.top, [&](int rank, unsigned long long key) {
+            a.top_ids[(size_t)row * a.top + rank] = key_index(key);
+            a.top_logp[(size_t)row * a.top + rank] = logp_of(n, key_logit(key));
+        });
+    } else {
+        unsigned long long *keys = a.part_keys + ((size_t)row * a.slices + slice) * a.top;
+        rank_keys<NT>(list, count, a.top, [&](int rank, unsigned long long key) { keys[rank] = key; });
+        for (int k = count + tid; k < a.top; k += NT) keys[k] = 0;
+    }
+}
+
+// Joins the slices of a row: at most 32 of at most 32 keys.
+constexpr int SLICES_MAX = 32;
+template <bool F32>
+__global__ __launch_bounds__(256) void logprobs_join_kernel(LogprobArgs a)
+{
+    __shared__ unsigned long long keys[SLICES_MAX * PEQA_MAX_TOP];
+    const int row = blockIdx.x;
+    const float *p = a.part + 4 * (size_t)row * a.slices;
+    float m = LOWEST, s = 0.f, u = 0.f;
+    for (int i = 0; i < a.slices; ++i) m = fmaxf(m, p[4 * i]);
+    for (int i = 0; i < a.slices; ++i) {
+        Stats st{p[4 * i], p[4 * i + 1], p[4 * i + 2]};
+        st.move_to(m);
+        s += st.s;
+        u += st.u;
+    }
+    const Answer n = answer_of(m, s, u);
+    if (threadIdx.x == 0) write_row<F32>(a, row, Row<F32>(a.logits, row, a.stride), n);
+    if (a.top == 0) return;
+    const int count = a.slices * a.top;
+    for (int i = threadIdx.x; i < count; i += 256) keys[i] = a.part_keys[(size_t)row * count + i];
+    __syncthreads();
+    for (int i = threadIdx.x; i < count; i += 256) {
+        const unsigned long long key = keys[i];
+        if (key == 0) continue;
+        int rank = 0;
+        for (int j = 0; j < count; ++j) rank += keys[j] > key;
+        if (rank < a.top) {
+            a.top_ids[(size_t)row * a.top + rank] = key_index(key);
+            a.top_logp[(size_t)row * a.top + rank] = logp_of(n, key_logit(key));
+        }
+    }
+}
+
+// d_j = g ([j = target] - p_j) - h p_j (log p_j + H): one read and one write of the logits.
+constexpr int GRAD_VECTORS = 2;      // vectors of eight of a thread
+template <bool F32>
+__global__ __launch_bounds__(256) void logprobs_bwd_kernel(GradArgs a)
+{
+    const int row = (int)(blockIdx.x / (unsigned)a.blocks), block = (int)(blockIdx.x - (unsigned)row * (unsigned)a.blocks);
+    const Row<F32> r(a.logits, row, a.stride);
+    typedef typename Row<F32>::T E;
+    const int t = a.targets ? a.targets[row] : -1;
+    const bool live = t >= 0 && t < a.V;
+    const float lse = a.lse[row];
+    const float g = live && a.d_logp ? a.d_logp[row] : 0.f, h = a.d_entropy ? a.d_entropy[row] : 0.f;
+    const float H = a.d_entropy ? a.entropy[row] : 0.f;
+    const bool none = (g == 0.f && h == 0.f) || lse == -__builtin_inff();
+    E *out = static_cast<E *>(a.d_logits) + row * a.d_stride;
+    const bool aligned = (int)((reinterpret_cast<uintptr_t>(out) & 15u) / sizeof(E)) == r.off;
+    const int all = r.vectors(a.V);
+#pragma unroll
+    for (int k = 0; k < GRAD_VECTORS; ++k) {
+        const int v = (block * GRAD_VECTORS + k) * 256 + (int)threadIdx.x;
+        if (v >= all) return;
+        float x[8];
+        if (none) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] = 0.f;
+        } else {
+            read_vector<F32>(r, v, a.V, x);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float logp = x[i] - lse, p = exp_of(logp);
+                x[i] = -p * (g + h * (fmaxf(logp, FAR) + H));
+                if (8 * v + i - r.off == t) x[i] += g;
+            }
+        }
+        if (aligned && !r.edge(v, a.V)) {
+            u32x4 *o = reinterpret_cast<u32x4 *>(out + (8ll * v - r.off));
+            if constexpr (F32) {
+                o[0] = u32x4{__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3])};
+                o[1] = u32x4{__float_as_uint(x[4]), __float_as_uint(x[5]), __float_as_uint(x[6]), __float_as_uint(x[7])};
+            } else {
+                o[0] = u32x4{pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7])};
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int j = 8 * v + i - r.off;
+                if (j < 0 || j >= a.V) continue;
+                if constexpr (F32) out[j] = x[i];
+                else out[j] = (uint16_t)float_to_bf16_bits(x[i]);
+            }
+        }
+    }
+}
+
+// Slices of a row (0: the whole row by one workgroup) and vectors in one.
+struct LogprobPlan {
+    int slices, slice;
+    size_t part_bytes, key_bytes;
+};
+LogprobPlan logprob_plan(int T, int V, int top)
+{
+    LogprobPlan p{};
+    const int vectors = (V + 7 + 7) / 8;                       // with any offset of the row
+    int slices = PLAN_UNITS / T;
+    const int most = vectors / 2048;                            // two vectors a thread at least
+    slices = slices < most ? slices : most;
+    slices = slices < SLICES_MAX ? slices : SLICES_MAX;
+    p.slices = slices > 1 ? slices : 1;
+    p.slice = (vectors + p.slices - 1) / p.slices;
+    if (p.slices > 1) {
+        p.part_bytes = round256((size_t)T * p.slices * 4 * sizeof(float));
+        p.key_bytes = round256((size_t)T * p.slices * top * sizeof(unsigned long long));
+    }
+    return p;
+}
+
+peqa_status check_logits(int32_t dtype, int32_t T, int32_t vocab)
+{
+    if (dtype != PEQA_LOGITS_BF16 && dtype != PEQA_LOGITS_F32) return PEQA_ERR_PARAM;
+    if (T < 1 || vocab < 1 || vocab > (1 << 30)) return PEQA_ERR_SHAPE;
+    return PEQA_OK;
+}
+
+inline bool aligned_to(const void *p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
+
+}  // namespace
+}  // namespace peqa
+
+extern "C" {
+
+size_t peqa_token_logprobs_workspace_bytes(int32_t T, int32_t vocab, int32_t top)
+{
+    if (peqa::check_logits(PEQA_LOGITS_BF16, T, vocab) != PEQA_OK || top < 0 || top > PEQA_MAX_TOP || top > vocab) return 0;
+    const peqa::LogprobPlan p = peqa::logprob_plan(T, vocab, top);
+    const size_t bytes = p.part_bytes + p.key_bytes;
+    return bytes ? bytes : 256;
+}
+
+peqa_status peqa_token_logprobs(const void *logits, int32_t dtype, int32_t T, int32_t vocab, int64_t stride, const int32_t *targets,
+                                int32_t top, float *logp, float *entropy, float *lse, float *top_logp, int32_t *top_ids, void *workspace,
+                                size_t workspace_bytes, void *stream)
+{
+    const peqa_status st = peqa::check_logits(dtype, T, vocab);
+    if (st != PEQA_OK) return st;
+    if (top < 0 || top > PEQA_MAX_TOP || top > vocab) return PEQA_ERR_PARAM;
+    if (!logits || (logp && !targets) || (top > 0 && (!top_logp || !top_ids))) return PEQA_ERR_NULL;
+    if (!logp && !entropy && !lse && top == 0) return PEQA_ERR_NULL;
+    if (stride < vocab) return PEQA_ERR_SHAPE;
+    if (!peqa::aligned_to(logits, dtype == PEQA_LOGITS_F32 ? 4 : 2) || !peqa::aligned_to(targets, 4) || !peqa::aligned_to(logp, 4) ||
+        !peqa::aligned_to(entropy, 4) || !peqa::aligned_to(lse, 4) || !peqa::aligned_to(top_logp, 4) || !peqa::aligned_to(top_ids, 4))
+        return PEQA_ERR_ALIGN;
+    const peqa::LogprobPlan p = peqa::logprob_plan(T, vocab, top);
+    if (p.slices > 1) {
+        if (!workspace || workspace_bytes < p.part_bytes + p.key_bytes) return PEQA_ERR_WORKSPACE;
+        if (!aligned16(workspace)) return PEQA_ERR_ALIGN;
+    }
+    peqa::LogprobArgs a{};
+    a.logits = logits; a.targets = targets; a.logp = logp; a.entropy = entropy; a.lse = lse; a.top_logp = top_logp; a.top_ids = top_ids;
+    a.part = static_cast<float *>(workspace);
+    a.part_keys = p.slices > 1 ? reinterpret_cast<unsigned long long *>(static_cast<char *>(workspace) + p.part_bytes) : nullptr;
+    a.stride = stride;
+    a.T = T; a.V = vocab; a.top = top; a.slices = p.slices; a.slice = p.slice;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    const unsigned grid = (unsigned)T * (unsigned)p.slices;
+    peqa::trace_before(peqa::KID_LOGPROBS, s);
+    if (dtype == PEQA_LOGITS_F32)
+        hipLaunchKernelGGL((peqa::logprobs_kernel<true, 1024>), dim3(grid), dim3(1024), 0, s, a);
+    else
+        hipLaunchKernelGGL((peqa::logprobs_kernel<false, 1024>), dim3(grid), dim3(1024), 0, s, a);
+    peqa::trace_after(peqa::KID_LOGPROBS, s);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess || p.slices == 1) return dev_status(e);
+    peqa::trace_before(peqa::KID_LOGPROBS_JOIN, s);
+    if (dtype == PEQA_LOGITS_F32)
+        hipLaunchKernelGGL((peqa::logprobs_join_kernel<true>), dim3((unsigned)T), dim3(256), 0, s, a);
+    else
+        hipLaunchKernelGGL((peqa::logprobs_join_kernel<false>), dim3((unsigned)T), dim3(256), 0, s, a);
+    peqa::trace_after(peqa::KID_LOGPROBS_JOIN, s);
+    return dev_status(hipGetLastError());
+}
+
+peqa_status peqa_token_logprobs_bwd(const void *logits, int32_t dtype, int32_t T, int32_t vocab, int64_t stride, const int32_t *targets,
+                                    const float *lse, const float *entropy, const float *d_logp, const float *d_entropy, void *d_logits,
+                                    int64_t d_stride, void *stream)
+{
+    const peqa_status st = peqa::check_logits(dtype, T, vocab);
+    if (st != PEQA_OK) return st;
+    if (!logits || !lse || !d_logits || (!d_logp && !d_entropy) || (d_logp && !targets) || (d_entropy && !entropy)) return PEQA_ERR_NULL;
+    if (stride < vocab || d_stride < vocab || (d_logits == logits && d_stride != stride)) return PEQA_ERR_SHAPE;
+    const size_t el = dtype == PEQA_LOGITS_F32 ? 4 : 2;
+    if (!peqa::aligned_to(logits, el) || !peqa::aligned_to(d_logits, el) || !peqa::aligned_to(targets, 4) || !peqa::aligned_to(lse, 4) ||
+        !peqa::aligned_to(entropy, 4) || !peqa::aligned_to(d_logp, 4) || !peqa::aligned_to(d_entropy, 4))
+        return PEQA_ERR_ALIGN;
+    peqa::GradArgs a{};
+    a.logits = logits; a.targets = targets; a.lse = lse; a.entropy = entropy; a.d_logp = d_logp; a.d_entropy = d_entropy;
+    a.d_logits = d_logits; a.stride = stride; a.d_stride = d_stride; a.T = T; a.V = vocab;
+    const int vectors = (vocab + 7 + 7) / 8;
+    a.blocks = (vectors + 256 * peqa::GRAD_VECTORS - 1) / (256 * peqa::GRAD_VECTORS);
+    if (a.blocks > INT32_MAX / T) return PEQA_ERR_SHAPE;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    const unsigned grid = (unsigned)T * (unsigned)a.blocks;
+    peqa::trace_before(peqa::KID_LOGPROBS_BWD, s);
+    if (dtype == PEQA_LOGITS_F32)
+        hipLaunchKernelGGL((peqa::logprobs_bwd_kernel<true>), dim3(grid), dim3(256), 0, s, a);
+    else
+        hipLaunchKernelGGL((peqa::logprobs_bwd_kernel<false>), dim3(grid), dim3(256), 0, s, a);
+    peqa::trace_after(peqa::KID_LOGPROBS_BWD, s);
+    return dev_status(hipGetLastError());
+}
+
+}  // extern "C"

@@ -22,7 +22,9 @@ EXPORTS = ["peqa_check_layout", "peqa_packed_words", "peqa_num_scales", "peqa_wo
            "peqa_scale_update_multi", "peqa_device_info",
            "peqa_row_sums", "peqa_linear_fwd_fused_rs", "peqa_linear_bwd_rs",
            "peqa_set_option", "peqa_get_option", "peqa_linear_fwd_static",
-           "peqa_block_workspace_bytes", "peqa_block_fwd", "peqa_block_bwd", "peqa_trace_select"]
+           "peqa_block_workspace_bytes", "peqa_block_fwd", "peqa_block_bwd", "peqa_trace_select",
+           "peqa_check_cache", "peqa_rope_append", "peqa_paged_attention_workspace_bytes", "peqa_paged_attention",
+           "peqa_token_logprobs_workspace_bytes", "peqa_token_logprobs", "peqa_token_logprobs_bwd"]
 
 
 class Layout(ctypes.Structure):
@@ -37,6 +39,20 @@ class Layout(ctypes.Structure):
 class AdamW(ctypes.Structure):
     _fields_ = [("lr", ctypes.c_float), ("beta1", ctypes.c_float), ("beta2", ctypes.c_float),
                 ("eps", ctypes.c_float), ("weight_decay", ctypes.c_float), ("step", ctypes.c_int32)]
+
+
+PEQA_CACHE_BF16, PEQA_CACHE_FP8 = 0, 1
+PEQA_LOGITS_BF16, PEQA_LOGITS_F32 = 0, 1
+PEQA_MAX_TOP = 32
+
+
+class KVCache(ctypes.Structure):
+    """peqa_kv_cache; made by kv_cache(), which keeps the tensors that it points into."""
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("table", ctypes.c_void_p), ("k_scale", ctypes.c_void_p),
+                ("v_scale", ctypes.c_void_p), ("page_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64),
+                ("slot_stride", ctypes.c_int64), ("table_stride", ctypes.c_int64), ("n_pages", ctypes.c_int32),
+                ("page_size", ctypes.c_int32), ("kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("n_seqs", ctypes.c_int32), ("n_blocks", ctypes.c_int32), ("dtype", ctypes.c_int32), ("reserved", ctypes.c_int32)]
 
 
 class PeqaError(RuntimeError):
@@ -119,6 +135,21 @@ def lib():
         L.peqa_trace_end.argtypes = [i32, ctypes.POINTER(ctypes.c_char_p), ctypes.POINTER(i32),
                                      ctypes.POINTER(ctypes.c_float)]
         L.peqa_trace_end.restype = i32
+        i64, CP = ctypes.c_int64, ctypes.POINTER(KVCache)
+        L.peqa_check_cache.argtypes = [CP]
+        L.peqa_check_cache.restype = i32
+        L.peqa_rope_append.argtypes = [CP, i32, vp, vp, vp, vp, i32, i32, i32, i32, vp, i64, vp, i64, vp, i64, vp, i64, vp]
+        L.peqa_rope_append.restype = i32
+        L.peqa_paged_attention_workspace_bytes.argtypes = [CP, i32, i32, i32, i32]
+        L.peqa_paged_attention_workspace_bytes.restype = sz
+        L.peqa_paged_attention.argtypes = [CP, i32, i32, vp, i64, vp, vp, i32, i32, ctypes.c_float, vp, i64, vp, vp, sz, vp]
+        L.peqa_paged_attention.restype = i32
+        L.peqa_token_logprobs_workspace_bytes.argtypes = [i32, i32, i32]
+        L.peqa_token_logprobs_workspace_bytes.restype = sz
+        L.peqa_token_logprobs.argtypes = [vp, i32, i32, i32, i64, vp, i32, vp, vp, vp, vp, vp, vp, sz, vp]
+        L.peqa_token_logprobs.restype = i32
+        L.peqa_token_logprobs_bwd.argtypes = [vp, i32, i32, i32, i64, vp, vp, vp, vp, vp, vp, i64, vp]
+        L.peqa_token_logprobs_bwd.restype = i32
         _lib = L
     return _lib
 
@@ -371,3 +402,97 @@ def trace_end(max_kernels=32):
     total_ms = (ctypes.c_float * max_kernels)()
     n = lib().peqa_trace_end(max_kernels, names, launches, total_ms)
     return {names[i].decode(): (int(launches[i]), float(total_ms[i])) for i in range(n)}
+
+
+def kv_cache(k, v, table, k_scale=None, v_scale=None):
+    """The cache of two pools [pages, kv_heads, page_size, head_dim] (any strides, the same of both, the last 1; one byte per
+    element: 8-bit floats, two: bf16) and a table [sequences, blocks] of int32."""
+    assert k.shape == v.shape and k.dim() == 4 and k.stride() == v.stride() and k.stride(3) == 1 and k.dtype == v.dtype, \
+        "pools [pages, kv_heads, page_size, head_dim] of one type with the same strides, the last 1"
+    assert table.dim() == 2 and table.stride(1) == 1 and table.element_size() == 4, "table [sequences, blocks] of int32"
+    assert k.element_size() in (1, 2)
+    c = KVCache(k.data_ptr(), v.data_ptr(), table.data_ptr(), _ptr(k_scale), _ptr(v_scale), k.stride(0), k.stride(1), k.stride(2),
+                max(table.stride(0), table.shape[1]), k.shape[0], k.shape[2], k.shape[1], k.shape[3], table.shape[0], table.shape[1],
+                PEQA_CACHE_FP8 if k.element_size() == 1 else PEQA_CACHE_BF16, 0)
+    c.tensors = (k, v, table, k_scale, v_scale)
+    return c
+
+
+def check_cache(cache):
+    return int(lib().peqa_check_cache(ctypes.byref(cache)))
+
+
+def _rows(x, heads, dim):
+    """(pointer, row stride) of a tensor [rows, heads, dim] whose rows are contiguous."""
+    s0, s1, s2 = x.stride()
+    assert x.shape[1] == heads and x.shape[2] == dim and s2 == 1 and (s1 == dim or heads == 1) and x.element_size() == 2, \
+        "tensors [rows, heads, head_dim] of bf16 whose rows are contiguous"
+    return x.data_ptr(), s0 if x.shape[0] > 1 else heads * dim
+
+
+def rope_append(cache, q, k, v, pos, cos, sin, q_out, seq=None, interleaved=False, stream=None):
+    """q, q_out [T, heads, head_dim] or None, k, v [T, kv_heads, head_dim], pos, seq [T] int32, cos, sin [positions, rot / 2] fp32
+    or None (no rotation)."""
+    T, dim = k.shape[0], cache.head_dim
+    kp, ks = _rows(k, cache.kv_heads, dim)
+    vp, vs = _rows(v, cache.kv_heads, dim)
+    heads, qp, qs, op, os_ = 0, None, 0, None, 0
+    if q is not None:
+        heads = q.shape[1]
+        qp, qs = _rows(q, heads, dim)
+        if q_out is not None:
+            op, os_ = _rows(q_out, heads, dim)
+            assert q_out.shape[0] == T and q.shape[0] == T
+    assert v.shape[0] == T and pos.shape[0] == T and (seq is None or seq.shape[0] == T)
+    n_pos, half = cos.shape if cos is not None else (0, 0)
+    assert cos is None or sin.shape == cos.shape
+    _check(lib().peqa_rope_append(cache, T, _ptr(pos), _ptr(seq), _ptr(cos), _ptr(sin), n_pos, 2 * half, int(interleaved),
+                                  heads, qp, qs, kp, ks, vp, vs, op, os_, _stream(stream)), "peqa_rope_append")
+
+
+def paged_attention_workspace_bytes(cache, heads, rows, max_len, window=0):
+    return int(lib().peqa_paged_attention_workspace_bytes(ctypes.byref(cache), int(rows), int(heads), int(max_len), int(window)))
+
+
+def paged_attention(cache, q, lens, max_len, scale, out, workspace, workspace_bytes_, lse=None, seq=None, window=0, stream=None):
+    """q, out [rows, heads, head_dim], lens, seq [rows] int32, lse [rows, heads] fp32."""
+    rows, heads, dim = q.shape
+    qp, qs = _rows(q, heads, cache.head_dim)
+    op, os_ = _rows(out, heads, dim)
+    assert out.shape[0] == rows and lens.shape[0] == rows and (seq is None or seq.shape[0] == rows)
+    assert lse is None or lse.shape == (rows, heads)
+    _check(lib().peqa_paged_attention(cache, rows, heads, qp, qs, _ptr(lens), _ptr(seq), max_len, window, scale, op, os_,
+                                      _ptr(lse), _ptr(workspace), workspace_bytes_, _stream(stream)), "peqa_paged_attention")
+
+
+def _logits(x):
+    """(pointer, type, rows, words, row stride) of logits [T, vocab]."""
+    (T, V), (s0, s1), size = x.shape, x.stride(), x.element_size()
+    assert (s1 == 1 or V == 1) and size in (2, 4), "logits [T, vocab] of bf16 or fp32 with contiguous rows"
+    return x.data_ptr(), PEQA_LOGITS_F32 if size == 4 else PEQA_LOGITS_BF16, T, V, s0 if T > 1 else V
+
+
+def token_logprobs_workspace_bytes(T, vocab, top=0):
+    return int(lib().peqa_token_logprobs_workspace_bytes(int(T), int(vocab), int(top)))
+
+
+def token_logprobs(logits, targets, logp, entropy, lse, top_logp, top_ids, workspace, workspace_bytes_, stream=None):
+    """logits [T, vocab], targets [T] int32, logp, entropy, lse [T] fp32 or None, top_logp, top_ids [T, top] or None."""
+    xp, dtype, T, V, stride = _logits(logits)
+    top = 0
+    if top_ids is not None:
+        top = top_ids.shape[1]
+        assert top_ids.shape[0] == T and top_logp.shape == top_ids.shape
+    assert targets is None or targets.shape[0] == T
+    _check(lib().peqa_token_logprobs(xp, dtype, T, V, stride, _ptr(targets), top, _ptr(logp), _ptr(entropy), _ptr(lse),
+                                     _ptr(top_logp), _ptr(top_ids), _ptr(workspace), workspace_bytes_, _stream(stream)),
+           "peqa_token_logprobs")
+
+
+def token_logprobs_bwd(logits, targets, lse, entropy, d_logp, d_entropy, d_logits, stream=None):
+    """d_logits [T, vocab], the gradient of sum(d_logp * logp + d_entropy * entropy); may be `logits` itself."""
+    xp, dtype, T, V, stride = _logits(logits)
+    dp, d_dtype, dT, dV, d_stride = _logits(d_logits)
+    assert (d_dtype, dT, dV) == (dtype, T, V) and (targets is None or targets.shape[0] == T)
+    _check(lib().peqa_token_logprobs_bwd(xp, dtype, T, V, stride, _ptr(targets), _ptr(lse), _ptr(entropy), _ptr(d_logp),
+                                         _ptr(d_entropy), dp, d_stride, _stream(stream)), "peqa_token_logprobs_bwd")
