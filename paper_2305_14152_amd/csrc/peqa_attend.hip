@@ -388,40 +388,68 @@ __global__ __launch_bounds__(64 * WAVES) void attend_kernel(AttendArgs a)
     }
 }
 
-// Joins the chunks of the rows that have several: one wave per row and head.
+// Joins the chunks of the rows that have several: one workgroup per row and head.  A group of D / 4 lanes reads the
+// sums of a chunk, 16 bytes a lane; the groups take the chunks in turn, four loads of a lane in flight, and meet in LDS.
 template <int D, bool FP8>
 __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a)
 {
-    constexpr int E = D / 64;
-    const int lane = threadIdx.x & 63;
-    const long long rh = blockIdx.x * 4ll + (threadIdx.x >> 6);
-    if (rh >= (long long)a.rows * a.heads) return;
-    const int row = (int)(rh / a.heads), head = (int)(rh - (long long)row * a.heads);
+    constexpr int LANES = D / 4, GROUPS = 256 / LANES, BATCH = 256;
+    __shared__ float weight[BATCH], wave_x[4];
+    __shared__ f32x4 sums[GROUPS][LANES];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int row = (int)(blockIdx.x / (unsigned)a.heads), head = (int)(blockIdx.x - (unsigned)row * (unsigned)a.heads);
     const RowRange range = row_range(a, row);
     const int n = (range.len - range.from + a.chunk - 1) / a.chunk;
     if (n < 2) return;
+    const size_t rh = (size_t)row * a.heads + head;
     const float *ml = a.part_ml + 2 * rh * a.splits;
     float top = LOWEST;
-    for (int s = lane; s < n; s += 64) top = fmaxf(top, ml[2 * s]);
+    for (int s = tid; s < n; s += 256) top = fmaxf(top, ml[2 * s]);
 #pragma unroll
     for (int o = 32; o >= 1; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
-    float total = 0.f, sum[E];
+    if (lane == 0) wave_x[wave] = top;
+    __syncthreads();
+    top = fmaxf(fmaxf(wave_x[0], wave_x[1]), fmaxf(wave_x[2], wave_x[3]));
+    const int at = tid % LANES, group = tid / LANES;
+    const f32x4 *part = reinterpret_cast<const f32x4 *>(a.part + rh * a.splits * D) + at;
+    f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+    float total = 0.f;
+    for (int s0 = 0; s0 < n; s0 += BATCH) {
+        const int here = n - s0 < BATCH ? n - s0 : BATCH;
+        __syncthreads();                                       // (also: everyone has read wave_x)
+        float w = 0.f;
+        if (tid < here) {
+            w = __builtin_amdgcn_exp2f(ml[2 * (s0 + tid)] - top);
+            total += w * ml[2 * (s0 + tid) + 1];
+        }
+        weight[tid] = w;
+        __syncthreads();
+        for (int i = group; i < here; i += 4 * GROUPS) {
+            f32x4 x[4];
 #pragma unroll
-    for (int e = 0; e < E; ++e) sum[e] = 0.f;
-    const float *part = a.part + rh * a.splits * D + E * lane;
-    for (int s = 0; s < n; ++s) {
-        const float w = __builtin_amdgcn_exp2f(ml[2 * s] - top);
-        total += w * ml[2 * s + 1];
+            for (int k = 0; k < 4; ++k) x[k] = part[(size_t)(s0 + (i + k * GROUPS < here ? i + k * GROUPS : i)) * LANES];
 #pragma unroll
-        for (int e = 0; e < E; ++e) sum[e] += w * part[(size_t)s * D + e];
+            for (int k = 0; k < 4; ++k) {
+                const float wk = i + k * GROUPS < here ? weight[i + k * GROUPS] : 0.f;
+                if (i + k * GROUPS < here) sum += x[k] * wk;
+            }
+        }
     }
+#pragma unroll
+    for (int o = 32; o >= 1; o >>= 1) total += __shfl_xor(total, o);
+    if (lane == 0) wave_x[wave] = total;
+    sums[group][at] = sum;
+    __syncthreads();
+    if (tid >= LANES) return;
+    total = (wave_x[0] + wave_x[1]) + (wave_x[2] + wave_x[3]);
+#pragma unroll
+    for (int k = 1; k < GROUPS; ++k) sum += sums[k][at];
     const bool any = total > 0.f || total != total;
     const float v_scale = FP8 && a.cache.v_scale ? a.cache.v_scale[head / a.group] : 1.f;
     const float by = any ? v_scale / total : 0.f;
-    uint16_t *o = a.out + row * a.out_stride + (long long)head * D + E * lane;
-#pragma unroll
-    for (int e = 0; e < E; ++e) o[e] = (uint16_t)float_to_bf16_bits(sum[e] * by);
-    if (a.lse && lane == 0) a.lse[rh] = any ? (top + __builtin_amdgcn_logf(total)) * LN2 : -__builtin_inff();
+    uint16_t *o = a.out + row * a.out_stride + (long long)head * D + 4 * at;
+    *reinterpret_cast<u32x2 *>(o) = u32x2{pack_bf16x2(sum[0] * by, sum[1] * by), pack_bf16x2(sum[2] * by, sum[3] * by)};
+    if (a.lse && tid == 0) a.lse[rh] = any ? (top + __builtin_amdgcn_logf(total)) * LN2 : -__builtin_inff();
 }
 
 template <int D, bool FP8>
@@ -441,7 +469,7 @@ hipError_t launch_attend(const AttendArgs &a, int hb, hipStream_t stream)
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || a.splits == 1) return e;
     trace_before(KID_ATTEND_JOIN, stream);
-    hipLaunchKernelGGL((attend_join_kernel<D, FP8>), dim3((unsigned)(((long long)a.rows * a.heads + 3) / 4)), dim3(256), 0, stream, a);
+    hipLaunchKernelGGL((attend_join_kernel<D, FP8>), dim3((unsigned)a.rows * (unsigned)a.heads), dim3(256), 0, stream, a);
     trace_after(KID_ATTEND_JOIN, stream);
     return hipGetLastError();
 }
@@ -461,9 +489,15 @@ AttendPlan attend_plan(const peqa_kv_cache *C, int rows, int heads, int max_len,
     const long long span = window > 0 && (long long)window + TILE - 1 < max_len ? (long long)window + TILE - 1 : max_len;
     const long long items = (long long)rows * C->kv_heads * p.blocks;
     // workgroups for every unit several times over, but no chunk under two tiles a wave
-    long long want = (PLAN_UNITS * 8ll + items - 1) / items;
+#ifndef WANT
+#define WANT 8
+#endif
+    long long want = (PLAN_UNITS * (long long)WANT + items - 1) / items;
     long long chunk = (span + want - 1) / want;
-    const long long least = 2 * WAVES * TILE;
+#ifndef LEAST
+#define LEAST 2
+#endif
+    const long long least = LEAST * WAVES * TILE;
     if (chunk < least) chunk = least;
     if (chunk > CHUNK_MAX) chunk = CHUNK_MAX;
     p.chunk = (int)((chunk + TILE * WAVES - 1) / (TILE * WAVES) * (TILE * WAVES));
