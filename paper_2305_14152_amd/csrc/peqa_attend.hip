@@ -7,8 +7,9 @@
 // queries, so that a lane ends with eight scores of ONE head, which are the weights' operand of the second product as they
 // stand, and values^T x weights, for which a lane loads whole 16-byte pieces of eight positions and turns the 8 x 8 elements
 // in registers.
-// Positions are split twice: tiles of 32 over the waves of a workgroup, chunks over workgroups; what the waves have is
-// joined in LDS, and what the chunks have by a second kernel.
+// Positions are split over the waves of a workgroup in tiles of 32, whose sums meet in LDS, and over workgroups, joined by a second
+// kernel (attend_plan): a workgroup has a whole item (a row with the heads of one key head), a chunk of one, or an equal share
+// of all items laid end to end.
 #include "peqa_cache.h"
 #include "peqa_host.h"
 
@@ -23,9 +24,16 @@ typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 
 constexpr int TILE = 32;                 // positions per step of a wave
 constexpr int WAVES = 4;
-constexpr int CHUNK_MAX = 4096;          // positions of a workgroup at most (its pages' numbers are in LDS)
+constexpr int UNIT = 64;                 // positions that shares are counted in
+constexpr int CHUNK = 4096;              // positions whose pages are in LDS at a time
+constexpr int SCAN_ROWS = 1024;          // rows of a launch of equal shares at most: every workgroup adds up their lengths
 constexpr float LOWEST = -3.0e38f;       // finite stand-in for the maximum of nothing: e^(-inf - LOWEST) is 0, not NaN
 constexpr float LN2 = 0.693147180559945309f, LOG2E = 1.44269504088896341f;
+
+// An item in several workgroups, for the join (n < 2: none): the slots of its n parts are first, next, next + step, ...
+struct ItemParts {
+    int row, item, n, first, next, step;
+};
 
 struct AttendArgs {
     CacheArgs cache;
@@ -33,31 +41,122 @@ struct AttendArgs {
     const int32_t *lens, *seq;
     uint16_t *out;
     float *lse;
-    float *part;               // [rows, heads, splits, head_dim] sums of the chunks, relative to their maxima
-    float *part_ml;            // [rows, heads, splits, 2] maximum (of powers of two) and sum
+    // Parts of items that are in several workgroups: a slot has the heads of one workgroup.
+    float *part;               // [slots, per_wg, head_dim] weighted sums, relative to the maximum
+    float *part_ml;            // [slots, per_wg, 2] maximum (of powers of two) and sum
+    ItemParts *parts;          // [rows * items of a row], or [shares]: of the item that ends in a share and began before it
     long long q_stride, out_stride;
     float scale;               // times log2 e
     int rows, heads, group;    // heads per key head
     int max_len, window;
-    int chunk, splits, blocks; // positions of a chunk, chunks of the longest row, workgroups per key head
+    int blocks, per_wg;        // workgroups' worth of heads per key head, and heads in one
+    int splits, chunk_units;   // chunks of the longest row, and units in one
+    int shares;                // workgroups of a launch of equal shares; 0: workgroups of chunks
 };
 
-// What of a row there is: positions [lo, len), of which chunk s has [from + s chunk, ..) (from: lo rounded down to a tile).
+// What of a row there is: positions [lo, len), walked from `from` on (lo rounded down to a unit), in `units`.
 struct RowRange {
-    int seq, lo, from, len;
+    int lo, from, len, units;
 };
-__device__ __forceinline__ RowRange row_range(const AttendArgs &a, int row)
+__device__ __forceinline__ RowRange row_range(const AttendArgs &a, int len)
 {
     RowRange r;
-    r.seq = a.seq ? a.seq[row] : row;
-    int len = a.lens[row];
-    len = len < a.max_len ? len : a.max_len;
-    if (r.seq < 0 || r.seq >= a.cache.n_seqs || len < 0) len = 0;
     r.len = len;
     r.lo = a.window > 0 && len > a.window ? len - a.window : 0;
-    r.from = r.lo & ~(TILE - 1);
+    r.from = r.lo & ~(UNIT - 1);
+    r.units = (len - r.from + UNIT - 1) / UNIT;
+    if (r.units == 0) r.units = 1;                         // an empty row is an item too: of zeros
     return r;
 }
+// A row's sequence and the positions it has.
+struct RowInfo {
+    int seq, len;
+};
+__device__ __forceinline__ RowInfo row_info(const AttendArgs &a, int row)
+{
+    RowInfo r;
+    r.seq = a.seq ? a.seq[row] : row;
+    r.len = a.lens[row];
+    r.len = r.len < a.max_len ? r.len : a.max_len;
+    if (r.seq < 0 || r.seq >= a.cache.n_seqs || r.len < 0) { r.len = 0; r.seq = 0; }
+    return r;
+}
+
+// What a workgroup does: units [at, until) of all items laid end to end; `at` is in row `row`, whose first unit is `row_at`.
+// Shares are cut at multiples of `length` from a line on which every item has START more units in front: what a workgroup
+// takes to begin one and to leave its result.
+constexpr int START = 3;
+struct Share {
+    int at, until, length, row, row_at;
+};
+
+// Share number `share` of a launch of equal shares; leaves what all rows have in `info`.  scan: WAVES + 6 numbers of LDS.
+__device__ __forceinline__ Share share_of(const AttendArgs &a, int share, int per_row, RowInfo *info, int *scan)
+{
+    constexpr int EACH = SCAN_ROWS / (64 * WAVES);
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    int units[EACH], sum = 0;
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+        const int row = i * 64 * WAVES + tid;
+        units[i] = 0;
+        if (row < a.rows) info[row] = row_info(a, row);
+    }
+    __syncthreads();
+    const int each = (a.rows + 64 * WAVES - 1) / (64 * WAVES);
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+        const int row = tid * each + i;
+        if (i < each && row < a.rows) units[i] = (row_range(a, info[row].len).units + START) * per_row;
+        sum += units[i];
+    }
+    int upto = sum;
+#pragma unroll
+    for (int o = 1; o < 64; o *= 2) {
+        const int other = __shfl_up(upto, o);
+        if (lane >= o) upto += other;
+    }
+    if (lane == 63) scan[wave] = upto;
+    __syncthreads();
+    int before = upto - sum, total = 0;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) {
+        before += w < wave ? scan[w] : 0;
+        total += scan[w];
+    }
+    Share s;
+    s.length = __builtin_amdgcn_readfirstlane((total + a.shares - 1) / a.shares);
+    const int cut[2] = {share * s.length, share * s.length + s.length};
+    int *found = scan + WAVES;                             // row, its first unit, unit: of both cuts
+    if (tid < 6) found[tid] = tid % 3 == 0 ? a.rows : total - START * per_row * a.rows;    // cuts past the end
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+            if (cut[k] >= before && cut[k] < before + units[i]) {
+                const int row = tid * each + i, of_item = units[i] / per_row, in = cut[k] - before, item = in / of_item;
+                const int unit = in - item * of_item - START, row_at = before - START * per_row * row;
+                found[3 * k] = row;
+                found[3 * k + 1] = row_at;
+                found[3 * k + 2] = row_at + item * (of_item - START) + (unit > 0 ? unit : 0);
+            }
+        before += units[i];
+    }
+    __syncthreads();
+    // (all that a share is, is the same for the whole workgroup)
+    s.row = __builtin_amdgcn_readfirstlane(found[0]);
+    s.row_at = __builtin_amdgcn_readfirstlane(found[1]);
+    s.at = __builtin_amdgcn_readfirstlane(found[2]);
+    s.until = __builtin_amdgcn_readfirstlane(found[5]);
+    return s;
+}
+
+// A piece of a share: at most CHUNK positions [begin, end) of an item.  A segment is what a share has of an item: one or more pieces.
+struct Piece {
+    int row, item, kv_head, first_head, seq, lo, begin, end, slot;    // first_head: of the heads that share kv_head
+    bool first, last, alone;                               // of its segment; alone: the segment is the whole item
+};
 
 __device__ __forceinline__ f32x4 mfma_bf16(u32x4 x, u32x4 y, f32x4 c)
 {
@@ -78,8 +177,12 @@ template <bool HI> __device__ __forceinline__ uint32_t fp8_f16(uint32_t v)
     return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(v, 1.f, HI));
 }
 
+// Workgroups of a unit: two, of one wave per SIMD each, with up to 256 registers a lane; of the widest heads, whose two tiles
+// alone are as many, one with up to 512.
+constexpr int wgs_per_unit(int D, bool fp8) { return D > 128 && !fp8 ? 1 : 2; }
+
 template <int D, bool FP8, int HB>
-__global__ __launch_bounds__(64 * WAVES) void attend_kernel(AttendArgs a)
+__global__ __launch_bounds__(64 * WAVES, wgs_per_unit(D, FP8)) void attend_kernel(AttendArgs a)
 {
     // Columns of the matrix instructions: 16 heads with 8-bit values, whose weights are fp16; with bf16 values eight heads twice,
     // the upper ones with what rounding the weights to bf16 leaves, so that they have 16 bits.
@@ -89,123 +192,181 @@ __global__ __launch_bounds__(64 * WAVES) void attend_kernel(AttendArgs a)
     constexpr int W = D / 16 / SEG;                   // neighbouring elements of a segment that a lane has: 4 or 8
     constexpr int KB = FP8 ? D / 64 : D / 32;         // 16-byte pieces of a key that a lane loads
     constexpr int VR = FP8 ? W / 4 : W / 2;           // registers of a value's segment
-    __shared__ int32_t pages[CHUNK_MAX / 8 + 8];
+    constexpr int EL = FP8 ? 1 : 2;                   // bytes of an element
+    constexpr bool AHEAD = HB * D <= 128 || wgs_per_unit(D, FP8) == 1;    // registers for two tiles
+    __shared__ long long page_at[2][CHUNK / 8];             // where a piece's pages begin, in bytes; -1: not there
+    __shared__ RowInfo info[SCAN_ROWS];
+    __shared__ int scan[WAVES + 6];
     __shared__ float wave_m[WAVES][HB][16], wave_l[WAVES][HB][16];
     __shared__ f32x4 joined[WAVES / 2][HB * SEG * W][64];
 
     const CacheArgs &C = a.cache;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int c = lane & 15, g = lane >> 4;
-    unsigned idx = blockIdx.x;
-    const unsigned per_split = (unsigned)(C.kv_heads * a.blocks);
-    const int hb = (int)(idx % per_split);
-    idx /= per_split;
-    const int split = (int)(idx % (unsigned)a.splits), row = (int)(idx / (unsigned)a.splits);
-    const int kv_head = hb / a.blocks, first = (hb - kv_head * a.blocks) * COLS * HB;    // of the heads that share kv_head
-    const RowRange range = row_range(a, row);
-    const int begin = range.from + split * a.chunk;
-    const int end = begin + a.chunk < range.len ? begin + a.chunk : range.len;
-    if (begin >= range.len && split > 0) return;
-    const bool alone = range.len - range.from <= a.chunk;
+    const int per_row = C.kv_heads * a.blocks;
+    const int slot_bytes = (int)C.slot_stride * EL;
 
-    // this lane's head in every block of columns
-    int head[HB];
-    bool live[HB];
-#pragma unroll
-    for (int b = 0; b < HB; ++b) {
-        const int i = first + b * COLS + (c & (COLS - 1));
-        live[b] = i < a.group;
-        head[b] = kv_head * a.group + (live[b] ? i : 0);
+    Share share;
+    int info_row = 0;                                      // the row of info[0]
+    int parts_at = (int)blockIdx.x, chunk_slot = 0;
+    if (a.shares > 0) {
+        share = share_of(a, (int)blockIdx.x, per_row, info, scan);
+        if (threadIdx.x == 0) a.parts[parts_at].n = 0;
+        if (share.at >= share.until) return;
+    } else {
+        // workgroups by row, chunk and item: the items of a row at the same time, whose heads' places in a page are neighbours
+        const int of_row = (int)(blockIdx.x / (unsigned)per_row), item = (int)(blockIdx.x - (unsigned)of_row * (unsigned)per_row);
+        share.row = (int)((unsigned)of_row / (unsigned)a.splits);
+        const int split = of_row - share.row * a.splits;
+        const RowInfo here = row_info(a, share.row);
+        const int units = __builtin_amdgcn_readfirstlane(row_range(a, here.len).units);
+        if (split * a.chunk_units >= units) return;
+        if (threadIdx.x == 0) info[0] = here;
+        __syncthreads();
+        info_row = share.row;
+        share.row_at = 0;
+        share.length = a.chunk_units;
+        share.at = item * units + split * a.chunk_units;
+        share.until = item * units + ((split + 1) * a.chunk_units < units ? (split + 1) * a.chunk_units : units);
+        parts_at = share.row * per_row + item;
+        chunk_slot = parts_at * a.splits + split;
+        if (a.splits > 1 && split == 0 && threadIdx.x == 0)
+            a.parts[parts_at] = ItemParts{share.row, item, (units + a.chunk_units - 1) / a.chunk_units, chunk_slot, chunk_slot + 1, 1};
     }
+    const int share_begin = share.at;
 
-    // numbers of the chunk's pages
-    const int block0 = begin >> C.page_shift, nblocks = end > begin ? ((end - 1) >> C.page_shift) - block0 + 1 : 0;
-    for (int i = threadIdx.x; i < nblocks; i += 64 * WAVES) {
-        const int p = C.table[range.seq * C.table_stride + block0 + i];
-        pages[i] = p >= 0 && p < C.n_pages ? p : -1;
-    }
-    u32x4 q[HB][QK];
-#pragma unroll
-    for (int b = 0; b < HB; ++b) {
-        const uint16_t *src = a.q + row * a.q_stride + (long long)head[b] * D;
-#pragma unroll
-        for (int s = 0; s < QK; ++s) {
-            // the keys' pieces decide which elements a step has
-            const int at = FP8 ? 64 * (s >> 1) + 16 * g + 8 * (s & 1) : 32 * s + 8 * g;
-            q[b][s] = *reinterpret_cast<const u32x4 *>(src + at);
-            if (!live[b]) q[b][s] = u32x4{0, 0, 0, 0};
+    int segment_from = 0;                                  // the unit of its item that the segment began at
+    auto next_piece = [&]() __attribute__((always_inline)) {
+        Piece p;
+        p.row = share.row;
+        p.seq = __builtin_amdgcn_readfirstlane(info[p.row - info_row].seq);
+        const RowRange range = row_range(a, __builtin_amdgcn_readfirstlane(info[p.row - info_row].len));
+        const int in_row = share.at - share.row_at;
+        p.item = in_row / range.units;
+        p.kv_head = p.item / a.blocks;
+        p.first_head = (p.item - p.kv_head * a.blocks) * COLS * HB;
+        const int from = in_row - p.item * range.units, left = share.until - share.at;
+        int n = range.units - from < left ? range.units - from : left;
+        n = n < CHUNK / UNIT ? n : CHUNK / UNIT;
+        p.lo = range.lo;
+        p.begin = range.from + from * UNIT;
+        const bool over = from + n == range.units;         // the item ends here
+        p.end = over ? range.len : p.begin + n * UNIT;
+        p.first = share.at == share_begin || from == 0;
+        if (p.first) segment_from = from;
+        p.last = over || n == left;
+        p.alone = over && segment_from == 0;               // (of a chunk: segment_from is its first unit)
+        if (a.shares == 0) {
+            p.slot = chunk_slot;
+        } else {
+            // of the share's first segment, where an item goes on, and of its last one
+            p.slot = 2 * (int)blockIdx.x + (share.at - from + segment_from == share_begin ? 0 : 1);
+            if (over && segment_from > 0 && threadIdx.x == 0) {
+                // the item's first unit on the line of the cuts, and the share that has it
+                const int start = share.row_at + START * per_row * p.row + p.item * (range.units + START), w = (start + START) / share.length;
+                a.parts[blockIdx.x] = ItemParts{p.row, p.item, (int)blockIdx.x - w + 1, 2 * w + (w * share.length >= start ? 0 : 1), 2 * w + 2, 2};
+            }
         }
-    }
-    __syncthreads();
+        share.at += n;
+        if (in_row + n == range.units * per_row) { share.row_at = share.at; ++share.row; }
+        return p;
+    };
+    constexpr int ENTRIES = CHUNK / 8 / (64 * WAVES);      // of a piece's part of the table, per thread
+    int32_t entry[ENTRIES];
+    auto read_table = [&](const Piece &p) __attribute__((always_inline)) {
+        const int block0 = p.begin >> C.page_shift, blocks = p.end > p.begin ? ((p.end - 1) >> C.page_shift) - block0 + 1 : 0;
+        const int32_t *table = C.table + p.seq * C.table_stride + block0;
+#pragma unroll
+        for (int i = 0; i < ENTRIES; ++i) {
+            const int at = i * 64 * WAVES + (int)threadIdx.x;
+            entry[i] = at < blocks ? table[at] : -1;
+        }
+    };
+    auto keep_table = [&](int buffer) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < ENTRIES; ++i)
+            page_at[buffer][i * 64 * WAVES + threadIdx.x] = entry[i] >= 0 && entry[i] < C.n_pages ? entry[i] * C.page_stride * EL : -1ll;
+    };
 
-    const float k_scale = FP8 && C.k_scale ? C.k_scale[kv_head] : 1.f;
-    const float scale = a.scale * k_scale;
-    const uint8_t *kbase = static_cast<const uint8_t *>(C.k) + kv_head * C.head_stride * (FP8 ? 1 : 2);
-    const uint8_t *vbase = static_cast<const uint8_t *>(C.v) + kv_head * C.head_stride * (FP8 ? 1 : 2);
-    constexpr int EL = FP8 ? 1 : 2;
-
-    float m[HB], l[HB];
+    int head[HB], buffer = 0;
+    bool live[HB];
+    u32x4 q[HB][QK];
+    auto read_queries = [&](const Piece &p) __attribute__((always_inline)) {
+#pragma unroll
+        for (int b = 0; b < HB; ++b) {
+            const int i = p.first_head + b * COLS + (c & (COLS - 1));
+            const uint16_t *src = a.q + p.row * a.q_stride + (long long)(p.kv_head * a.group + (i < a.group ? i : 0)) * D;
+#pragma unroll
+            for (int s = 0; s < QK; ++s) {
+                // the keys' pieces decide which elements a step has
+                const int at = FP8 ? 64 * (s >> 1) + 16 * g + 8 * (s & 1) : 32 * s + 8 * g;
+                q[b][s] = *reinterpret_cast<const u32x4 *>(src + at);
+            }
+        }
+    };
+    float m[HB], l[HB], scale = 0.f;
     f32x4 acc[HB][SEG * W];
-#pragma unroll
-    for (int b = 0; b < HB; ++b) {
-        m[b] = LOWEST;
-        l[b] = 0.f;
-#pragma unroll
-        for (int e = 0; e < SEG * W; ++e) acc[b][e] = f32x4{0.f, 0.f, 0.f, 0.f};
-    }
-
-    for (int t0 = begin + wave * TILE; t0 < end; t0 += WAVES * TILE) {
-        // addresses: of the keys at t0 + c, t0 + 16 + c, of the values at t0 + 4 g .. and t0 + 16 + 4 g ..; positions past the
-        // end read the last one
-        bool whole = t0 >= range.lo && t0 + TILE <= end;
-        long long kat[2], vat[2][4];
-        bool vthere[2];
+    Piece cur;
+    // A tile in registers: pieces of the keys at t0 + c and t0 + 16 + c, of the values at t0 + 4 g .. + 3 and t0 + 16 + 4 g .. + 3 (a page
+    // has whole quads of positions).  Positions past the end are read from the last one's place, quads from the last one's.
+    struct Tile {
+        u32x4 k[2][KB];
+        uint32_t v[8][SEG][VR];
+        uint32_t there;                                // bits 0, 1: the quads' pages are there; 2: the keys' too
+    };
+    auto load = [&](Tile &t, const Piece &p, int t0) __attribute__((always_inline)) {
+        const int last = p.end - 1, block0 = p.begin >> C.page_shift;
+        const uint8_t *kbase = static_cast<const uint8_t *>(C.k) + p.kv_head * C.head_stride * EL + 16 * g;
+        const uint8_t *vbase = static_cast<const uint8_t *>(C.v) + p.kv_head * C.head_stride * EL + W * EL * c;
+        const long long *pages = page_at[buffer];
+        t.there = 4;
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
-            const int kp = t0 + 16 * s + c, kq = kp < end ? kp : end - 1;
-            const int page = pages[(kq >> C.page_shift) - block0];
-            whole = whole && page >= 0;
-            kat[s] = ((page < 0 ? 0 : page) * C.page_stride + (kq & C.page_mask) * C.slot_stride + (FP8 ? 16 : 8) * g) * EL;
-            const int vp = t0 + 16 * s + 4 * g, vq = vp < end ? vp : end - 1;
-            const int vpage = pages[(vq >> C.page_shift) - block0];
-            vthere[s] = vpage >= 0;
+            const int pos = t0 + 16 * s + c, at = pos < last ? pos : last;
+            long long page = pages[(at >> C.page_shift) - block0];
+            if (page < 0) { page = 0; t.there &= ~4u; }
+            const uint8_t *src = kbase + page + (uint32_t)((at & C.page_mask) * slot_bytes);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int at = vp + i < end ? vp + i : end - 1;
-                vat[s][i] = ((vpage < 0 ? 0 : vpage) * C.page_stride + (at & C.page_mask) * C.slot_stride + W * c) * EL;
-            }
+            for (int j = 0; j < KB; ++j) t.k[s][j] = *reinterpret_cast<const u32x4 *>(src + 64 * j);
         }
-        u32x4 k[2][KB];
 #pragma unroll
-        for (int s = 0; s < 2; ++s)
+        for (int s = 0; s < 2; ++s) {
+            const int pos = t0 + 16 * s + 4 * g, quad = last & ~3, at = pos < quad ? pos : quad;
+            long long page = pages[(at >> C.page_shift) - block0];
+            if (page < 0) page = 0; else t.there |= 1u << s;
+            const uint8_t *src = vbase + page + (uint32_t)((at & C.page_mask) * slot_bytes);
 #pragma unroll
-            for (int j = 0; j < KB; ++j)
-                k[s][j] = *reinterpret_cast<const u32x4 *>(kbase + kat[s] + 64 * j);
-        uint32_t v[8][SEG][VR];
+            for (int i = 0; i < 4; ++i, src += slot_bytes)
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
+                for (int e = 0; e < SEG; ++e) {
+                    uint32_t *v = t.v[4 * s + i][e];
+                    if constexpr (VR == 4) {
+                        const u32x4 x = *reinterpret_cast<const u32x4 *>(src + 128 * EL * e);
 #pragma unroll
-            for (int s = 0; s < SEG; ++s) {
-                const uint8_t *src = vbase + vat[i >> 2][i & 3] + 128 * EL * s;
-                if constexpr (VR == 4) {
-                    const u32x4 x = *reinterpret_cast<const u32x4 *>(src);
+                        for (int r = 0; r < VR; ++r) v[r] = x[r];
+                    } else if constexpr (VR == 2) {
+                        const u32x2 x = *reinterpret_cast<const u32x2 *>(src + 128 * EL * e);
 #pragma unroll
-                    for (int r = 0; r < VR; ++r) v[i][s][r] = x[r];
-                } else if constexpr (VR == 2) {
-                    const u32x2 x = *reinterpret_cast<const u32x2 *>(src);
-#pragma unroll
-                    for (int r = 0; r < VR; ++r) v[i][s][r] = x[r];
-                } else {
-                    v[i][s][0] = *reinterpret_cast<const uint32_t *>(src);
+                        for (int r = 0; r < VR; ++r) v[r] = x[r];
+                    } else {
+                        v[0] = *reinterpret_cast<const uint32_t *>(src + 128 * EL * e);
+                    }
                 }
-            }
-        const bool full = __ballot(!whole) == 0;
+        }
+    };
+    auto step = [&](Tile &t, int t0) __attribute__((always_inline)) {
+        auto &k = t.k;
+        auto &v = t.v;
+        const bool full = t0 >= cur.lo && t0 + TILE <= cur.end && __ballot(t.there != 7u) == 0;
+        auto seen = [&](int i) {
+            const int p = t0 + 16 * (i >> 2) + 4 * g + (i & 3);
+            return p >= cur.lo && p < cur.end && (t.there >> (i >> 2) & 1u);
+        };
         if (!full) {
             // what masked positions hold must not meet a weight of 0: NaN and infinities would stay
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const int p = t0 + 16 * (i >> 2) + 4 * g + (i & 3);
-                const bool in = p >= range.lo && p < end && vthere[i >> 2];
+                const bool in = seen(i);
 #pragma unroll
                 for (int s = 0; s < SEG; ++s)
 #pragma unroll
@@ -234,10 +395,7 @@ __global__ __launch_bounds__(64 * WAVES) void attend_kernel(AttendArgs a)
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 y[i] = x[i >> 2][i & 3] * scale;
-                if (!full) {
-                    const int p = t0 + 16 * (i >> 2) + 4 * g + (i & 3);
-                    y[i] = p >= range.lo && p < end && vthere[i >> 2] ? y[i] : -__builtin_inff();
-                }
+                if (!full) y[i] = seen(i) ? y[i] : -__builtin_inff();
                 top = fmaxf(top, y[i]);
             }
             top = fmaxf(top, __shfl_xor(top, 16));
@@ -303,93 +461,160 @@ __global__ __launch_bounds__(64 * WAVES) void attend_kernel(AttendArgs a)
                     }
                 }
             }
-    }
+    };
 
-    // the waves' maxima and sums, then their accumulators in a tree
+    auto join_waves = [&]() __attribute__((always_inline)) {
+        // the waves' maxima and sums, then their accumulators in a tree
 #pragma unroll
-    for (int b = 0; b < HB; ++b) {
-        l[b] += __shfl_xor(l[b], 16);
-        l[b] += __shfl_xor(l[b], 32);
-        if (g == 0) { wave_m[wave][b][c] = m[b]; wave_l[wave][b][c] = l[b]; }
-    }
-    __syncthreads();
-    float total[HB], top[HB];
-#pragma unroll
-    for (int b = 0; b < HB; ++b) {
-        top[b] = LOWEST;
-#pragma unroll
-        for (int w = 0; w < WAVES; ++w) top[b] = fmaxf(top[b], wave_m[w][b][c]);
-        total[b] = 0.f;
-#pragma unroll
-        for (int w = 0; w < WAVES; ++w) total[b] += wave_l[w][b][c] * __builtin_amdgcn_exp2f(wave_m[w][b][c] - top[b]);
-        const float mine = __builtin_amdgcn_exp2f(m[b] - top[b]);
-#pragma unroll
-        for (int e = 0; e < SEG * W; ++e) acc[b][e] *= mine;
-    }
-#pragma unroll
-    for (int half = WAVES / 2; half >= 1; half /= 2) {
-        if (wave >= half && wave < 2 * half)
-#pragma unroll
-            for (int b = 0; b < HB; ++b)
-#pragma unroll
-                for (int e = 0; e < SEG * W; ++e) joined[wave - half][b * SEG * W + e][lane] = acc[b][e];
+        for (int b = 0; b < HB; ++b) {
+            l[b] += __shfl_xor(l[b], 16);
+            l[b] += __shfl_xor(l[b], 32);
+            if (g == 0) { wave_m[wave][b][c] = m[b]; wave_l[wave][b][c] = l[b]; }
+        }
         __syncthreads();
-        if (wave < half)
+        float total[HB], top[HB];
 #pragma unroll
-            for (int b = 0; b < HB; ++b)
+        for (int b = 0; b < HB; ++b) {
+            top[b] = LOWEST;
 #pragma unroll
-                for (int e = 0; e < SEG * W; ++e) acc[b][e] += joined[wave][b * SEG * W + e][lane];
-        __syncthreads();
-    }
-    if (wave != 0) return;
-
-    const float v_scale = FP8 && C.v_scale ? C.v_scale[kv_head] : 1.f;
+            for (int w = 0; w < WAVES; ++w) top[b] = fmaxf(top[b], wave_m[w][b][c]);
+            total[b] = 0.f;
 #pragma unroll
-    for (int b = 0; b < HB; ++b) {
-        if constexpr (!FP8)
+            for (int w = 0; w < WAVES; ++w) total[b] += wave_l[w][b][c] * __builtin_amdgcn_exp2f(wave_m[w][b][c] - top[b]);
+            const float mine = __builtin_amdgcn_exp2f(m[b] - top[b]);
 #pragma unroll
-            for (int e = 0; e < SEG * W; ++e)
+            for (int e = 0; e < SEG * W; ++e) acc[b][e] *= mine;
+        }
 #pragma unroll
-                for (int r = 0; r < 4; ++r) acc[b][e][r] += __shfl_xor(acc[b][e][r], 8);
-        if (!live[b] || c >= COLS) continue;
-        // this lane: elements 128 s + W (4 g + r) + e
-        const size_t rh = (size_t)row * a.heads + head[b];
-        if (alone) {
-            const float by = total[b] > 0.f || total[b] != total[b] ? v_scale / total[b] : 0.f;
-            uint16_t *o = a.out + row * a.out_stride + (long long)head[b] * D;
+        for (int half = WAVES / 2; half >= 1; half /= 2) {
+            if (wave >= half && wave < 2 * half)
 #pragma unroll
-            for (int s = 0; s < SEG; ++s)
+                for (int b = 0; b < HB; ++b)
 #pragma unroll
-                for (int r = 0; r < 4; ++r)
+                    for (int e = 0; e < SEG * W; ++e) joined[wave - half][b * SEG * W + e][lane] = acc[b][e];
+            __syncthreads();
+            if (wave < half)
 #pragma unroll
-                    for (int e = 0; e < W; e += 4) {
-                        const u32x2 x = {pack_bf16x2(acc[b][s * W + e][r] * by, acc[b][s * W + e + 1][r] * by),
-                                         pack_bf16x2(acc[b][s * W + e + 2][r] * by, acc[b][s * W + e + 3][r] * by)};
-                        *reinterpret_cast<u32x2 *>(o + 128 * s + W * (4 * g + r) + e) = x;
-                    }
-            if (a.lse && g == 0)
-                a.lse[rh] = total[b] > 0.f || total[b] != total[b] ? (top[b] + __builtin_amdgcn_logf(total[b])) * LN2 : -__builtin_inff();
-        } else {
-            const size_t at = rh * a.splits + split;
-            float *o = a.part + at * D;
+                for (int b = 0; b < HB; ++b)
 #pragma unroll
-            for (int s = 0; s < SEG; ++s)
+                    for (int e = 0; e < SEG * W; ++e) acc[b][e] += joined[wave][b * SEG * W + e][lane];
+            __syncthreads();
+        }
+        if (wave == 0) {
+        const float v_scale = FP8 && C.v_scale ? C.v_scale[cur.kv_head] : 1.f;
 #pragma unroll
-                for (int r = 0; r < 4; ++r)
+        for (int b = 0; b < HB; ++b) {
+            if constexpr (!FP8)
 #pragma unroll
-                    for (int e = 0; e < W; e += 4)
-                        *reinterpret_cast<f32x4 *>(o + 128 * s + W * (4 * g + r) + e) =
-                            f32x4{acc[b][s * W + e][r], acc[b][s * W + e + 1][r], acc[b][s * W + e + 2][r], acc[b][s * W + e + 3][r]};
-            if (g == 0) {
-                a.part_ml[2 * at] = top[b];
-                a.part_ml[2 * at + 1] = total[b];
+                for (int e = 0; e < SEG * W; ++e)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) acc[b][e][r] += __shfl_xor(acc[b][e][r], 8);
+            if (!live[b] || c >= COLS) continue;
+            // this lane: elements 128 s + W (4 g + r) + e
+            const size_t rh = (size_t)cur.row * a.heads + head[b];
+            if (cur.alone) {
+                const float by = total[b] > 0.f || total[b] != total[b] ? v_scale / total[b] : 0.f;
+                uint16_t *o = a.out + cur.row * a.out_stride + (long long)head[b] * D;
+#pragma unroll
+                for (int s = 0; s < SEG; ++s)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r)
+#pragma unroll
+                        for (int e = 0; e < W; e += 4) {
+                            const u32x2 x = {pack_bf16x2(acc[b][s * W + e][r] * by, acc[b][s * W + e + 1][r] * by),
+                                             pack_bf16x2(acc[b][s * W + e + 2][r] * by, acc[b][s * W + e + 3][r] * by)};
+                            *reinterpret_cast<u32x2 *>(o + 128 * s + W * (4 * g + r) + e) = x;
+                        }
+                if (a.lse && g == 0)
+                    a.lse[rh] = total[b] > 0.f || total[b] != total[b] ? (top[b] + __builtin_amdgcn_logf(total[b])) * LN2 : -__builtin_inff();
+            } else {
+                const size_t at = (size_t)cur.slot * a.per_wg + b * COLS + c;
+                float *o = a.part + at * D;
+#pragma unroll
+                for (int s = 0; s < SEG; ++s)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r)
+#pragma unroll
+                        for (int e = 0; e < W; e += 4)
+                            *reinterpret_cast<f32x4 *>(o + 128 * s + W * (4 * g + r) + e) =
+                                f32x4{acc[b][s * W + e][r], acc[b][s * W + e + 1][r], acc[b][s * W + e + 2][r], acc[b][s * W + e + 3][r]};
+                if (g == 0) {
+                    a.part_ml[2 * at] = top[b];
+                    a.part_ml[2 * at + 1] = total[b];
+                }
             }
         }
+        }
+    };
+
+    // While a piece is computed, the next one's part of the table is on its way; its first tiles and queries are while a segment's sums
+    // are joined.  Two tiles of a wave are in flight where they fit in the registers.
+    constexpr int STEP = WAVES * TILE;
+    Tile x;
+    cur = next_piece();
+    read_table(cur);
+    read_queries(cur);
+    keep_table(0);
+    __syncthreads();
+    if (cur.begin + wave * TILE < cur.end) load(x, cur, cur.begin + wave * TILE);
+    for (;;) {
+        if (cur.first) {
+            scale = a.scale * (FP8 && C.k_scale ? C.k_scale[cur.kv_head] : 1.f);
+#pragma unroll
+            for (int b = 0; b < HB; ++b) {
+                const int i = cur.first_head + b * COLS + (c & (COLS - 1));
+                live[b] = i < a.group;
+                head[b] = cur.kv_head * a.group + i;
+                m[b] = LOWEST;
+                l[b] = 0.f;
+#pragma unroll
+                for (int e = 0; e < SEG * W; ++e) acc[b][e] = f32x4{0.f, 0.f, 0.f, 0.f};
+            }
+        }
+        const bool more = share.at < share.until;
+        Piece next = cur;
+        if (more) {
+            next = next_piece();
+            read_table(next);
+        }
+        int t0 = cur.begin + wave * TILE;
+        if constexpr (AHEAD) {
+            Tile y;
+            if (t0 < cur.end)
+                for (;;) {
+                    const bool then = t0 + STEP < cur.end;
+                    if (then) load(y, cur, t0 + STEP);
+                    step(x, t0);
+                    if (!then) break;
+                    t0 += STEP;
+                    const bool again = t0 + STEP < cur.end;
+                    if (again) load(x, cur, t0 + STEP);
+                    step(y, t0);
+                    if (!again) break;
+                    t0 += STEP;
+                }
+        } else {
+            while (t0 < cur.end) {
+                step(x, t0);
+                t0 += STEP;
+                if (t0 < cur.end) load(x, cur, t0);
+            }
+        }
+        if (more) {
+            buffer ^= 1;
+            keep_table(buffer);
+            __syncthreads();
+            if (next.first) read_queries(next);
+            if (next.begin + wave * TILE < next.end) load(x, next, next.begin + wave * TILE);
+        }
+        if (cur.last) join_waves();
+        if (!more) return;
+        cur = next;
     }
 }
 
-// Joins the chunks of the rows that have several: one workgroup per row and head.  A group of D / 4 lanes reads the
-// sums of a chunk, 16 bytes a lane; the groups take the chunks in turn, four loads of a lane in flight, and meet in LDS.
+// Joins the parts of an item that is in several workgroups: a workgroup per entry of `parts` and head.  A group of D / 4 lanes reads
+// the sums of a part, 16 bytes a lane; the groups take the parts in turn, four loads of a lane in flight, and meet in LDS.
 template <int D, bool FP8>
 __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a)
 {
@@ -397,21 +622,23 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a)
     __shared__ float weight[BATCH], wave_x[4];
     __shared__ f32x4 sums[GROUPS][LANES];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int row = (int)(blockIdx.x / (unsigned)a.heads), head = (int)(blockIdx.x - (unsigned)row * (unsigned)a.heads);
-    const RowRange range = row_range(a, row);
-    const int n = (range.len - range.from + a.chunk - 1) / a.chunk;
+    const int heads = a.group < a.per_wg ? a.group : a.per_wg;
+    const int entry = (int)(blockIdx.x / (unsigned)heads), i = (int)(blockIdx.x - (unsigned)entry * (unsigned)heads);
+    const ItemParts item = a.parts[entry];
+    const int n = item.n;
     if (n < 2) return;
-    const size_t rh = (size_t)row * a.heads + head;
-    const float *ml = a.part_ml + 2 * rh * a.splits;
+    const int kv_head = item.item / a.blocks, of_group = (item.item - kv_head * a.blocks) * a.per_wg + i;
+    if (of_group >= a.group) return;
+    const int head = kv_head * a.group + of_group;
+    auto slot = [&](int s) { return (size_t)(s == 0 ? item.first : item.next + (s - 1) * item.step) * a.per_wg + i; };
     float top = LOWEST;
-    for (int s = tid; s < n; s += 256) top = fmaxf(top, ml[2 * s]);
+    for (int s = tid; s < n; s += 256) top = fmaxf(top, a.part_ml[2 * slot(s)]);
 #pragma unroll
     for (int o = 32; o >= 1; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
     if (lane == 0) wave_x[wave] = top;
     __syncthreads();
     top = fmaxf(fmaxf(wave_x[0], wave_x[1]), fmaxf(wave_x[2], wave_x[3]));
     const int at = tid % LANES, group = tid / LANES;
-    const f32x4 *part = reinterpret_cast<const f32x4 *>(a.part + rh * a.splits * D) + at;
     f32x4 sum = {0.f, 0.f, 0.f, 0.f};
     float total = 0.f;
     for (int s0 = 0; s0 < n; s0 += BATCH) {
@@ -419,20 +646,22 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a)
         __syncthreads();                                       // (also: everyone has read wave_x)
         float w = 0.f;
         if (tid < here) {
-            w = __builtin_amdgcn_exp2f(ml[2 * (s0 + tid)] - top);
-            total += w * ml[2 * (s0 + tid) + 1];
+            const float *ml = a.part_ml + 2 * slot(s0 + tid);
+            w = __builtin_amdgcn_exp2f(ml[0] - top);
+            total += w * ml[1];
         }
         weight[tid] = w;
         __syncthreads();
-        for (int i = group; i < here; i += 4 * GROUPS) {
+        for (int k0 = group; k0 < here; k0 += 4 * GROUPS) {
             f32x4 x[4];
 #pragma unroll
-            for (int k = 0; k < 4; ++k) x[k] = part[(size_t)(s0 + (i + k * GROUPS < here ? i + k * GROUPS : i)) * LANES];
-#pragma unroll
             for (int k = 0; k < 4; ++k) {
-                const float wk = i + k * GROUPS < here ? weight[i + k * GROUPS] : 0.f;
-                if (i + k * GROUPS < here) sum += x[k] * wk;
+                const int s = k0 + k * GROUPS < here ? k0 + k * GROUPS : k0;
+                x[k] = *reinterpret_cast<const f32x4 *>(a.part + slot(s0 + s) * D + 4 * at);
             }
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (k0 + k * GROUPS < here) sum += x[k] * weight[k0 + k * GROUPS];
         }
     }
 #pragma unroll
@@ -445,68 +674,75 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a)
 #pragma unroll
     for (int k = 1; k < GROUPS; ++k) sum += sums[k][at];
     const bool any = total > 0.f || total != total;
-    const float v_scale = FP8 && a.cache.v_scale ? a.cache.v_scale[head / a.group] : 1.f;
+    const float v_scale = FP8 && a.cache.v_scale ? a.cache.v_scale[kv_head] : 1.f;
     const float by = any ? v_scale / total : 0.f;
-    uint16_t *o = a.out + row * a.out_stride + (long long)head * D + 4 * at;
+    uint16_t *o = a.out + item.row * a.out_stride + (long long)head * D + 4 * at;
     *reinterpret_cast<u32x2 *>(o) = u32x2{pack_bf16x2(sum[0] * by, sum[1] * by), pack_bf16x2(sum[2] * by, sum[3] * by)};
-    if (a.lse && tid == 0) a.lse[rh] = any ? (top + __builtin_amdgcn_logf(total)) * LN2 : -__builtin_inff();
+    if (a.lse && tid == 0) a.lse[(size_t)item.row * a.heads + head] = any ? (top + __builtin_amdgcn_logf(total)) * LN2 : -__builtin_inff();
 }
 
+// How a call is cut: column blocks of a workgroup, workgroups' worth of heads per key head, heads of a workgroup, chunks or shares.
+struct AttendPlan {
+    int hb, blocks, per_wg, splits, chunk_units, shares, entries;
+    long long grid;
+    size_t part_bytes, ml_bytes, parts_bytes;
+};
+
 template <int D, bool FP8>
-hipError_t launch_attend(const AttendArgs &a, int hb, hipStream_t stream)
+hipError_t launch_attend(const AttendArgs &a, const AttendPlan &p, hipStream_t stream)
 {
-    const unsigned grid = (unsigned)a.rows * (unsigned)a.splits * (unsigned)(a.cache.kv_heads * a.blocks);
+    auto kernel = attend_kernel<D, FP8, 1>;
+    if constexpr (D <= 128)
+        if (p.hb == 2) kernel = attend_kernel<D, FP8, 2>;
     trace_before(KID_ATTEND, stream);
-    if constexpr (D <= 128) {
-        if (hb == 2)
-            hipLaunchKernelGGL((attend_kernel<D, FP8, 2>), dim3(grid), dim3(64 * WAVES), 0, stream, a);
-        else
-            hipLaunchKernelGGL((attend_kernel<D, FP8, 1>), dim3(grid), dim3(64 * WAVES), 0, stream, a);
-    } else {
-        hipLaunchKernelGGL((attend_kernel<D, FP8, 1>), dim3(grid), dim3(64 * WAVES), 0, stream, a);
-    }
+    hipLaunchKernelGGL(kernel, dim3((unsigned)p.grid), dim3(64 * WAVES), 0, stream, a);
     trace_after(KID_ATTEND, stream);
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess || a.splits == 1) return e;
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess || p.entries == 0) return e;
     trace_before(KID_ATTEND_JOIN, stream);
-    hipLaunchKernelGGL((attend_join_kernel<D, FP8>), dim3((unsigned)a.rows * (unsigned)a.heads), dim3(256), 0, stream, a);
+    hipLaunchKernelGGL((attend_join_kernel<D, FP8>), dim3((unsigned)(p.entries * (a.group < p.per_wg ? a.group : p.per_wg))),
+                       dim3(256), 0, stream, a);
     trace_after(KID_ATTEND_JOIN, stream);
     return hipGetLastError();
 }
-
-// How a call is cut: column blocks of a workgroup, workgroups per key head, chunk and chunks of the longest row.
-struct AttendPlan {
-    int hb, blocks, chunk, splits;
-    size_t part_bytes, ml_bytes;
-};
 
 AttendPlan attend_plan(const peqa_kv_cache *C, int rows, int heads, int max_len, int window)
 {
     AttendPlan p{};
     const int group = heads / C->kv_heads, cols = C->dtype == PEQA_CACHE_FP8 ? 16 : 8;
     p.hb = C->head_dim <= 128 && group > cols ? 2 : 1;
-    p.blocks = (group + cols * p.hb - 1) / (cols * p.hb);
-    const long long span = window > 0 && (long long)window + TILE - 1 < max_len ? (long long)window + TILE - 1 : max_len;
-    const long long items = (long long)rows * C->kv_heads * p.blocks;
-    // workgroups for every unit several times over, but no chunk under two tiles a wave
-#ifndef WANT
-#define WANT 8
-#endif
-    long long want = (PLAN_UNITS * (long long)WANT + items - 1) / items;
-    long long chunk = (span + want - 1) / want;
-#ifndef LEAST
-#define LEAST 2
-#endif
-    const long long least = LEAST * WAVES * TILE;
-    if (chunk < least) chunk = least;
-    if (chunk > CHUNK_MAX) chunk = CHUNK_MAX;
-    p.chunk = (int)((chunk + TILE * WAVES - 1) / (TILE * WAVES) * (TILE * WAVES));
-    p.splits = (int)((span + p.chunk - 1) / p.chunk);
-    if (p.splits < 1) p.splits = 1;
-    if (p.splits > 1) {
-        const size_t parts = (size_t)rows * (size_t)heads * (size_t)p.splits;
-        p.part_bytes = round256(parts * (size_t)C->head_dim * sizeof(float));
-        p.ml_bytes = round256(parts * 2 * sizeof(float));
+    p.per_wg = cols * p.hb;
+    p.blocks = (group + p.per_wg - 1) / p.per_wg;
+    const long long span = window > 0 && (long long)window + UNIT - 1 < max_len ? (long long)window + UNIT - 1 : max_len;
+    const long long items = (long long)rows * C->kv_heads * p.blocks, units = items * ((span + UNIT - 1) / UNIT + START);
+    p.grid = items;
+    p.splits = 1;
+    p.chunk_units = (int)((span + UNIT - 1) / UNIT);
+    if (p.chunk_units < 1) p.chunk_units = 1;
+    const int fit = wgs_per_unit(C->head_dim, C->dtype == PEQA_CACHE_FP8) * PLAN_UNITS;
+    long long slots = 0;
+    if (span <= 512 || items >= 16 * fit) {
+        // whole items
+    } else if (rows > 1 && rows <= SCAN_ROWS && units >= 48ll * fit && units < (1ll << 30)) {
+        p.shares = fit;
+        p.grid = p.entries = fit;
+        slots = 2 * fit;
+    } else {
+        // one row: as many chunks as there is room for workgroups; else four times as many, as rows may be of different lengths
+        long long chunk = span * items / (rows == 1 ? fit : 4 * fit);
+        chunk = chunk < 512 ? 512 : chunk;
+        p.chunk_units = (int)((chunk + UNIT - 1) / UNIT);
+        p.splits = (int)((span + p.chunk_units * UNIT - 1) / (p.chunk_units * UNIT));
+        p.grid = items * p.splits;
+        if (p.splits > 1) {
+            p.entries = (int)items;                            // (under 16 fit)
+            slots = items * p.splits;
+        }
+    }
+    if (slots > 0) {
+        p.part_bytes = round256((size_t)(slots * p.per_wg) * (size_t)C->head_dim * sizeof(float));
+        p.ml_bytes = round256((size_t)(slots * p.per_wg) * 2 * sizeof(float));
+        p.parts_bytes = round256((size_t)p.entries * sizeof(ItemParts));
     }
     return p;
 }
@@ -519,8 +755,8 @@ peqa_status check_attend(const peqa_kv_cache *C, int32_t rows, int32_t heads, in
     if ((int64_t)max_len > (int64_t)C->n_blocks * C->page_size) return PEQA_ERR_SHAPE;
     if (window < 0) return PEQA_ERR_PARAM;
     const AttendPlan p = attend_plan(C, rows, heads, max_len, window);
-    const int64_t wgs = (int64_t)C->kv_heads * p.blocks * p.splits;
-    if (wgs > INT32_MAX / rows || (int64_t)rows * heads > INT32_MAX) return PEQA_ERR_SHAPE;
+    if ((int64_t)C->kv_heads * p.blocks * ((max_len + UNIT - 1) / UNIT + START) > (1 << 30)) return PEQA_ERR_SHAPE;    // units of a row
+    if (p.grid > INT32_MAX / 64) return PEQA_ERR_SHAPE;
     return PEQA_OK;
 }
 
@@ -533,7 +769,7 @@ size_t peqa_paged_attention_workspace_bytes(const peqa_kv_cache *C, int32_t rows
 {
     if (peqa::check_attend(C, rows, heads, max_len, window) != PEQA_OK) return 0;
     const peqa::AttendPlan p = peqa::attend_plan(C, rows, heads, max_len, window);
-    const size_t bytes = p.part_bytes + p.ml_bytes;
+    const size_t bytes = p.part_bytes + p.ml_bytes + p.parts_bytes;
     return bytes ? bytes : 256;                                // (0 would read as "invalid")
 }
 
@@ -550,27 +786,32 @@ peqa_status peqa_paged_attention(const peqa_kv_cache *C, int32_t rows, int32_t h
     if (!aligned16(q) || !aligned16(out) || q_stride % 8 || out_stride % 8) return PEQA_ERR_ALIGN;
     if ((reinterpret_cast<uintptr_t>(lens) | reinterpret_cast<uintptr_t>(seq) | reinterpret_cast<uintptr_t>(lse)) & 3) return PEQA_ERR_ALIGN;
     const peqa::AttendPlan p = peqa::attend_plan(C, rows, heads, max_len, window);
-    if (p.splits > 1) {
-        if (!workspace || workspace_bytes < p.part_bytes + p.ml_bytes) return PEQA_ERR_WORKSPACE;
+    if (p.entries > 0) {
+        if (!workspace || workspace_bytes < p.part_bytes + p.ml_bytes + p.parts_bytes) return PEQA_ERR_WORKSPACE;
         if (!aligned16(workspace)) return PEQA_ERR_ALIGN;
     }
     peqa::AttendArgs a{};
     a.cache = peqa::cache_args(C);
     a.q = q; a.lens = lens; a.seq = seq; a.out = out; a.lse = lse;
-    a.part = static_cast<float *>(workspace);
-    a.part_ml = p.splits > 1 ? reinterpret_cast<float *>(static_cast<char *>(workspace) + p.part_bytes) : nullptr;
+    if (p.entries > 0) {
+        char *w = static_cast<char *>(workspace);
+        a.part = reinterpret_cast<float *>(w);
+        a.part_ml = reinterpret_cast<float *>(w + p.part_bytes);
+        a.parts = reinterpret_cast<peqa::ItemParts *>(w + p.part_bytes + p.ml_bytes);
+    }
     a.q_stride = q_stride; a.out_stride = out_stride;
     a.scale = scale * peqa::LOG2E;
     a.rows = rows; a.heads = heads; a.group = heads / C->kv_heads;
     a.max_len = max_len; a.window = window;
-    a.chunk = p.chunk; a.splits = p.splits; a.blocks = p.blocks;
+    a.blocks = p.blocks; a.per_wg = p.per_wg;
+    a.splits = p.splits; a.chunk_units = p.chunk_units; a.shares = p.shares;
     hipStream_t s = static_cast<hipStream_t>(stream);
     const bool fp8 = C->dtype == PEQA_CACHE_FP8;
     hipError_t e;
     switch (C->head_dim) {
-    case 64: e = fp8 ? peqa::launch_attend<64, true>(a, p.hb, s) : peqa::launch_attend<64, false>(a, p.hb, s); break;
-    case 128: e = fp8 ? peqa::launch_attend<128, true>(a, p.hb, s) : peqa::launch_attend<128, false>(a, p.hb, s); break;
-    default: e = fp8 ? peqa::launch_attend<256, true>(a, p.hb, s) : peqa::launch_attend<256, false>(a, p.hb, s); break;
+    case 64: e = fp8 ? peqa::launch_attend<64, true>(a, p, s) : peqa::launch_attend<64, false>(a, p, s); break;
+    case 128: e = fp8 ? peqa::launch_attend<128, true>(a, p, s) : peqa::launch_attend<128, false>(a, p, s); break;
+    default: e = fp8 ? peqa::launch_attend<256, true>(a, p, s) : peqa::launch_attend<256, false>(a, p, s); break;
     }
     return dev_status(e);
 }

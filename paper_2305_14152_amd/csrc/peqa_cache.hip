@@ -173,6 +173,7 @@ peqa_status peqa_check_cache(const peqa_kv_cache *C)
     if ((int64_t)C->n_blocks * C->page_size > INT32_MAX || C->table_stride < C->n_blocks) return PEQA_ERR_SHAPE;
     if (C->page_stride < 0 || C->head_stride < 0 || C->slot_stride < C->head_dim) return PEQA_ERR_SHAPE;
     const int64_t unit = C->dtype == PEQA_CACHE_FP8 ? 16 : 8;
+    if (C->slot_stride > (INT32_MAX / 2) / C->page_size) return PEQA_ERR_SHAPE;    // a head's slots of a page: 32-bit offsets in kernels
     if (!aligned16(C->k) || !aligned16(C->v) || C->page_stride % unit || C->head_stride % unit || C->slot_stride % unit)
         return PEQA_ERR_ALIGN;
     if ((reinterpret_cast<uintptr_t>(C->table) | reinterpret_cast<uintptr_t>(C->k_scale) | reinterpret_cast<uintptr_t>(C->v_scale)) & 3)

@@ -126,7 +126,7 @@ def check_attention(torch, peqa, cache, q, lens, max_len, window=0, seq=None, sc
     got_lse = lse.cpu().double().numpy()
     empty = np.isinf(want_lse)
     assert (got_lse[empty] == -math.inf).all()
-    assert (np.abs(got_lse - want_lse)[~empty] <= 2.0 ** -14 * (1 + np.abs(want_lse[~empty]))).all()
+    assert (np.abs(got_lse[~empty] - want_lse[~empty]) <= 2.0 ** -14 * (1 + np.abs(want_lse[~empty]))).all()
     assert (wide[:, heads * dim:] == 7.0).all()
     peqa.paged_attention(cache, q, dev(lens), max_len, scale, out, ws, room, seq=dev(seq), window=window)      # without lse: the same bits
     assert torch.equal(out, first)
@@ -174,6 +174,29 @@ def test_split_and_joined(env, fp8, heads, kv_heads, dim, lens):
     q = torch.randn((len(lens), heads, dim), generator=gen).to(torch.bfloat16).cuda()
     check_attention(torch, peqa, cache, q, lens, max(lens), fp8=fp8)
     check_attention(torch, peqa, cache, q, lens, max(lens), window=5000, fp8=fp8)
+
+
+@pytest.mark.parametrize("fp8,heads,kv_heads,dim,rows,most,window", [
+    (False, 8, 8, 128, 20, 16384, 0), (True, 32, 4, 128, 40, 16384, 0), (False, 24, 2, 64, 50, 32768, 0), (True, 34, 2, 256, 60, 16384, 0),
+    (False, 5, 5, 256, 30, 16384, 0), (False, 4, 4, 128, 1000, 2048, 0), (True, 4, 4, 64, 300, 4096, 1500), (False, 18, 1, 128, 200, 16384, 0),
+])
+def test_equal_shares(env, fp8, heads, kv_heads, dim, rows, most, window):
+    """Bounds that make a launch of equal shares of all rows: few long rows among short and empty ones, in every order of lengths."""
+    torch, peqa = env
+    print("shares", fp8, heads, kv_heads, dim, rows, most, window, flush=True)
+    gen = torch.Generator().manual_seed(rows + dim)
+    lens = [int(n) for n in torch.randint(0, 200, (rows,), generator=gen)]
+    for r, n in ((0, 0), (1, 1), (2, min(most, 4500)), (3, 64), (rows // 2, min(most, 9000)), (rows - 2, 2047), (rows - 1, 0)):
+        lens[r] = n
+    page = 64
+    cache = make_cache(torch, peqa, gen, lens, kv_heads, dim, page, fp8)
+    k, v, table, ks, vs = cache.tensors
+    wide = torch.full((rows, most // page), -1, dtype=torch.int32, device="cuda")
+    wide[:, :table.shape[1]] = table
+    cache = peqa.kv_cache(k, v, wide, ks, vs)
+    q = torch.randn((rows, heads, dim), generator=gen).to(torch.bfloat16).cuda()
+    check_attention(torch, peqa, cache, q, lens, most, window=window, fp8=fp8)
+    check_attention(torch, peqa, cache, q, [min(n, 5) for n in lens], most, window=window, fp8=fp8)     # nothing but short rows
 
 
 def test_rows_of_one_sequence_and_rows_of_none(env):
