@@ -88,17 +88,46 @@ template <bool F32> __device__ __forceinline__ void floats(const Raw &w, float x
         }
     }
 }
-// Any vector of a row, what is not the row's as -inf; whole vectors by 16-byte loads.
-template <bool F32> __device__ __forceinline__ void read_vector(const Row<F32> &r, int v, int V, float x[8])
+template <bool F32> __device__ __forceinline__ Raw nothing()
 {
-    if (!r.edge(v, V)) {
-        floats<F32>(load_vector<F32>(r, v), x);
-        return;
+    constexpr uint32_t inf = F32 ? 0xFF800000u : 0xFF80FF80u;
+    Raw w;
+    w.a = u32x4{inf, inf, inf, inf};
+    if constexpr (F32) w.b = w.a;
+    return w;
+}
+// Element i of a vector, i not a constant.
+template <bool F32> __device__ __forceinline__ float element(const Raw &w, int i)
+{
+    if constexpr (F32) {
+        const uint32_t lo = i & 2 ? (i & 1 ? w.a[3] : w.a[2]) : (i & 1 ? w.a[1] : w.a[0]);
+        const uint32_t hi = i & 2 ? (i & 1 ? w.b[3] : w.b[2]) : (i & 1 ? w.b[1] : w.b[0]);
+        return __uint_as_float(i & 4 ? hi : lo);
     }
+    const uint32_t pair = i & 4 ? (i & 2 ? w.a[3] : w.a[2]) : (i & 2 ? w.a[1] : w.a[0]);
+    return i & 1 ? bf16_hi(pair) : bf16_lo(pair);
+}
+// A vector that is not all the row's, the rest of it as -inf; nothing but the row's elements is read.
+template <bool F32> __device__ __forceinline__ Raw read_edge(const Row<F32> &r, int v, int V)
+{
+    uint32_t x[8];
+#pragma unroll
     for (int i = 0; i < 8; ++i) {
-        const int j = 8 * v + i - r.off;
-        x[i] = j >= 0 && j < V ? r.one(j) : -__builtin_inff();
+        const int j = 8 * v + i - r.off, inside = j < 0 ? 0 : j < V ? j : V - 1;
+        const uint32_t bits = __float_as_uint(r.one(inside));
+        x[i] = j == inside ? bits : 0xFF800000u;
     }
+    Raw w;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if constexpr (F32) { w.a[i] = x[i]; w.b[i] = x[4 + i]; }
+        else w.a[i] = x[2 * i] >> 16 | (x[2 * i + 1] & 0xFFFF0000u);
+    }
+    return w;
+}
+template <bool F32> __device__ __forceinline__ Raw read_vector(const Row<F32> &r, int v, int V)
+{
+    return r.edge(v, V) ? read_edge<F32>(r, v, V) : load_vector<F32>(r, v);
 }
 
 // Order of the alternatives as unsigned numbers: by logit, then the lower index first.  -0 counts as 0, NaN as -inf.
@@ -152,75 +181,159 @@ __device__ __forceinline__ Answer answer_of(float m, float s, float u)
 }
 __device__ __forceinline__ float logp_of(const Answer &r, float x) { return r.lse == -__builtin_inff() ? r.lse : (x - r.m) - r.log_s; }
 
-template <bool F32>
-__device__ __forceinline__ void write_row(const LogprobArgs &a, int row, const Row<F32> &r, const Answer &n)
+// The target and its logit: asked for before the pass over the row, used after it.
+struct Target {
+    bool live;
+    float x;
+};
+template <bool F32> __device__ __forceinline__ Target target_of(const LogprobArgs &a, int row, const Row<F32> &r)
 {
-    if (a.logp) {
-        const int t = a.targets[row];
-        a.logp[row] = t >= 0 && t < a.V ? logp_of(n, r.one(t)) : 0.f;
-    }
+    const int t = a.logp ? a.targets[row] : -1;
+    const bool live = t >= 0 && t < a.V;
+    return Target{live, live ? r.one(t) : 0.f};
+}
+__device__ __forceinline__ void write_row(const LogprobArgs &a, int row, const Target &t, const Answer &n)
+{
+    if (a.logp) a.logp[row] = t.live ? logp_of(n, t.x) : 0.f;
     if (a.entropy) a.entropy[row] = n.entropy;
     if (a.lse) a.lse[row] = n.lse;
 }
 
-// The `top` largest of `count` different keys in LDS, by counting for every key how many are larger.
-template <int NT, typename Out> __device__ __forceinline__ void rank_keys(const unsigned long long *keys, int count, int top, Out out)
+// A lane's key, the same for the whole wave.
+__device__ __forceinline__ unsigned long long lane_key(unsigned long long key, int lane)
 {
-    for (int i = threadIdx.x; i < count; i += NT) {
-        const unsigned long long key = keys[i];
+    return (unsigned long long)(uint32_t)__builtin_amdgcn_readlane((int)(key >> 32), lane) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)key, lane);
+}
+
+// out(rank, key) for the `top` largest of `count` different keys in LDS.  Of up to 64, as there mostly are, the first wave has a key in
+// every lane and compares them with one after the other; of more, a wave takes a key and counts by ballots how many are larger.
+template <int WAVES, typename Out> __device__ __forceinline__ void rank_keys(const unsigned long long *keys, int count, int top, Out out)
+{
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    if (count <= 64) {
+        if (wave > 0) return;
+        const unsigned long long mine = lane < count ? keys[lane] : 0;
         int rank = 0;
-        for (int j = 0; j < count; ++j) rank += keys[j] > key;
-        if (rank < top) out(rank, key);
+        for (int j = 0; j < count; ++j) rank += lane_key(mine, j) > mine;
+        if (lane < count && rank < top) out(rank, mine);
+        return;
+    }
+    for (int j = wave; j < count; j += WAVES) {
+        const unsigned long long key = keys[j];
+        int rank = 0;
+        for (int i = 0; i < count && rank < top; i += 64) rank += __popcll(__ballot(i + lane < count && keys[i + lane < count ? i + lane : 0] > key));
+        if (rank < top && lane == 0) out(rank, key);
     }
 }
 
-// One workgroup of NT threads per slice of a row.
-template <bool F32, int NT>
+// One workgroup of NT threads per slice of a row.  The logits pass once, BATCH vectors of a thread in flight; per batch one maximum is
+// found and one carry-over done.  With TOP every thread also keeps the vector with its largest logit.
+//
+// Alternatives.  The threads with the same lane are a group.  At least `top` groups have an element no smaller than the top-th
+// largest of the 64 groups' largest ones: what is no smaller than this bound, a few more than `top` if the large logits lie
+// anywhere, contains the answer, and lies with the few threads whose own largest is no smaller.  Their vectors are looked at once more
+// (from registers where a batch is all they have, else by all threads), the keys gathered in LDS and ranked.  The order in which
+// they are gathered does not matter: keys are different and ranks are counts.
+constexpr int BATCH = 4;
+template <bool F32, int NT, bool TOP>
 __global__ __launch_bounds__(NT) void logprobs_kernel(LogprobArgs a)
 {
     constexpr int WAVES = NT / 64;
     __shared__ float wave_m[WAVES], wave_s[WAVES], wave_u[WAVES];
-    __shared__ unsigned long long best[NT], list[CANDIDATES], bound;
-    __shared__ int gathered;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    __shared__ unsigned long long best[TOP ? NT : 1], list[TOP ? CANDIDATES : 1], bound;
+    __shared__ int gathered, n_owners;
+    __shared__ short owner[TOP ? NT : 1];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int row = (int)(blockIdx.x / (unsigned)a.slices), slice = (int)(blockIdx.x - (unsigned)row * (unsigned)a.slices);
     const Row<F32> r(a.logits, row, a.stride);
     const int all = r.vectors(a.V);
     const int v0 = slice * a.slice < all ? slice * a.slice : all, v1 = slice + 1 < a.slices && v0 + a.slice < all ? v0 + a.slice : all;
 
+    const Target target = a.slices == 1 ? target_of(a, row, r) : Target{false, 0.f};
     Stats st{LOWEST, 0.f, 0.f};
     float most = -__builtin_inff();
-    int at = v0 + tid < v1 ? v0 + tid : -1;                // the vector with the first of this thread's largest
-    for (int v = v0 + tid; v < v1; v += NT) {
+    int at = -1;                                           // TOP: the vector with the first of this thread's largest
+    // vectors that are all the row's; a first and a last one that are not are threads 0's and 1's
+    const int f0 = v0 < v1 && r.edge(v0, a.V) ? v0 + 1 : v0, f1 = v1 > f0 && r.edge(v1 - 1, a.V) ? v1 - 1 : v1;
+    const int edge = tid == 0 && f0 > v0 ? v0 : tid == 1 && f1 < v1 ? f1 : -1;
+    Raw w[BATCH], ahead[BATCH], largest = nothing<F32>();
+    float top = LOWEST;
+    auto look = [&](const Raw &raw, int v) __attribute__((always_inline)) {
         float x[8];
-        read_vector<F32>(r, v, a.V, x);
-        float vm = x[0];
+        floats<F32>(raw, x);
+        float vm = -__builtin_inff();                      // (stays of eight NaN)
 #pragma unroll
-        for (int i = 1; i < 8; ++i) vm = fmaxf(vm, x[i]);
-        if (vm > most) { most = vm; at = v; }
-        st.move_to(fmaxf(st.m, vm));
+        for (int i = 0; i < 8; ++i) vm = fmaxf(vm, x[i]);
+        top = fmaxf(top, vm);
+        if constexpr (TOP) {
+            const bool more = vm > most || (vm == most && (unsigned)v < (unsigned)at);      // (at = -1: none yet)
+            most = more ? vm : most;
+            at = more ? v : at;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                largest.a[i] = more ? raw.a[i] : largest.a[i];
+                if constexpr (F32) largest.b[i] = more ? raw.b[i] : largest.b[i];
+            }
+        }
+    };
+    auto add = [&](const Raw &raw) __attribute__((always_inline)) {
+        float x[8];
+        floats<F32>(raw, x);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             const float y = x[i] - st.m, e = exp_of(y);
             st.s += e;
             st.u += e * fmaxf(y, FAR);
         }
+    };
+    auto read = [&](int vb) __attribute__((always_inline)) {
+#pragma unroll
+        for (int k = 0; k < BATCH; ++k) {
+            const int v = vb + k * NT + tid;
+            ahead[k] = v >= f0 && v < f1 ? load_vector<F32>(r, v) : nothing<F32>();
+        }
+    };
+    // the next batch is in flight while one is added up (2048 rows of 32000 bf16 logits: 31.6 -> 29.5 us); with TOP the registers that
+    // it takes cost more (20 alternatives: 38.3 -> 39.4)
+    read(v0);
+    for (int vb = v0; vb < v1; vb += BATCH * NT) {
+        if (TOP && vb > v0) read(vb);
+#pragma unroll
+        for (int k = 0; k < BATCH; ++k) w[k] = ahead[k];
+        if (!TOP && vb + BATCH * NT < v1) read(vb + BATCH * NT);
+        top = st.m;
+#pragma unroll
+        for (int k = 0; k < BATCH; ++k)
+            if (vb + k * NT + wave * 64 < v1) look(w[k], vb + k * NT + tid);       // (uniform)
+        st.move_to(top);
+#pragma unroll
+        for (int k = 0; k < BATCH; ++k)
+            if (vb + k * NT + wave * 64 < v1) add(w[k]);
     }
 
-    unsigned long long mine = 0;
-    if (a.top > 0) {
-        if (at >= 0) {
+    Raw part = nothing<F32>();
+    if (edge >= 0) {
+        part = read_edge<F32>(r, edge, a.V);
+        top = st.m;
+        look(part, edge);
+        st.move_to(top);
+        add(part);
+    }
+
+    unsigned long long mine = 0;                           // this thread's largest key
+    if constexpr (TOP) {
+        if (at >= 0 && (at < f1 || at == edge)) {         // (else a place past the slice: no element)
             float x[8];
-            read_vector<F32>(r, at, a.V, x);
-            for (int i = 7; i >= 0; --i) {
-                const int j = 8 * at + i - r.off;
-                if (j < 0 || j >= a.V) continue;
-                const unsigned long long key = key_of(x[i], j);
-                mine = key > mine ? key : mine;
-            }
+            floats<F32>(largest, x);
+            const int begin = r.off - 8 * at > 0 ? r.off - 8 * at : 0;      // elements before are not the row's
+            int i0 = begin;
+#pragma unroll
+            for (int i = 7; i >= 0; --i)
+                if (fmaxf(x[i], -__builtin_inff()) == most && i >= begin) i0 = i;
+            mine = key_of(most, 8 * at + i0 - r.off);
         }
         best[tid] = mine;
-        if (tid == 0) { gathered = 0; bound = 0; }
+        if (tid == 0) { gathered = 0; n_owners = 0; bound = 0; }
     }
     float m = st.m;
 #pragma unroll
@@ -229,97 +342,118 @@ __global__ __launch_bounds__(NT) void logprobs_kernel(LogprobArgs a)
     __syncthreads();
     m = wave_m[0];
 #pragma unroll
-    for (int w = 1; w < WAVES; ++w) m = fmaxf(m, wave_m[w]);
+    for (int k = 1; k < WAVES; ++k) m = fmaxf(m, wave_m[k]);
     st.move_to(m);
     st.s = wave_sum(st.s);
     st.u = wave_sum(st.u);
     if (lane == 0) { wave_s[wave] = st.s; wave_u[wave] = st.u; }
-    if (a.top > 0) {
-        // The threads with the same lane are a group.  At least `top` groups have an element no smaller than the top-th
-        // largest of the 64 groups' best ones: all that is larger than or equal to this bound, a few more than `top` if the
-        // large logits lie anywhere, contains the answer.  Every wave looks at some of the groups' best.
+    if constexpr (TOP) {
+        // every wave looks at some of the groups' largest
         unsigned long long column = 0;
 #pragma unroll
-        for (int w = 0; w < WAVES; ++w) column = best[w * 64 + lane] > column ? best[w * 64 + lane] : column;
+        for (int k = 0; k < WAVES; ++k) column = best[k * 64 + lane] > column ? best[k * 64 + lane] : column;
 #pragma unroll
         for (int i = 0; i < 64 / WAVES; ++i) {
-            const int l = wave * (64 / WAVES) + i;
-            const unsigned long long key = __shfl(column, l);
+            const unsigned long long key = lane_key(column, wave * (64 / WAVES) + i);
             if (key != 0 && __popcll(__ballot(column > key)) == a.top - 1 && lane == 0) bound = key;
         }
     }
     __syncthreads();
     float s = 0.f, u = 0.f;
 #pragma unroll
-    for (int w = 0; w < WAVES; ++w) { s += wave_s[w]; u += wave_u[w]; }
+    for (int k = 0; k < WAVES; ++k) { s += wave_s[k]; u += wave_u[k]; }
     const Answer n = answer_of(m, s, u);
-    if (a.slices == 1) {
-        if (tid == 0) write_row<F32>(a, row, r, n);
-    } else if (tid == 0) {
-        float *p = a.part + 4 * ((size_t)row * a.slices + slice);
-        p[0] = m;
-        p[1] = s;
-        p[2] = u;
+    if (tid == 0) {
+        if (a.slices == 1) {
+            write_row(a, row, target, n);
+        } else {
+            float *p = a.part + 4 * ((size_t)row * a.slices + slice);
+            p[0] = m;
+            p[1] = s;
+            p[2] = u;
+        }
     }
-    if (a.top == 0) return;
-
-    const unsigned long long least = bound;                // 0: fewer than `top` groups have elements
-    if (mine != 0 && mine >= least) {
-        for (int v = v0 + tid; v < v1; v += NT) {
+    if constexpr (TOP) {
+        const unsigned long long least = bound;            // 0: fewer than `top` groups have elements
+        const float least_x = least != 0 ? key_logit(least) : -__builtin_inff();
+        const int least_j = least != 0 ? key_index(least) : 1 << 30;
+        // which of a vector's eight elements are no smaller than the bound
+        auto above = [&](const Raw &raw, int v) __attribute__((always_inline)) {
             float x[8];
-            read_vector<F32>(r, v, a.V, x);
+            floats<F32>(raw, x);
+            uint32_t mask = 0, ties = 0;
+#pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const int j = 8 * v + i - r.off;
-                if (j < 0 || j >= a.V) continue;
-                const unsigned long long key = key_of(x[i], j);
-                if (key < least) continue;
-                const int place = atomicAdd(&gathered, 1);
-                if (place < CANDIDATES) list[place] = key;
+                const float y = fmaxf(x[i], -__builtin_inff());           // (NaN counts as -inf)
+                mask |= y > least_x ? 1u << i : 0u;
+                ties |= y == least_x ? 1u << i : 0u;
             }
-        }
-    }
-    __syncthreads();
-    int count = gathered;
-    if (count > CANDIDATES) {
-        // Many large logits in few groups: the answer one by one, the largest key below the last one found.
-        unsigned long long below = ~0ull;
-        for (int k = 0; k < a.top; ++k) {
-            unsigned long long top = 0;
-            for (int v = v0 + tid; v < v1; v += NT) {
-                float x[8];
-                read_vector<F32>(r, v, a.V, x);
-                for (int i = 0; i < 8; ++i) {
-                    const int j = 8 * v + i - r.off;
-                    if (j < 0 || j >= a.V) continue;
-                    const unsigned long long key = key_of(x[i], j);
-                    if (key < below && key > top) top = key;
-                }
+            const int before = r.off - 8 * v, upto = least_j + 1 + before, end = a.V + before;   // elements of the row, of ties
+            mask |= upto >= 8 ? ties : upto > 0 ? ties & ((1u << upto) - 1u) : 0u;
+            if (before > 0) mask &= 0xFFu << before;
+            return end < 8 ? mask & ((1u << end) - 1u) : mask;
+        };
+        auto gather = [&](const Raw &raw, int v) __attribute__((always_inline)) {
+            uint32_t mask = above(raw, v);
+#pragma unroll 1
+            while (mask != 0) {
+                const int i = __builtin_ctz(mask), place = atomicAdd(&gathered, 1);
+                mask &= mask - 1;
+                if (place < CANDIDATES) list[place] = key_of(element<F32>(raw, i), 8 * v + i - r.off);
             }
-#pragma unroll
-            for (int o = 32; o >= 1; o >>= 1) {
-                const unsigned long long other = __shfl_xor(top, o);
-                top = other > top ? other : top;
-            }
-            __syncthreads();
-            if (lane == 0) best[wave] = top;
-            __syncthreads();
-            below = best[0];
-#pragma unroll
-            for (int w = 1; w < WAVES; ++w) below = best[w] > below ? best[w] : below;
-            if (tid == 0) list[k] = below;
-        }
-        count = a.top;
+        };
+        const bool owns = mine != 0 && mine >= least;
+        if (owns) owner[atomicAdd(&n_owners, 1)] = (short)tid;
         __syncthreads();
-    }
-    if (a.slices == 1) {
-        rank_keys<NT>(list, count, a.top, [&](int rank, unsigned long long key) {
-            a.top_ids[(size_t)row * a.top + rank] = key_index(key);
-            a.top_logp[(size_t)row * a.top + rank] = logp_of(n, key_logit(key));
-        });
-    } else {
-        unsigned long long *keys = a.part_keys + ((size_t)row * a.slices + slice) * a.top;
-        rank_keys<NT>(list, count, a.top, [&](int rank, unsigned long long key) { keys[rank] = key; });
-        for (int k = count + tid; k < a.top; k += NT) keys[k] = 0;
+        const int owners = n_owners, rounds = (v1 - v0 + NT - 1) / NT;
+        for (int i = tid; i < owners * rounds; i += NT) {
+            const int round = i / owners, v = v0 + round * NT + owner[i - round * owners];
+            if (v >= f0 && v < f1) gather(load_vector<F32>(r, v), v);
+        }
+        if (owns && edge >= 0) gather(part, edge);
+        __syncthreads();
+        int count = gathered;
+        if (count > CANDIDATES) {
+            // Many large logits in few groups: the answer one by one, the largest key below the last one found.
+            unsigned long long below = ~0ull;
+            for (int k = 0; k < a.top; ++k) {
+                unsigned long long top = 0;
+                for (int v = v0 + tid; v < v1; v += NT) {
+                    float x[8];
+                    floats<F32>(read_vector<F32>(r, v, a.V), x);
+                    for (int i = 0; i < 8; ++i) {
+                        const int j = 8 * v + i - r.off;
+                        if (j < 0 || j >= a.V) continue;
+                        const unsigned long long key = key_of(x[i], j);
+                        if (key < below && key > top) top = key;
+                    }
+                }
+#pragma unroll
+                for (int o = 32; o >= 1; o >>= 1) {
+                    const unsigned long long other = __shfl_xor(top, o);
+                    top = other > top ? other : top;
+                }
+                __syncthreads();
+                if (lane == 0) best[wave] = top;
+                __syncthreads();
+                below = best[0];
+#pragma unroll
+                for (int q = 1; q < WAVES; ++q) below = best[q] > below ? best[q] : below;
+                if (tid == 0) list[k] = below;
+            }
+            count = a.top;
+            __syncthreads();
+        }
+        if (a.slices == 1) {
+            rank_keys<WAVES>(list, count, a.top, [&](int rank, unsigned long long key) {
+                a.top_ids[(size_t)row * a.top + rank] = key_index(key);
+                a.top_logp[(size_t)row * a.top + rank] = logp_of(n, key_logit(key));
+            });
+        } else {
+            unsigned long long *keys = a.part_keys + ((size_t)row * a.slices + slice) * a.top;
+            rank_keys<WAVES>(list, count, a.top, [&](int rank, unsigned long long key) { keys[rank] = key; });
+            for (int k = count + tid; k < a.top; k += NT) keys[k] = 0;
+        }
     }
 }
 
@@ -329,7 +463,9 @@ template <bool F32>
 __global__ __launch_bounds__(256) void logprobs_join_kernel(LogprobArgs a)
 {
     __shared__ unsigned long long keys[SLICES_MAX * PEQA_MAX_TOP];
+    __shared__ int gathered;
     const int row = blockIdx.x;
+    const Target target = target_of(a, row, Row<F32>(a.logits, row, a.stride));
     const float *p = a.part + 4 * (size_t)row * a.slices;
     float m = LOWEST, s = 0.f, u = 0.f;
     for (int i = 0; i < a.slices; ++i) m = fmaxf(m, p[4 * i]);
@@ -340,21 +476,29 @@ __global__ __launch_bounds__(256) void logprobs_join_kernel(LogprobArgs a)
         u += st.u;
     }
     const Answer n = answer_of(m, s, u);
-    if (threadIdx.x == 0) write_row<F32>(a, row, Row<F32>(a.logits, row, a.stride), n);
+    if (threadIdx.x == 0) write_row(a, row, target, n);
     if (a.top == 0) return;
-    const int count = a.slices * a.top;
-    for (int i = threadIdx.x; i < count; i += 256) keys[i] = a.part_keys[(size_t)row * count + i];
+    // Every slice's keys fall, and each has at least ceil(top / slices) keys no smaller than the least of the slices' keys with that
+    // number: `top` in all, so what is smaller is not looked at.  (0: a slice has fewer.)
+    const int count = a.slices * a.top, lane = threadIdx.x & 63;
+    const unsigned long long *from = a.part_keys + (size_t)row * count;
+    unsigned long long least = lane < a.slices ? from[lane * a.top + (a.top + a.slices - 1) / a.slices - 1] : ~0ull;
+#pragma unroll
+    for (int o = 32; o >= 1; o >>= 1) {
+        const unsigned long long other = __shfl_xor(least, o);
+        least = other < least ? other : least;
+    }
+    if (threadIdx.x == 0) gathered = 0;
     __syncthreads();
     for (int i = threadIdx.x; i < count; i += 256) {
-        const unsigned long long key = keys[i];
-        if (key == 0) continue;
-        int rank = 0;
-        for (int j = 0; j < count; ++j) rank += keys[j] > key;
-        if (rank < a.top) {
-            a.top_ids[(size_t)row * a.top + rank] = key_index(key);
-            a.top_logp[(size_t)row * a.top + rank] = logp_of(n, key_logit(key));
-        }
+        const unsigned long long key = from[i];
+        if (key != 0 && key >= least) keys[atomicAdd(&gathered, 1)] = key;
     }
+    __syncthreads();
+    rank_keys<4>(keys, gathered, a.top, [&](int rank, unsigned long long key) {
+        a.top_ids[(size_t)row * a.top + rank] = key_index(key);
+        a.top_logp[(size_t)row * a.top + rank] = logp_of(n, key_logit(key));
+    });
 }
 
 // d_j = g ([j = target] - p_j) - h p_j (log p_j + H): one read and one write of the logits.
@@ -383,7 +527,7 @@ __global__ __launch_bounds__(256) void logprobs_bwd_kernel(GradArgs a)
 #pragma unroll
             for (int i = 0; i < 8; ++i) x[i] = 0.f;
         } else {
-            read_vector<F32>(r, v, a.V, x);
+            floats<F32>(read_vector<F32>(r, v, a.V), x);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const float logp = x[i] - lse, p = exp_of(logp);
@@ -413,7 +557,7 @@ __global__ __launch_bounds__(256) void logprobs_bwd_kernel(GradArgs a)
 
 // Slices of a row (0: the whole row by one workgroup) and vectors in one.
 struct LogprobPlan {
-    int slices, slice;
+    int slices, slice, threads;
     size_t part_bytes, key_bytes;
 };
 LogprobPlan logprob_plan(int T, int V, int top)
@@ -421,10 +565,11 @@ LogprobPlan logprob_plan(int T, int V, int top)
     LogprobPlan p{};
     const int vectors = (V + 7 + 7) / 8;                       // with any offset of the row
     int slices = PLAN_UNITS / T;
-    const int most = vectors / 2048;                            // two vectors a thread at least
+    const int most = vectors / 2048;
     slices = slices < most ? slices : most;
     slices = slices < SLICES_MAX ? slices : SLICES_MAX;
     p.slices = slices > 1 ? slices : 1;
+    p.threads = T >= PLAN_UNITS || vectors < 1024 ? 256 : 512;
     p.slice = (vectors + p.slices - 1) / p.slices;
     if (p.slices > 1) {
         p.part_bytes = round256((size_t)T * p.slices * 4 * sizeof(float));
@@ -482,18 +627,18 @@ peqa_status peqa_token_logprobs(const void *logits, int32_t dtype, int32_t T, in
     hipStream_t s = static_cast<hipStream_t>(stream);
     const unsigned grid = (unsigned)T * (unsigned)p.slices;
     peqa::trace_before(peqa::KID_LOGPROBS, s);
-    if (dtype == PEQA_LOGITS_F32)
-        hipLaunchKernelGGL((peqa::logprobs_kernel<true, 1024>), dim3(grid), dim3(1024), 0, s, a);
-    else
-        hipLaunchKernelGGL((peqa::logprobs_kernel<false, 1024>), dim3(grid), dim3(1024), 0, s, a);
+    const bool f32 = dtype == PEQA_LOGITS_F32;
+    auto kernel = p.threads == 256 ? (top > 0 ? (f32 ? peqa::logprobs_kernel<true, 256, true> : peqa::logprobs_kernel<false, 256, true>)
+                                              : (f32 ? peqa::logprobs_kernel<true, 256, false> : peqa::logprobs_kernel<false, 256, false>))
+                                   : (top > 0 ? (f32 ? peqa::logprobs_kernel<true, 512, true> : peqa::logprobs_kernel<false, 512, true>)
+                                              : (f32 ? peqa::logprobs_kernel<true, 512, false> : peqa::logprobs_kernel<false, 512, false>));
+    hipLaunchKernelGGL(kernel, dim3(grid), dim3((unsigned)p.threads), 0, s, a);
     peqa::trace_after(peqa::KID_LOGPROBS, s);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || p.slices == 1) return dev_status(e);
     peqa::trace_before(peqa::KID_LOGPROBS_JOIN, s);
-    if (dtype == PEQA_LOGITS_F32)
-        hipLaunchKernelGGL((peqa::logprobs_join_kernel<true>), dim3((unsigned)T), dim3(256), 0, s, a);
-    else
-        hipLaunchKernelGGL((peqa::logprobs_join_kernel<false>), dim3((unsigned)T), dim3(256), 0, s, a);
+    auto join = f32 ? peqa::logprobs_join_kernel<true> : peqa::logprobs_join_kernel<false>;
+    hipLaunchKernelGGL(join, dim3((unsigned)T), dim3(256), 0, s, a);
     peqa::trace_after(peqa::KID_LOGPROBS_JOIN, s);
     return dev_status(hipGetLastError());
 }
