@@ -167,6 +167,20 @@ __device__ __forceinline__ f32x4 mfma_f16(u32x4 x, u32x4 y, f32x4 c)
     return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, x), __builtin_bit_cast(f16x8, y), c, 0, 0, 0);
 }
 
+// f over the four lanes of a wave with the same lane % 16, in all of them: rows of 16 lanes change places, then halves.
+template <typename F> __device__ __forceinline__ float across_groups(float v, F f)
+{
+    auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = f(__uint_as_float(a[0]), __uint_as_float(a[1]));
+    auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return f(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+// The sum of lanes c and c + 8 of every 16, in both.
+__device__ __forceinline__ float add_halves(float v)
+{
+    return v + __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(v), 0x128 /* row_ror:8 */, 0xF, 0xF, true));
+}
+
 // Four 8-bit floats as bf16, or two as fp16: exact.
 template <bool HI> __device__ __forceinline__ uint32_t fp8_bf16(uint32_t v)
 {
@@ -191,6 +205,7 @@ __global__ __launch_bounds__(64 * WAVES, wgs_per_unit(D, FP8)) void attend_kerne
     constexpr int SEG = D > 128 ? D / 128 : 1;        // segments of 128 elements of a value
     constexpr int W = D / 16 / SEG;                   // neighbouring elements of a segment that a lane has: 4 or 8
     constexpr int KB = FP8 ? D / 64 : D / 32;         // 16-byte pieces of a key that a lane loads
+    constexpr int DS = D / SEG;
     constexpr int VR = FP8 ? W / 4 : W / 2;           // registers of a value's segment
     constexpr int EL = FP8 ? 1 : 2;                   // bytes of an element
     constexpr bool AHEAD = HB * D <= 128 || wgs_per_unit(D, FP8) == 1;    // registers for two tiles
@@ -198,7 +213,7 @@ __global__ __launch_bounds__(64 * WAVES, wgs_per_unit(D, FP8)) void attend_kerne
     __shared__ RowInfo info[SCAN_ROWS];
     __shared__ int scan[WAVES + 6];
     __shared__ float wave_m[WAVES][HB][16], wave_l[WAVES][HB][16];
-    __shared__ f32x4 joined[WAVES / 2][HB * SEG * W][64];
+    __shared__ __attribute__((aligned(16))) float joined[WAVES][COLS][DS + 4];
 
     const CacheArgs &C = a.cache;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -288,8 +303,7 @@ __global__ __launch_bounds__(64 * WAVES, wgs_per_unit(D, FP8)) void attend_kerne
             page_at[buffer][i * 64 * WAVES + threadIdx.x] = entry[i] >= 0 && entry[i] < C.n_pages ? entry[i] * C.page_stride * EL : -1ll;
     };
 
-    int head[HB], buffer = 0;
-    bool live[HB];
+    int buffer = 0;
     u32x4 q[HB][QK];
     auto read_queries = [&](const Piece &p) __attribute__((always_inline)) {
 #pragma unroll
@@ -306,7 +320,7 @@ __global__ __launch_bounds__(64 * WAVES, wgs_per_unit(D, FP8)) void attend_kerne
     };
     float m[HB], l[HB], scale = 0.f;
     f32x4 acc[HB][SEG * W];
-    Piece cur;
+    Piece cur{};
     // A tile in registers: pieces of the keys at t0 + c and t0 + 16 + c, of the values at t0 + 4 g .. + 3 and t0 + 16 + 4 g .. + 3 (a page
     // has whole quads of positions).  Positions past the end are read from the last one's place, quads from the last one's.
     struct Tile {
@@ -398,8 +412,7 @@ __global__ __launch_bounds__(64 * WAVES, wgs_per_unit(D, FP8)) void attend_kerne
                 if (!full) y[i] = seen(i) ? y[i] : -__builtin_inff();
                 top = fmaxf(top, y[i]);
             }
-            top = fmaxf(top, __shfl_xor(top, 16));
-            top = fmaxf(top, __shfl_xor(top, 32));
+            top = across_groups(top, [](float x, float y) { return fmaxf(x, y); });
             const float mn = fmaxf(m[b], top), fall = __builtin_amdgcn_exp2f(m[b] - mn);
             m[b] = mn;
             float p[8], sum = 0.f;
@@ -463,141 +476,91 @@ __global__ __launch_bounds__(64 * WAVES, wgs_per_unit(D, FP8)) void attend_kerne
             }
     };
 
-    auto join_waves = [&]() __attribute__((always_inline)) {
-        // the waves' maxima and sums, then their accumulators in a tree
-#pragma unroll
-        for (int b = 0; b < HB; ++b) {
-            l[b] += __shfl_xor(l[b], 16);
-            l[b] += __shfl_xor(l[b], 32);
-            if (g == 0) { wave_m[wave][b][c] = m[b]; wave_l[wave][b][c] = l[b]; }
-        }
-        __syncthreads();
-        float total[HB], top[HB];
-#pragma unroll
-        for (int b = 0; b < HB; ++b) {
-            top[b] = LOWEST;
-#pragma unroll
-            for (int w = 0; w < WAVES; ++w) top[b] = fmaxf(top[b], wave_m[w][b][c]);
-            total[b] = 0.f;
-#pragma unroll
-            for (int w = 0; w < WAVES; ++w) total[b] += wave_l[w][b][c] * __builtin_amdgcn_exp2f(wave_m[w][b][c] - top[b]);
-            const float mine = __builtin_amdgcn_exp2f(m[b] - top[b]);
-#pragma unroll
-            for (int e = 0; e < SEG * W; ++e) acc[b][e] *= mine;
-        }
-#pragma unroll
-        for (int half = WAVES / 2; half >= 1; half /= 2) {
-            if (wave >= half && wave < 2 * half)
-#pragma unroll
-                for (int b = 0; b < HB; ++b)
-#pragma unroll
-                    for (int e = 0; e < SEG * W; ++e) joined[wave - half][b * SEG * W + e][lane] = acc[b][e];
-            __syncthreads();
-            if (wave < half)
-#pragma unroll
-                for (int b = 0; b < HB; ++b)
-#pragma unroll
-                    for (int e = 0; e < SEG * W; ++e) acc[b][e] += joined[wave][b * SEG * W + e][lane];
-            __syncthreads();
-        }
-        if (wave == 0) {
+    // The waves' sums: everything goes to LDS as it is, and every thread scales and adds four elements of a head.
+    auto join_waves = [&](bool more) __attribute__((always_inline)) {
         const float v_scale = FP8 && C.v_scale ? C.v_scale[cur.kv_head] : 1.f;
 #pragma unroll
         for (int b = 0; b < HB; ++b) {
-            if constexpr (!FP8)
+            l[b] = across_groups(l[b], [](float x, float y) { return x + y; });
+            if (g == 0) { wave_m[wave][b][c] = m[b]; wave_l[wave][b][c] = l[b]; }
 #pragma unroll
-                for (int e = 0; e < SEG * W; ++e)
+            for (int s = 0; s < SEG; ++s) {
+                if (b + s > 0) __syncthreads();
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) acc[b][e][r] += __shfl_xor(acc[b][e][r], 8);
-            if (!live[b] || c >= COLS) continue;
-            // this lane: elements 128 s + W (4 g + r) + e
-            const size_t rh = (size_t)cur.row * a.heads + head[b];
-            if (cur.alone) {
-                const float by = total[b] > 0.f || total[b] != total[b] ? v_scale / total[b] : 0.f;
-                uint16_t *o = a.out + cur.row * a.out_stride + (long long)head[b] * D;
+                for (int r = 0; r < 4; ++r)
 #pragma unroll
-                for (int s = 0; s < SEG; ++s)
+                    for (int e = 0; e < W; e += 4) {
+                        f32x4 x;
 #pragma unroll
-                    for (int r = 0; r < 4; ++r)
+                        for (int i = 0; i < 4; ++i) x[i] = FP8 ? acc[b][s * W + e + i][r] : add_halves(acc[b][s * W + e + i][r]);
+                        // this lane: elements 128 s + W (4 g + r) + e
+                        if (c < COLS) *reinterpret_cast<f32x4 *>(&joined[wave][c][W * (4 * g + r) + e]) = x;
+                    }
+                __syncthreads();
+                for (int u = threadIdx.x; u < COLS * DS / 4; u += 64 * WAVES) {
+                    const int col = u / (DS / 4), at = 4 * (u % (DS / 4)), of_group = cur.first_head + b * COLS + col;
+                    if (of_group >= a.group) break;
+                    float top = LOWEST, total = 0.f;
 #pragma unroll
-                        for (int e = 0; e < W; e += 4) {
-                            const u32x2 x = {pack_bf16x2(acc[b][s * W + e][r] * by, acc[b][s * W + e + 1][r] * by),
-                                             pack_bf16x2(acc[b][s * W + e + 2][r] * by, acc[b][s * W + e + 3][r] * by)};
-                            *reinterpret_cast<u32x2 *>(o + 128 * s + W * (4 * g + r) + e) = x;
+                    for (int w = 0; w < WAVES; ++w) top = fmaxf(top, wave_m[w][b][col]);
+                    f32x4 x = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int w = 0; w < WAVES; ++w) {
+                        const float by = __builtin_amdgcn_exp2f(wave_m[w][b][col] - top);
+                        total += wave_l[w][b][col] * by;
+                        x += *reinterpret_cast<const f32x4 *>(&joined[w][col][at]) * by;
+                    }
+                    const int head = cur.kv_head * a.group + of_group;
+                    if (cur.alone) {
+                        const bool any = total > 0.f || total != total;
+                        const float by = any ? v_scale / total : 0.f;
+                        uint16_t *o = a.out + cur.row * a.out_stride + (long long)head * D + 128 * s + at;
+                        *reinterpret_cast<u32x2 *>(o) = u32x2{pack_bf16x2(x[0] * by, x[1] * by), pack_bf16x2(x[2] * by, x[3] * by)};
+                        if (a.lse && at == 0 && s == 0)
+                            a.lse[(size_t)cur.row * a.heads + head] = any ? (top + __builtin_amdgcn_logf(total)) * LN2 : -__builtin_inff();
+                    } else {
+                        const size_t place = (size_t)cur.slot * a.per_wg + b * COLS + col;
+                        *reinterpret_cast<f32x4 *>(a.part + place * D + 128 * s + at) = x;
+                        if (at == 0 && s == 0) {
+                            a.part_ml[2 * place] = top;
+                            a.part_ml[2 * place + 1] = total;
                         }
-                if (a.lse && g == 0)
-                    a.lse[rh] = total[b] > 0.f || total[b] != total[b] ? (top[b] + __builtin_amdgcn_logf(total[b])) * LN2 : -__builtin_inff();
-            } else {
-                const size_t at = (size_t)cur.slot * a.per_wg + b * COLS + c;
-                float *o = a.part + at * D;
-#pragma unroll
-                for (int s = 0; s < SEG; ++s)
-#pragma unroll
-                    for (int r = 0; r < 4; ++r)
-#pragma unroll
-                        for (int e = 0; e < W; e += 4)
-                            *reinterpret_cast<f32x4 *>(o + 128 * s + W * (4 * g + r) + e) =
-                                f32x4{acc[b][s * W + e][r], acc[b][s * W + e + 1][r], acc[b][s * W + e + 2][r], acc[b][s * W + e + 3][r]};
-                if (g == 0) {
-                    a.part_ml[2 * at] = top[b];
-                    a.part_ml[2 * at + 1] = total[b];
+                    }
                 }
             }
         }
-        }
+        if (more) __syncthreads();
     };
 
     // While a piece is computed, the next one's part of the table is on its way; its first tiles and queries are while a segment's sums
-    // are joined.  Two tiles of a wave are in flight where they fit in the registers.
+    // are joined.  Two tiles of a wave are in flight where they fit in the registers.  The first piece is a next one like the others: a
+    // kernel's instructions come from memory when they are first met, and those of a short call are met once.
     constexpr int STEP = WAVES * TILE;
     Tile x;
-    cur = next_piece();
-    read_table(cur);
-    read_queries(cur);
-    keep_table(0);
-    __syncthreads();
-    if (cur.begin + wave * TILE < cur.end) load(x, cur, cur.begin + wave * TILE);
+    bool begun = false;
     for (;;) {
-        if (cur.first) {
-            scale = a.scale * (FP8 && C.k_scale ? C.k_scale[cur.kv_head] : 1.f);
-#pragma unroll
-            for (int b = 0; b < HB; ++b) {
-                const int i = cur.first_head + b * COLS + (c & (COLS - 1));
-                live[b] = i < a.group;
-                head[b] = cur.kv_head * a.group + i;
-                m[b] = LOWEST;
-                l[b] = 0.f;
-#pragma unroll
-                for (int e = 0; e < SEG * W; ++e) acc[b][e] = f32x4{0.f, 0.f, 0.f, 0.f};
-            }
-        }
         const bool more = share.at < share.until;
         Piece next = cur;
         if (more) {
             next = next_piece();
             read_table(next);
         }
-        int t0 = cur.begin + wave * TILE;
-        if constexpr (AHEAD) {
-            Tile y;
-            if (t0 < cur.end)
-                for (;;) {
-                    const bool then = t0 + STEP < cur.end;
-                    if (then) load(y, cur, t0 + STEP);
+        if (begun) {
+            int t0 = cur.begin + wave * TILE;
+            if constexpr (AHEAD) {
+                Tile y;
+                while (t0 < cur.end) {
+                    if (t0 + STEP < cur.end) load(y, cur, t0 + STEP);
                     step(x, t0);
-                    if (!then) break;
-                    t0 += STEP;
-                    const bool again = t0 + STEP < cur.end;
-                    if (again) load(x, cur, t0 + STEP);
-                    step(y, t0);
-                    if (!again) break;
+                    x = y;
                     t0 += STEP;
                 }
-        } else {
-            while (t0 < cur.end) {
-                step(x, t0);
-                t0 += STEP;
-                if (t0 < cur.end) load(x, cur, t0);
+            } else {
+                while (t0 < cur.end) {
+                    step(x, t0);
+                    t0 += STEP;
+                    if (t0 < cur.end) load(x, cur, t0);
+                }
             }
         }
         if (more) {
@@ -607,9 +570,20 @@ __global__ __launch_bounds__(64 * WAVES, wgs_per_unit(D, FP8)) void attend_kerne
             if (next.first) read_queries(next);
             if (next.begin + wave * TILE < next.end) load(x, next, next.begin + wave * TILE);
         }
-        if (cur.last) join_waves();
+        if (begun && cur.last) join_waves(more);
         if (!more) return;
         cur = next;
+        begun = true;
+        if (cur.first) {
+            scale = a.scale * (FP8 && C.k_scale ? C.k_scale[cur.kv_head] : 1.f);
+#pragma unroll
+            for (int b = 0; b < HB; ++b) {
+                m[b] = LOWEST;
+                l[b] = 0.f;
+#pragma unroll
+                for (int e = 0; e < SEG * W; ++e) acc[b][e] = f32x4{0.f, 0.f, 0.f, 0.f};
+            }
+        }
     }
 }
 
