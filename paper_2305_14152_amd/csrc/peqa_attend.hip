@@ -23,7 +23,6 @@ typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 
 constexpr int TILE = 32;                 // positions per step of a wave
-constexpr int WAVES = 4;
 constexpr int UNIT = 64;                 // positions that shares are counted in
 constexpr int CHUNK = 4096;              // positions whose pages are in LDS at a time
 constexpr int SCAN_ROWS = 1024;          // rows of a launch of equal shares at most: every workgroup adds up their lengths
@@ -91,6 +90,7 @@ struct Share {
 };
 
 // Share number `share` of a launch of equal shares; leaves what all rows have in `info`.  scan: WAVES + 6 numbers of LDS.
+template <int WAVES>
 __device__ __forceinline__ Share share_of(const AttendArgs &a, int share, int per_row, RowInfo *info, int *scan)
 {
     constexpr int EACH = SCAN_ROWS / (64 * WAVES);
@@ -195,7 +195,7 @@ template <bool HI> __device__ __forceinline__ uint32_t fp8_f16(uint32_t v)
 // alone are as many, one with up to 512.
 constexpr int wgs_per_unit(int D, bool fp8) { return D > 128 && !fp8 ? 1 : 2; }
 
-template <int D, bool FP8, int HB>
+template <int D, bool FP8, int HB, int WAVES>
 __global__ __launch_bounds__(64 * WAVES, wgs_per_unit(D, FP8)) void attend_kernel(AttendArgs a)
 {
     // Columns of the matrix instructions: 16 heads with 8-bit values, whose weights are fp16; with bf16 values eight heads twice,
@@ -213,7 +213,7 @@ __global__ __launch_bounds__(64 * WAVES, wgs_per_unit(D, FP8)) void attend_kerne
     __shared__ RowInfo info[SCAN_ROWS];
     __shared__ int scan[WAVES + 6];
     __shared__ float wave_m[WAVES][HB][16], wave_l[WAVES][HB][16];
-    __shared__ __attribute__((aligned(16))) float joined[WAVES][COLS][DS + 4];
+    __shared__ __attribute__((aligned(16))) float joined[WAVES][8][DS + 4];
 
     const CacheArgs &C = a.cache;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -224,8 +224,9 @@ __global__ __launch_bounds__(64 * WAVES, wgs_per_unit(D, FP8)) void attend_kerne
     Share share;
     int info_row = 0;                                      // the row of info[0]
     int parts_at = (int)blockIdx.x, chunk_slot = 0;
-    if (a.shares > 0) {
-        share = share_of(a, (int)blockIdx.x, per_row, info, scan);
+    const bool shares = WAVES == 4 && a.shares > 0;
+    if (shares) {
+        share = share_of<WAVES>(a, (int)blockIdx.x, per_row, info, scan);
         if (threadIdx.x == 0) a.parts[parts_at].n = 0;
         if (share.at >= share.until) return;
     } else {
@@ -271,7 +272,7 @@ __global__ __launch_bounds__(64 * WAVES, wgs_per_unit(D, FP8)) void attend_kerne
         if (p.first) segment_from = from;
         p.last = over || n == left;
         p.alone = over && segment_from == 0;               // (of a chunk: segment_from is its first unit)
-        if (a.shares == 0) {
+        if (!shares) {
             p.slot = chunk_slot;
         } else {
             // of the share's first segment, where an item goes on, and of its last one
@@ -484,46 +485,51 @@ __global__ __launch_bounds__(64 * WAVES, wgs_per_unit(D, FP8)) void attend_kerne
             l[b] = across_groups(l[b], [](float x, float y) { return x + y; });
             if (g == 0) { wave_m[wave][b][c] = m[b]; wave_l[wave][b][c] = l[b]; }
 #pragma unroll
-            for (int s = 0; s < SEG; ++s) {
-                if (b + s > 0) __syncthreads();
+            for (int half = 0; half < COLS / 8; ++half) {
+                const int first = cur.first_head + b * COLS + 8 * half;       // of the heads that share the key head: eight columns
+                if (b + half > 0 && first >= a.group) break;                  // (uniform)
 #pragma unroll
-                for (int r = 0; r < 4; ++r)
+                for (int s = 0; s < SEG; ++s) {
+                    if (b + half + s > 0) __syncthreads();
 #pragma unroll
-                    for (int e = 0; e < W; e += 4) {
-                        f32x4 x;
+                    for (int r = 0; r < 4; ++r)
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) x[i] = FP8 ? acc[b][s * W + e + i][r] : add_halves(acc[b][s * W + e + i][r]);
-                        // this lane: elements 128 s + W (4 g + r) + e
-                        if (c < COLS) *reinterpret_cast<f32x4 *>(&joined[wave][c][W * (4 * g + r) + e]) = x;
-                    }
-                __syncthreads();
-                for (int u = threadIdx.x; u < COLS * DS / 4; u += 64 * WAVES) {
-                    const int col = u / (DS / 4), at = 4 * (u % (DS / 4)), of_group = cur.first_head + b * COLS + col;
-                    if (of_group >= a.group) break;
-                    float top = LOWEST, total = 0.f;
+                        for (int e = 0; e < W; e += 4) {
+                            f32x4 x;
 #pragma unroll
-                    for (int w = 0; w < WAVES; ++w) top = fmaxf(top, wave_m[w][b][col]);
-                    f32x4 x = {0.f, 0.f, 0.f, 0.f};
+                            for (int i = 0; i < 4; ++i) x[i] = FP8 ? acc[b][s * W + e + i][r] : add_halves(acc[b][s * W + e + i][r]);
+                            // this lane: elements 128 s + W (4 g + r) + e
+                            if (c >> 3 == half) *reinterpret_cast<f32x4 *>(&joined[wave][c & 7][W * (4 * g + r) + e]) = x;
+                        }
+                    __syncthreads();
+                    for (int u = threadIdx.x; u < 8 * DS / 4; u += 64 * WAVES) {
+                        const int col = u / (DS / 4), at = 4 * (u % (DS / 4)), of_group = first + col;
+                        if (of_group >= a.group) break;
+                        float top = LOWEST, total = 0.f;
 #pragma unroll
-                    for (int w = 0; w < WAVES; ++w) {
-                        const float by = __builtin_amdgcn_exp2f(wave_m[w][b][col] - top);
-                        total += wave_l[w][b][col] * by;
-                        x += *reinterpret_cast<const f32x4 *>(&joined[w][col][at]) * by;
-                    }
-                    const int head = cur.kv_head * a.group + of_group;
-                    if (cur.alone) {
-                        const bool any = total > 0.f || total != total;
-                        const float by = any ? v_scale / total : 0.f;
-                        uint16_t *o = a.out + cur.row * a.out_stride + (long long)head * D + 128 * s + at;
-                        *reinterpret_cast<u32x2 *>(o) = u32x2{pack_bf16x2(x[0] * by, x[1] * by), pack_bf16x2(x[2] * by, x[3] * by)};
-                        if (a.lse && at == 0 && s == 0)
-                            a.lse[(size_t)cur.row * a.heads + head] = any ? (top + __builtin_amdgcn_logf(total)) * LN2 : -__builtin_inff();
-                    } else {
-                        const size_t place = (size_t)cur.slot * a.per_wg + b * COLS + col;
-                        *reinterpret_cast<f32x4 *>(a.part + place * D + 128 * s + at) = x;
-                        if (at == 0 && s == 0) {
-                            a.part_ml[2 * place] = top;
-                            a.part_ml[2 * place + 1] = total;
+                        for (int w = 0; w < WAVES; ++w) top = fmaxf(top, wave_m[w][b][8 * half + col]);
+                        f32x4 x = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                        for (int w = 0; w < WAVES; ++w) {
+                            const float by = __builtin_amdgcn_exp2f(wave_m[w][b][8 * half + col] - top);
+                            total += wave_l[w][b][8 * half + col] * by;
+                            x += *reinterpret_cast<const f32x4 *>(&joined[w][col][at]) * by;
+                        }
+                        const int head = cur.kv_head * a.group + of_group;
+                        if (cur.alone) {
+                            const bool any = total > 0.f || total != total;
+                            const float by = any ? v_scale / total : 0.f;
+                            uint16_t *o = a.out + cur.row * a.out_stride + (long long)head * D + 128 * s + at;
+                            *reinterpret_cast<u32x2 *>(o) = u32x2{pack_bf16x2(x[0] * by, x[1] * by), pack_bf16x2(x[2] * by, x[3] * by)};
+                            if (a.lse && at == 0 && s == 0)
+                                a.lse[(size_t)cur.row * a.heads + head] = any ? (top + __builtin_amdgcn_logf(total)) * LN2 : -__builtin_inff();
+                        } else {
+                            const size_t place = (size_t)cur.slot * a.per_wg + b * COLS + 8 * half + col;
+                            *reinterpret_cast<f32x4 *>(a.part + place * D + 128 * s + at) = x;
+                            if (at == 0 && s == 0) {
+                                a.part_ml[2 * place] = top;
+                                a.part_ml[2 * place + 1] = total;
+                            }
                         }
                     }
                 }
@@ -657,7 +663,7 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a)
 
 // How a call is cut: column blocks of a workgroup, workgroups' worth of heads per key head, heads of a workgroup, chunks or shares.
 struct AttendPlan {
-    int hb, blocks, per_wg, splits, chunk_units, shares, entries;
+    int hb, waves, blocks, per_wg, splits, chunk_units, shares, entries;
     long long grid;
     size_t part_bytes, ml_bytes, parts_bytes;
 };
@@ -665,11 +671,13 @@ struct AttendPlan {
 template <int D, bool FP8>
 hipError_t launch_attend(const AttendArgs &a, const AttendPlan &p, hipStream_t stream)
 {
-    auto kernel = attend_kernel<D, FP8, 1>;
-    if constexpr (D <= 128)
-        if (p.hb == 2) kernel = attend_kernel<D, FP8, 2>;
+    auto kernel = attend_kernel<D, FP8, 1, 4>;
+    if constexpr (D <= 128) {
+        if (p.hb == 2) kernel = attend_kernel<D, FP8, 2, 4>;
+        else if (p.waves == 8) kernel = attend_kernel<D, FP8, 1, 8>;
+    }
     trace_before(KID_ATTEND, stream);
-    hipLaunchKernelGGL(kernel, dim3((unsigned)p.grid), dim3(64 * WAVES), 0, stream, a);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)p.grid), dim3(64 * p.waves), 0, stream, a);
     trace_after(KID_ATTEND, stream);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || p.entries == 0) return e;
@@ -690,13 +698,15 @@ AttendPlan attend_plan(const peqa_kv_cache *C, int rows, int heads, int max_len,
     const long long span = window > 0 && (long long)window + UNIT - 1 < max_len ? (long long)window + UNIT - 1 : max_len;
     const long long items = (long long)rows * C->kv_heads * p.blocks, units = items * ((span + UNIT - 1) / UNIT + START);
     p.grid = items;
+    p.waves = 4;
     p.splits = 1;
     p.chunk_units = (int)((span + UNIT - 1) / UNIT);
     if (p.chunk_units < 1) p.chunk_units = 1;
     const int fit = wgs_per_unit(C->head_dim, C->dtype == PEQA_CACHE_FP8) * PLAN_UNITS;
     long long slots = 0;
     if (span <= 512 || items >= 16 * fit) {
-        // whole items
+        // whole items; of few short ones all tiles are in flight at once, two of each of eight waves
+        if (span > 128 && items <= PLAN_UNITS && p.hb == 1 && C->head_dim <= 128) p.waves = 8;
     } else if (rows > 1 && rows <= SCAN_ROWS && units >= 48ll * fit && units < (1ll << 30)) {
         p.shares = fit;
         p.grid = p.entries = fit;
@@ -704,8 +714,9 @@ AttendPlan attend_plan(const peqa_kv_cache *C, int rows, int heads, int max_len,
     } else {
         // one row: as many chunks as there is room for workgroups; else four times as many, as rows may be of different lengths
         long long chunk = span * items / (rows == 1 ? fit : 4 * fit);
-        chunk = chunk < 512 ? 512 : chunk;
-        p.chunk_units = (int)((chunk + UNIT - 1) / UNIT);
+                chunk = chunk < 512 ? 512 : chunk;
+        const long long splits = (span + chunk / 2) / chunk;   // of the longest row, all alike
+        p.chunk_units = (int)((span + splits * UNIT - 1) / (splits * UNIT));
         p.splits = (int)((span + p.chunk_units * UNIT - 1) / (p.chunk_units * UNIT));
         p.grid = items * p.splits;
         if (p.splits > 1) {
