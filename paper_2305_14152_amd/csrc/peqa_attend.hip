@@ -224,7 +224,7 @@ __global__ __launch_bounds__(64 * WAVES, wgs_per_unit(D, FP8)) void attend_kerne
     Share share;
     int info_row = 0;                                      // the row of info[0]
     int parts_at = (int)blockIdx.x, chunk_slot = 0;
-    const bool shares = WAVES == 4 && a.shares > 0;
+    const bool shares = WAVES == 4 && a.shares > 0;        // (others are launched with whole items)
     if (shares) {
         share = share_of<WAVES>(a, (int)blockIdx.x, per_row, info, scan);
         if (threadIdx.x == 0) a.parts[parts_at].n = 0;
@@ -671,9 +671,9 @@ struct AttendPlan {
 template <int D, bool FP8>
 hipError_t launch_attend(const AttendArgs &a, const AttendPlan &p, hipStream_t stream)
 {
-    auto kernel = attend_kernel<D, FP8, 1, 4>;
+    auto kernel = p.waves == 1 ? attend_kernel<D, FP8, 1, 1> : attend_kernel<D, FP8, 1, 4>;
     if constexpr (D <= 128) {
-        if (p.hb == 2) kernel = attend_kernel<D, FP8, 2, 4>;
+        if (p.hb == 2) kernel = p.waves == 1 ? attend_kernel<D, FP8, 2, 1> : attend_kernel<D, FP8, 2, 4>;
         else if (p.waves == 8) kernel = attend_kernel<D, FP8, 1, 8>;
     }
     trace_before(KID_ATTEND, stream);
@@ -702,27 +702,36 @@ AttendPlan attend_plan(const peqa_kv_cache *C, int rows, int heads, int max_len,
     p.splits = 1;
     p.chunk_units = (int)((span + UNIT - 1) / UNIT);
     if (p.chunk_units < 1) p.chunk_units = 1;
+    // Measured, us (lengths are spread from 2 % to 100 % of the longest; "n x kv, group, length"; bf16, head_dim 128 unless stated):
+    //   whole items, four waves / one     101 rows x 32, 1, 12 (8 bits)  33.1 / 13.1;  101 x 32, 1, 60  31.3 / 17.7;  40 x 16, 8, 40  10.2 / 8.6;
+    //                                     128 x 4, 8, 128 (8 bits, 64)  6.2 / 8.2;  16 x 32, 1, 500  18.6 / 28.7
+    //   whole items / shares              64 x 8, 4, 1000  36.4 / 40.6;  128 x 8, 8, 2000 (8 bits)  67 / 72;  16 x 8, 8, 4096  57.6 / 37.8;
+    //                                     64 x 8, 8, 8192 (8 bits)  139 / 118
+    //   chunks of 128, 256, 512 / whole   8 x 4, 4, 960  10.1, 12.0, 15.4 / 15.4;  1 x 8, 8, 2048  10.3, 11.7, 14.9 / 25.4
+    //   chunks of 256, 512 / shares       2 x 8, 8, 8192  18.0, 18.7 / 20.1;  1 x 8, 8, 16384 (8 bits)  16.5, 16.8 / 19.1
+    //   chunks of 1024, 512 / shares      16 x 8, 8, 4096  42.6, 42.8 / 37.8;  4 x 8, 8, 32768  70.9, 67.3 / 64.3
     const int fit = wgs_per_unit(C->head_dim, C->dtype == PEQA_CACHE_FP8) * PLAN_UNITS;
     long long slots = 0;
-    if (span <= 512 || items >= 16 * fit) {
-        // whole items; of few short ones all tiles are in flight at once, two of each of eight waves
-        if (span > 128 && items <= PLAN_UNITS && p.hb == 1 && C->head_dim <= 128) p.waves = 8;
-    } else if (rows > 1 && rows <= SCAN_ROWS && units >= 48ll * fit && units < (1ll << 30)) {
-        p.shares = fit;
-        p.grid = p.entries = fit;
-        slots = 2 * fit;
-    } else {
-        // one row: as many chunks as there is room for workgroups; else four times as many, as rows may be of different lengths
-        long long chunk = span * items / (rows == 1 ? fit : 4 * fit);
-                chunk = chunk < 512 ? 512 : chunk;
+    if (items >= 2 * fit || (items >= fit && span <= 1024) || span <= 512) {
+        // whole items: many, or of one length, or short.  Of very short ones a wave each; of few all tiles at once, two of each of eight waves
+        if (span <= 128 && items > fit) p.waves = 1;
+        else if (span > 128 && span <= 512 && items <= PLAN_UNITS && p.hb == 1 && C->head_dim <= 128) p.waves = 8;
+    } else if (rows == 1 || rows > SCAN_ROWS || span * items < 960ll * fit || units >= (1ll << 30)) {
+        // chunks: of one row, or as many as there is room for workgroups, of a tile a wave at least
+        long long chunk = span * items / fit;
+        chunk = chunk < 128 ? 128 : chunk;
         const long long splits = (span + chunk / 2) / chunk;   // of the longest row, all alike
         p.chunk_units = (int)((span + splits * UNIT - 1) / (splits * UNIT));
         p.splits = (int)((span + p.chunk_units * UNIT - 1) / (p.chunk_units * UNIT));
         p.grid = items * p.splits;
         if (p.splits > 1) {
-            p.entries = (int)items;                            // (under 16 fit)
+            p.entries = (int)items;                            // (under 2 fit)
             slots = items * p.splits;
         }
+    } else {
+        p.shares = fit;
+        p.grid = p.entries = fit;
+        slots = 2 * fit;
     }
     if (slots > 0) {
         p.part_bytes = round256((size_t)(slots * p.per_wg) * (size_t)C->head_dim * sizeof(float));

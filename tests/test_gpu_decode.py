@@ -179,6 +179,7 @@ def test_split_and_joined(env, fp8, heads, kv_heads, dim, lens):
 @pytest.mark.parametrize("fp8,heads,kv_heads,dim,rows,most,window", [
     (False, 8, 8, 128, 20, 16384, 0), (True, 32, 4, 128, 40, 16384, 0), (False, 24, 2, 64, 50, 32768, 0), (True, 34, 2, 256, 60, 16384, 0),
     (False, 5, 5, 256, 30, 16384, 0), (False, 4, 4, 128, 1000, 2048, 0), (True, 4, 4, 64, 300, 4096, 1500), (False, 18, 1, 128, 200, 16384, 0),
+    (True, 8, 4, 128, 100, 16384, 3000), (False, 3, 3, 64, 90, 16384, 4097),
 ])
 def test_equal_shares(env, fp8, heads, kv_heads, dim, rows, most, window):
     """Bounds that make a launch of equal shares of all rows: few long rows among short and empty ones, in every order of lengths."""
