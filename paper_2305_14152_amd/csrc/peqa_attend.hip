@@ -711,6 +711,10 @@ AttendPlan attend_plan(const peqa_kv_cache *C, int rows, int heads, int max_len,
     //   chunks of 256, 512 / shares       2 x 8, 8, 8192  18.0, 18.7 / 20.1;  1 x 8, 8, 16384 (8 bits)  16.5, 16.8 / 19.1
     //   chunks of 1024, 512 / shares      16 x 8, 8, 4096  42.6, 42.8 / 37.8;  4 x 8, 8, 32768  70.9, 67.3 / 64.3
     const int fit = wgs_per_unit(C->head_dim, C->dtype == PEQA_CACHE_FP8) * PLAN_UNITS;
+    // Of bf16 rows of 256 bytes one workgroup has two tiles of every wave, 128 KB of a unit, in flight, which is enough; where a second one
+    // has no more items to pass it only makes everything wait longer.  512 / 256 of them: 32 x 8, 8, 4096 (all that long)  112.1 / 102.5;
+    // 16 x 8, 8, 4096  37.5 / 36.3;  8 x 32, 1, 8192  101.9 / 99.7;  but 16 x 32, 1, 2048  60 / 67, and of 8 bits 64 x 8, 8, 8192  118 / 129.
+    const int wgs = C->dtype == PEQA_CACHE_BF16 && C->head_dim >= 128 && items <= PLAN_UNITS ? PLAN_UNITS : fit;
     long long slots = 0;
     if (items >= 2 * fit || (items >= fit && span <= 1024) || span <= 512) {
         // whole items: many, or of one length, or short.  Of very short ones a wave each; of few all tiles at once, two of each of eight waves
@@ -718,7 +722,7 @@ AttendPlan attend_plan(const peqa_kv_cache *C, int rows, int heads, int max_len,
         else if (span > 128 && span <= 512 && items <= PLAN_UNITS && p.hb == 1 && C->head_dim <= 128) p.waves = 8;
     } else if (rows == 1 || rows > SCAN_ROWS || span * items < 960ll * fit || units >= (1ll << 30)) {
         // chunks: of one row, or as many as there is room for workgroups, of a tile a wave at least
-        long long chunk = span * items / fit;
+        long long chunk = span * items / wgs;
         chunk = chunk < 128 ? 128 : chunk;
         const long long splits = (span + chunk / 2) / chunk;   // of the longest row, all alike
         p.chunk_units = (int)((span + splits * UNIT - 1) / (splits * UNIT));
@@ -729,9 +733,9 @@ AttendPlan attend_plan(const peqa_kv_cache *C, int rows, int heads, int max_len,
             slots = items * p.splits;
         }
     } else {
-        p.shares = fit;
-        p.grid = p.entries = fit;
-        slots = 2 * fit;
+        p.shares = wgs;
+        p.grid = p.entries = wgs;
+        slots = 2 * wgs;
     }
     if (slots > 0) {
         p.part_bytes = round256((size_t)(slots * p.per_wg) * (size_t)C->head_dim * sizeof(float));
