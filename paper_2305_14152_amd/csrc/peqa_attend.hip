@@ -593,15 +593,15 @@ __global__ __launch_bounds__(64 * WAVES, wgs_per_unit(D, FP8)) void attend_kerne
     }
 }
 
-// Joins the parts of an item that is in several workgroups: a workgroup per entry of `parts` and head.  A group of D / 4 lanes reads
-// the sums of a part, 16 bytes a lane; the groups take the parts in turn, four loads of a lane in flight, and meet in LDS.
+// Joins the parts of an item that is in several workgroups: a workgroup per entry of `parts` and head.  A group of D / 4 lanes has some of
+// the parts, 16 bytes of a part's sums a lane with their maximum beside them, four parts in flight, and joins them as the tiles are
+// joined; the groups' results meet in LDS.  Bound by the latency of three loads after one another (the entry, the parts, the scale).
 template <int D, bool FP8>
 __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a)
 {
-    constexpr int LANES = D / 4, GROUPS = 256 / LANES, BATCH = 256;
-    __shared__ float weight[BATCH], wave_x[4];
+    constexpr int LANES = D / 4, GROUPS = 256 / LANES, FLIGHT = 4;
+    __shared__ float group_m[GROUPS], group_l[GROUPS];
     __shared__ f32x4 sums[GROUPS][LANES];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int heads = a.group < a.per_wg ? a.group : a.per_wg;
     const int entry = (int)(blockIdx.x / (unsigned)heads), i = (int)(blockIdx.x - (unsigned)entry * (unsigned)heads);
     const ItemParts item = a.parts[entry];
@@ -610,55 +610,54 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a)
     const int kv_head = item.item / a.blocks, of_group = (item.item - kv_head * a.blocks) * a.per_wg + i;
     if (of_group >= a.group) return;
     const int head = kv_head * a.group + of_group;
-    auto slot = [&](int s) { return (size_t)(s == 0 ? item.first : item.next + (s - 1) * item.step) * a.per_wg + i; };
-    float top = LOWEST;
-    for (int s = tid; s < n; s += 256) top = fmaxf(top, a.part_ml[2 * slot(s)]);
-#pragma unroll
-    for (int o = 32; o >= 1; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
-    if (lane == 0) wave_x[wave] = top;
-    __syncthreads();
-    top = fmaxf(fmaxf(wave_x[0], wave_x[1]), fmaxf(wave_x[2], wave_x[3]));
-    const int at = tid % LANES, group = tid / LANES;
+    const float v_scale = FP8 && a.cache.v_scale ? a.cache.v_scale[kv_head] : 1.f;
+    const int at = threadIdx.x % LANES, group = threadIdx.x / LANES;
+    float m = LOWEST, l = 0.f;
     f32x4 sum = {0.f, 0.f, 0.f, 0.f};
-    float total = 0.f;
-    for (int s0 = 0; s0 < n; s0 += BATCH) {
-        const int here = n - s0 < BATCH ? n - s0 : BATCH;
-        __syncthreads();                                       // (also: everyone has read wave_x)
-        float w = 0.f;
-        if (tid < here) {
-            const float *ml = a.part_ml + 2 * slot(s0 + tid);
-            w = __builtin_amdgcn_exp2f(ml[0] - top);
-            total += w * ml[1];
+    for (int s0 = group; s0 < n; s0 += FLIGHT * GROUPS) {
+        f32x4 x[FLIGHT];
+        float pm[FLIGHT], pl[FLIGHT], top = m;
+#pragma unroll
+        for (int k = 0; k < FLIGHT; ++k) {
+            const int s = s0 + k * GROUPS < n ? s0 + k * GROUPS : s0;
+            const size_t slot = (size_t)(s == 0 ? item.first : item.next + (s - 1) * item.step) * a.per_wg + i;
+            x[k] = *reinterpret_cast<const f32x4 *>(a.part + slot * D + 4 * at);
+            pm[k] = a.part_ml[2 * slot];
+            pl[k] = a.part_ml[2 * slot + 1];
         }
-        weight[tid] = w;
-        __syncthreads();
-        for (int k0 = group; k0 < here; k0 += 4 * GROUPS) {
-            f32x4 x[4];
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const int s = k0 + k * GROUPS < here ? k0 + k * GROUPS : k0;
-                x[k] = *reinterpret_cast<const f32x4 *>(a.part + slot(s0 + s) * D + 4 * at);
-            }
+        for (int k = 0; k < FLIGHT; ++k) top = fmaxf(top, pm[k]);
+        const float fall = __builtin_amdgcn_exp2f(m - top);
+        m = top;
+        l *= fall;
+        sum *= fall;
 #pragma unroll
-            for (int k = 0; k < 4; ++k)
-                if (k0 + k * GROUPS < here) sum += x[k] * weight[k0 + k * GROUPS];
+        for (int k = 0; k < FLIGHT; ++k) {
+            if (s0 + k * GROUPS >= n) continue;
+            const float by = __builtin_amdgcn_exp2f(pm[k] - top);
+            l += pl[k] * by;
+            sum += x[k] * by;
         }
     }
-#pragma unroll
-    for (int o = 32; o >= 1; o >>= 1) total += __shfl_xor(total, o);
-    if (lane == 0) wave_x[wave] = total;
     sums[group][at] = sum;
+    if (at == 0) { group_m[group] = m; group_l[group] = l; }
     __syncthreads();
-    if (tid >= LANES) return;
-    total = (wave_x[0] + wave_x[1]) + (wave_x[2] + wave_x[3]);
+    if (threadIdx.x >= LANES) return;
+    float top = LOWEST, total = 0.f;
 #pragma unroll
-    for (int k = 1; k < GROUPS; ++k) sum += sums[k][at];
+    for (int k = 0; k < GROUPS; ++k) top = fmaxf(top, group_m[k]);
+    sum = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int k = 0; k < GROUPS; ++k) {
+        const float by = __builtin_amdgcn_exp2f(group_m[k] - top);
+        total += group_l[k] * by;
+        sum += sums[k][at] * by;
+    }
     const bool any = total > 0.f || total != total;
-    const float v_scale = FP8 && a.cache.v_scale ? a.cache.v_scale[kv_head] : 1.f;
     const float by = any ? v_scale / total : 0.f;
     uint16_t *o = a.out + item.row * a.out_stride + (long long)head * D + 4 * at;
     *reinterpret_cast<u32x2 *>(o) = u32x2{pack_bf16x2(sum[0] * by, sum[1] * by), pack_bf16x2(sum[2] * by, sum[3] * by)};
-    if (a.lse && tid == 0) a.lse[(size_t)item.row * a.heads + head] = any ? (top + __builtin_amdgcn_logf(total)) * LN2 : -__builtin_inff();
+    if (a.lse && at == 0) a.lse[(size_t)item.row * a.heads + head] = any ? (top + __builtin_amdgcn_logf(total)) * LN2 : -__builtin_inff();
 }
 
 // How a call is cut: column blocks of a workgroup, workgroups' worth of heads per key head, heads of a workgroup, chunks or shares.

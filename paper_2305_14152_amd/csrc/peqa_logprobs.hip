@@ -231,9 +231,9 @@ template <int WAVES, typename Out> __device__ __forceinline__ void rank_keys(con
 //
 // Alternatives.  The threads with the same lane are a group.  At least `top` groups have an element no smaller than the top-th
 // largest of the 64 groups' largest ones: what is no smaller than this bound, a few more than `top` if the large logits lie
-// anywhere, contains the answer, and lies with the few threads whose own largest is no smaller.  Their vectors are looked at once more
-// (from registers where a batch is all they have, else by all threads), the keys gathered in LDS and ranked.  The order in which
-// they are gathered does not matter: keys are different and ranks are counts.
+// anywhere, contains the answer, and lies with the few threads whose own largest is no smaller.  Their vectors are looked at once
+// more by all threads, the keys gathered in LDS and ranked.  The order in which they are gathered does not matter: keys are different
+// and ranks are counts.
 constexpr int BATCH = 4;
 template <bool F32, int NT, bool TOP>
 __global__ __launch_bounds__(NT) void logprobs_kernel(LogprobArgs a)
@@ -557,7 +557,7 @@ __global__ __launch_bounds__(256) void logprobs_bwd_kernel(GradArgs a)
 
 // Slices of a row (0: the whole row by one workgroup) and vectors in one.
 struct LogprobPlan {
-    int slices, slice, threads;
+    int slices, slice;
     size_t part_bytes, key_bytes;
 };
 LogprobPlan logprob_plan(int T, int V, int top)
@@ -569,7 +569,6 @@ LogprobPlan logprob_plan(int T, int V, int top)
     slices = slices < most ? slices : most;
     slices = slices < SLICES_MAX ? slices : SLICES_MAX;
     p.slices = slices > 1 ? slices : 1;
-    p.threads = T >= PLAN_UNITS || vectors < 1024 ? 256 : 512;
     p.slice = (vectors + p.slices - 1) / p.slices;
     if (p.slices > 1) {
         p.part_bytes = round256((size_t)T * p.slices * 4 * sizeof(float));
@@ -628,11 +627,19 @@ peqa_status peqa_token_logprobs(const void *logits, int32_t dtype, int32_t T, in
     const unsigned grid = (unsigned)T * (unsigned)p.slices;
     peqa::trace_before(peqa::KID_LOGPROBS, s);
     const bool f32 = dtype == PEQA_LOGITS_F32;
-    auto kernel = p.threads == 256 ? (top > 0 ? (f32 ? peqa::logprobs_kernel<true, 256, true> : peqa::logprobs_kernel<false, 256, true>)
-                                              : (f32 ? peqa::logprobs_kernel<true, 256, false> : peqa::logprobs_kernel<false, 256, false>))
-                                   : (top > 0 ? (f32 ? peqa::logprobs_kernel<true, 512, true> : peqa::logprobs_kernel<false, 512, true>)
-                                              : (f32 ? peqa::logprobs_kernel<true, 512, false> : peqa::logprobs_kernel<false, 512, false>));
-    hipLaunchKernelGGL(kernel, dim3(grid), dim3((unsigned)p.threads), 0, s, a);
+    // Short rows: 128 threads, of few vectors each.  Else 256 (of fp32, and of many rows), or 512, which end a row sooner where there are
+    // not rows enough to fill the machine.  128 / 256 / 512, us: 4000 rows of 2000  7.2 / 9.4 / 14.9, with 20 alternatives 15.8 / 19.1 / 31.6;
+    // 64 of 4000 with 32  9.9 / 7.7 / 8.0;  16 of 32000 with 20  - / 11.2 / 9.1;  512 of 50257 with one  29.9 / 19.7 / 18.4;  2048 of 32000
+    // with 20  43.8 / 38.4 / 38.7;  fp32: 300 of 100000  35.3 / 28.8 / 30.8.
+    const int vectors = (vocab + 14) / 8, threads = vectors <= 512 && T >= peqa::PLAN_UNITS ? 128 : T >= (f32 ? 256 : 1024) ? 256 : 512;
+    auto pick = [&](auto n) {
+        constexpr int NT = decltype(n)::value;
+        return top > 0 ? (f32 ? peqa::logprobs_kernel<true, NT, true> : peqa::logprobs_kernel<false, NT, true>)
+                       : (f32 ? peqa::logprobs_kernel<true, NT, false> : peqa::logprobs_kernel<false, NT, false>);
+    };
+    auto kernel = threads == 128 ? pick(std::integral_constant<int, 128>{}) : threads == 256 ? pick(std::integral_constant<int, 256>{})
+                                                                                           : pick(std::integral_constant<int, 512>{});
+    hipLaunchKernelGGL(kernel, dim3(grid), dim3((unsigned)threads), 0, s, a);
     peqa::trace_after(peqa::KID_LOGPROBS, s);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || p.slices == 1) return dev_status(e);

@@ -82,7 +82,7 @@ def logits(torch, gen, T, V, dtype, pad=0, shift=0, std=3.0):
 @pytest.mark.parametrize("T,V,top,pad,shift", [
     (5, 1, 1, 0, 0), (3, 2, 2, 0, 1), (9, 7, 7, 0, 0), (4, 8, 5, 0, 0), (4, 9, 3, 0, 3), (7, 63, 32, 1, 0), (6, 1000, 32, 0, 0), (3, 1003, 20, 0, 5),
     (5, 8191, 32, 2, 1), (2, 8193, 1, 0, 0), (3, 32000, 20, 0, 0), (300, 513, 4, 0, 0), (1, 50257, 8, 0, 1), (4, 50257, 32, 0, 0),
-    (1, 260001, 32, 3, 2), (2, 131072, 32, 0, 0), (260, 40000, 2, 0, 0), (1, 16385, 0, 0, 0),
+    (1, 260001, 32, 3, 2), (2, 131072, 32, 0, 0), (260, 40000, 2, 0, 0), (1, 16385, 0, 0, 0), (1030, 5003, 3, 0, 0), (1025, 4200, 0, 0, 0),
 ])
 def test_logprobs(env, f32, T, V, top, pad, shift):
     torch, peqa = env
