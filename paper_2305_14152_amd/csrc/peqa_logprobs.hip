@@ -466,23 +466,25 @@ __global__ __launch_bounds__(256) void logprobs_join_kernel(LogprobArgs a)
     __shared__ int gathered;
     const int row = blockIdx.x;
     const Target target = target_of(a, row, Row<F32>(a.logits, row, a.stride));
-    const float *p = a.part + 4 * (size_t)row * a.slices;
-    float m = LOWEST, s = 0.f, u = 0.f;
-    for (int i = 0; i < a.slices; ++i) m = fmaxf(m, p[4 * i]);
-    for (int i = 0; i < a.slices; ++i) {
-        Stats st{p[4 * i], p[4 * i + 1], p[4 * i + 2]};
-        st.move_to(m);
-        s += st.s;
-        u += st.u;
+    // a lane per slice
+    const int lane = threadIdx.x & 63, count = a.slices * a.top;
+    const unsigned long long *from = a.part_keys + (size_t)row * count;
+    Stats st{LOWEST, 0.f, 0.f};
+    if (lane < a.slices) {
+        const f32x4 p = *reinterpret_cast<const f32x4 *>(a.part + 4 * ((size_t)row * a.slices + lane));
+        st = Stats{p[0], p[1], p[2]};
     }
+    // Every slice's keys fall, and each has at least ceil(top / slices) keys no smaller than the least of the slices' keys with that
+    // number: `top` in all, so what is smaller is not looked at.  (0: a slice has fewer.)
+    unsigned long long least = a.top > 0 && lane < a.slices ? from[lane * a.top + (a.top + a.slices - 1) / a.slices - 1] : ~0ull;
+    float m = st.m;
+#pragma unroll
+    for (int o = 32; o >= 1; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
+    st.move_to(m);
+    const float s = wave_sum(st.s), u = wave_sum(st.u);
     const Answer n = answer_of(m, s, u);
     if (threadIdx.x == 0) write_row(a, row, target, n);
     if (a.top == 0) return;
-    // Every slice's keys fall, and each has at least ceil(top / slices) keys no smaller than the least of the slices' keys with that
-    // number: `top` in all, so what is smaller is not looked at.  (0: a slice has fewer.)
-    const int count = a.slices * a.top, lane = threadIdx.x & 63;
-    const unsigned long long *from = a.part_keys + (size_t)row * count;
-    unsigned long long least = lane < a.slices ? from[lane * a.top + (a.top + a.slices - 1) / a.slices - 1] : ~0ull;
 #pragma unroll
     for (int o = 32; o >= 1; o >>= 1) {
         const unsigned long long other = __shfl_xor(least, o);
