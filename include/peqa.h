@@ -390,10 +390,11 @@ peqa_status peqa_scale_update_multi(int32_t n, const peqa_update_item *items, co
  *   page * page_stride + h * head_stride + (p % page_size) * slot_stride + d      (elements, in both pools)
  * so pools of any order of heads and slots, and pools that hold keys and values side by side, can be described.
  *   dtype PEQA_CACHE_BF16: bf16.  PEQA_CACHE_FP8: 8-bit floats with 4 exponent and 3 mantissa bits, no infinities, largest
- *   finite value 448 ("e4m3fn"); a stored value stands for itself times k_scale[h] or v_scale[h] (fp32, device; NULL = 1).
+ *   finite value 448 ("e4m3fn"); a stored value stands for itself times k_scale[h] or v_scale[h] (normal fp32 numbers,
+ *   device; NULL = 1).
  *   k, v and the strides are multiples of 16 bytes (PEQA_ERR_ALIGN); page_size is a power of two, 8 .. 1024; head_dim is
- *   64, 128 or 256; page_size * slot_stride is under 2^30.  A table entry outside [0, n_pages) stands for a page that is not there: nothing is stored to it and
- *   its positions are not attended to.
+ *   64, 128 or 256; page_size * slot_stride is under 2^30.  A table entry outside [0, n_pages) stands for a page that is
+ *   not there: nothing is stored to it and its positions are not attended to.
  * The struct is a HOST descriptor, read during the call; the table and the pools are read when the work runs.
  */
 typedef enum { PEQA_CACHE_BF16 = 0, PEQA_CACHE_FP8 = 1 } peqa_cache_dtype;

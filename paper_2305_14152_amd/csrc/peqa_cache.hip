@@ -17,6 +17,7 @@ struct AppendArgs {
     long long q_stride, k_stride, v_stride, q_out_stride;
     int T, heads, n_pos;
     int units;            // of 16 elements, per token: queries, keys, values
+    uint32_t units_inverse;   // floor(2^32 / units)
     int head_shift;       // units per head = 1 << head_shift
     int rot_units;        // rotated units of a head: rot / 16
 };
@@ -25,9 +26,8 @@ struct Eight {
     float x[8];
 };
 
-__device__ __forceinline__ Eight load8(const uint16_t *p)
+__device__ __forceinline__ Eight eight(u32x4 v)
 {
-    const u32x4 v = *reinterpret_cast<const u32x4 *>(p);
     Eight e;
 #pragma unroll
     for (int i = 0; i < 4; ++i) { e.x[2 * i] = bf16_lo(v[i]); e.x[2 * i + 1] = bf16_hi(v[i]); }
@@ -42,13 +42,15 @@ __device__ __forceinline__ u32x4 to_bf16(const Eight &e)
     return v;
 }
 
-// x / scale to 8-bit floats, nearest even, past the largest finite value to it; NaN stays NaN.
-__device__ __forceinline__ u32x2 to_fp8(const Eight &e, float scale)
+// x / scale to 8-bit floats, nearest even, past the largest finite value to it; NaN stays NaN.  The quotient is the product with the
+// reciprocal and one correction by its remainder, three instructions for the eleven of a division (half of the vector instructions of
+// keys and values); a quotient that is infinite has no remainder.
+__device__ __forceinline__ u32x2 to_fp8(const Eight &e, float scale, float inverse)
 {
     float y[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        const float d = e.x[i] / scale;
+        const float first = e.x[i] * inverse, d = fabsf(first) < 1024.f ? fmaf(fmaf(-first, scale, e.x[i]), inverse, first) : first;
         y[i] = d != d ? d : fminf(fmaxf(d, -448.f), 448.f);
     }
     u32x2 v;
@@ -68,15 +70,11 @@ template <bool FP8, bool INTERLEAVED>
 __global__ __launch_bounds__(256) void rope_append_kernel(AppendArgs a)
 {
     const unsigned idx = blockIdx.x * 256u + threadIdx.x;
-    const int t = (int)(idx / (unsigned)a.units), u = (int)(idx - (unsigned)t * (unsigned)a.units);
+    int t = (int)__umulhi(idx, a.units_inverse), u = (int)(idx - (unsigned)t * (unsigned)a.units);    // (t: one too small at most)
+    if (u >= a.units) { ++t; u -= a.units; }
     if (t >= a.T) return;
     const CacheArgs &C = a.cache;
     const int pos = a.pos[t], seq = a.seq ? a.seq[t] : t;
-    int page = -1;
-    if (pos >= 0 && (a.rot_units == 0 || pos < a.n_pos) && seq >= 0 && seq < C.n_seqs && (pos >> C.page_shift) < C.n_blocks)
-        page = C.table[seq * C.table_stride + (pos >> C.page_shift)];
-    const bool there = page >= 0 && page < C.n_pages;
-
     const int q_units = a.q ? a.heads << a.head_shift : 0;
     const bool is_q = u < q_units;
     const int w = is_q ? u : u - q_units;
@@ -89,6 +87,13 @@ __global__ __launch_bounds__(256) void rope_append_kernel(AppendArgs a)
     int at0 = part * 16, at1 = at0 + 8;
     if (!INTERLEAVED && rotated) { at0 = part * 8; at1 = at0 + a.rot_units * 8; }
 
+    // asked for before the page is known: the place in the table follows from the position, the page from the table
+    const uint16_t *x = (is_q ? a.q + t * a.q_stride : is_v ? a.v + t * a.v_stride : a.k + t * a.k_stride) + h * dim;
+    const u32x4 raw0 = *reinterpret_cast<const u32x4 *>(x + at0), raw1 = *reinterpret_cast<const u32x4 *>(x + at1);
+    int page = -1;
+    if (pos >= 0 && (a.rot_units == 0 || pos < a.n_pos) && seq >= 0 && seq < C.n_seqs && (pos >> C.page_shift) < C.n_blocks)
+        page = C.table[seq * C.table_stride + (pos >> C.page_shift)];
+    const bool there = page >= 0 && page < C.n_pages;
     if (!there) {
         if (is_q) {
             uint16_t *o = a.q_out + t * a.q_out_stride + h * dim;
@@ -97,8 +102,7 @@ __global__ __launch_bounds__(256) void rope_append_kernel(AppendArgs a)
         }
         return;
     }
-    const uint16_t *x = (is_q ? a.q + t * a.q_stride : is_v ? a.v + t * a.v_stride : a.k + t * a.k_stride) + h * dim;
-    Eight e0 = load8(x + at0), e1 = load8(x + at1);
+    Eight e0 = eight(raw0), e1 = eight(raw1);
     if (rotated) {
         const size_t row = (size_t)pos * (size_t)(a.rot_units * 8) + (size_t)(part * 8);
         float c[8], s[8];
@@ -136,10 +140,10 @@ __global__ __launch_bounds__(256) void rope_append_kernel(AppendArgs a)
     const long long place = page * C.page_stride + h * C.head_stride + (pos & C.page_mask) * C.slot_stride;
     if (FP8) {
         const float *scales = is_v ? C.v_scale : C.k_scale;
-        const float scale = scales ? scales[h] : 1.f;
+        const float scale = scales ? scales[h] : 1.f, inverse = 1.f / scale;
         uint8_t *o = static_cast<uint8_t *>(is_v ? C.v : C.k) + place;
-        *reinterpret_cast<u32x2 *>(o + at0) = to_fp8(e0, scale);
-        *reinterpret_cast<u32x2 *>(o + at1) = to_fp8(e1, scale);
+        *reinterpret_cast<u32x2 *>(o + at0) = to_fp8(e0, scale, inverse);
+        *reinterpret_cast<u32x2 *>(o + at1) = to_fp8(e1, scale, inverse);
     } else {
         uint16_t *o = static_cast<uint16_t *>(is_v ? C.v : C.k) + place;
         *reinterpret_cast<u32x4 *>(o + at0) = to_bf16(e0);
@@ -208,7 +212,8 @@ peqa_status peqa_rope_append(const peqa_kv_cache *C, int32_t T, const int32_t *p
     a.q = q; a.k = k; a.v = v; a.q_out = q_out;
     a.q_stride = q_stride; a.k_stride = k_stride; a.v_stride = v_stride; a.q_out_stride = q_out_stride;
     a.T = T; a.heads = heads; a.n_pos = n_pos;
-    a.units = (int)units;
+    a.units = (int)units;                                      // (two at least)
+    a.units_inverse = (uint32_t)((1ull << 32) / (uint64_t)units);
     a.head_shift = __builtin_ctz((unsigned)(D / 16));
     a.rot_units = rot / 16;
     return dev_status(peqa::launch_rope_append(C->dtype == PEQA_CACHE_FP8, interleaved != 0, a, (unsigned)((units * T + 255) / 256),
