@@ -182,7 +182,8 @@ def _stream(stream):
     if stream is None:
         if _current_stream is None:
             import torch
-            raw, device = torch._C._cuda_getCurrentRawStream, torch.cuda.current_device
+            torch.cuda.current_device()        # (initialises torch's side, which the calls below take for granted)
+            raw, device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
             _current_stream = lambda: raw(device())
         return _current_stream()
     return stream if isinstance(stream, int) else stream.cuda_stream
