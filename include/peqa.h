@@ -393,8 +393,8 @@ peqa_status peqa_scale_update_multi(int32_t n, const peqa_update_item *items, co
  *   finite value 448 ("e4m3fn"); a stored value stands for itself times k_scale[h] or v_scale[h] (normal fp32 numbers,
  *   device; NULL = 1).
  *   k, v and the strides are multiples of 16 bytes (PEQA_ERR_ALIGN); page_size is a power of two, 8 .. 1024; head_dim is
- *   64, 128 or 256; page_size * slot_stride is under 2^30.  A table entry outside [0, n_pages) stands for a page that is
- *   not there: nothing is stored to it and its positions are not attended to.
+ *   64, 128 or 256; page_size * slot_stride is under 2^30, n_blocks * page_size at most 2^30.  A table entry outside
+ *   [0, n_pages) stands for a page that is not there: nothing is stored to it and its positions are not attended to.
  * The struct is a HOST descriptor, read during the call; the table and the pools are read when the work runs.
  */
 typedef enum { PEQA_CACHE_BF16 = 0, PEQA_CACHE_FP8 = 1 } peqa_cache_dtype;
@@ -445,7 +445,8 @@ peqa_status peqa_rope_append(const peqa_kv_cache *C, int32_t T, const int32_t *p
  *            is split for it, so a tight bound is faster.  heads: a multiple of kv_heads.
  *   workspace: peqa_paged_attention_workspace_bytes(C, rows, heads, max_len, window).
  * Products and sums are fp32.  The softmax weights are rounded for the matrix instructions: against bf16 values in two
- * bf16 parts (16 bits), against 8-bit values to fp16 (11 bits).
+ * bf16 parts (16 bits), against 8-bit values to fp16 (11 bits).  The same call gives the same bits; the order in which a
+ * row's positions are added depends on max_len, window, the number of rows and, with many long rows, their lengths.
  */
 size_t peqa_paged_attention_workspace_bytes(const peqa_kv_cache *C, int32_t rows, int32_t heads, int32_t max_len,
                                             int32_t window);

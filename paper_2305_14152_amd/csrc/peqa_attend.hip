@@ -538,8 +538,8 @@ __global__ __launch_bounds__(64 * WAVES, wgs_per_unit(D, FP8)) void attend_kerne
         if (more) __syncthreads();
     };
 
-    // While a piece is computed, the next one's part of the table is on its way; its first tiles and queries are while a segment's sums
-    // are joined.  Two tiles of a wave are in flight where they fit in the registers.  The first piece is a next one like the others: a
+    // While a piece is computed, the next one's part of the table is on its way; its first tile and queries are while a segment's sums are
+    // joined.  Two tiles of a wave are in flight where they fit in the registers.  The first piece is a next one like the others: a
     // kernel's instructions come from memory when they are first met, and those of a short call are met once.
     constexpr int STEP = WAVES * TILE;
     Tile x;
@@ -595,7 +595,8 @@ __global__ __launch_bounds__(64 * WAVES, wgs_per_unit(D, FP8)) void attend_kerne
 
 // Joins the parts of an item that is in several workgroups: a workgroup per entry of `parts` and head.  A group of D / 4 lanes has some of
 // the parts, 16 bytes of a part's sums a lane with their maximum beside them, four parts in flight, and joins them as the tiles are
-// joined; the groups' results meet in LDS.  Bound by the latency of three loads after one another (the entry, the parts, the scale).
+// joined; the groups' results meet in LDS.  Bound by the latency of two loads after one another, the entry and the parts: 4.7 us where
+// 512 shares have few parts each.
 template <int D, bool FP8>
 __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a)
 {
@@ -752,8 +753,8 @@ peqa_status check_attend(const peqa_kv_cache *C, int32_t rows, int32_t heads, in
     if ((int64_t)max_len > (int64_t)C->n_blocks * C->page_size) return PEQA_ERR_SHAPE;
     if (window < 0) return PEQA_ERR_PARAM;
     const AttendPlan p = attend_plan(C, rows, heads, max_len, window);
-    if ((int64_t)C->kv_heads * p.blocks * ((max_len + UNIT - 1) / UNIT + START) > (1 << 30)) return PEQA_ERR_SHAPE;    // units of a row
-    if (p.grid > INT32_MAX / 64) return PEQA_ERR_SHAPE;
+    if ((int64_t)C->kv_heads * p.blocks * (((int64_t)max_len + UNIT - 1) / UNIT + START) > (1 << 30)) return PEQA_ERR_SHAPE;    // units of a row
+    if (p.grid * 64 * p.waves > (int64_t)UINT32_MAX) return PEQA_ERR_SHAPE;    // threads of a launch
     return PEQA_OK;
 }
 

@@ -174,7 +174,7 @@ peqa_status peqa_check_cache(const peqa_kv_cache *C)
     if (C->page_size < 8 || C->page_size > 1024 || (C->page_size & (C->page_size - 1))) return PEQA_ERR_SHAPE;
     if (C->head_dim != 64 && C->head_dim != 128 && C->head_dim != 256) return PEQA_ERR_SHAPE;
     if (C->n_pages < 1 || C->kv_heads < 1 || C->kv_heads > 4096 || C->n_seqs < 1 || C->n_blocks < 1) return PEQA_ERR_SHAPE;
-    if ((int64_t)C->n_blocks * C->page_size > INT32_MAX || C->table_stride < C->n_blocks) return PEQA_ERR_SHAPE;
+    if ((int64_t)C->n_blocks * C->page_size > (1 << 30) || C->table_stride < C->n_blocks) return PEQA_ERR_SHAPE;    // positions are 32-bit numbers
     if (C->page_stride < 0 || C->head_stride < 0 || C->slot_stride < C->head_dim) return PEQA_ERR_SHAPE;
     const int64_t unit = C->dtype == PEQA_CACHE_FP8 ? 16 : 8;
     if (C->slot_stride > (INT32_MAX / 2) / C->page_size) return PEQA_ERR_SHAPE;    // a head's slots of a page: 32-bit offsets in kernels

@@ -619,7 +619,7 @@ peqa_status peqa_token_logprobs(const void *logits, int32_t dtype, int32_t T, in
     if (top < 0 || top > PEQA_MAX_TOP || top > vocab) return PEQA_ERR_PARAM;
     if (!logits || (logp && !targets) || (top > 0 && (!top_logp || !top_ids))) return PEQA_ERR_NULL;
     if (!logp && !entropy && !lse && top == 0) return PEQA_ERR_NULL;
-    if (stride < vocab) return PEQA_ERR_SHAPE;
+    if (stride < vocab || (int64_t)T * 512 > (int64_t)UINT32_MAX) return PEQA_ERR_SHAPE;    // (threads of a launch)
     if (!peqa::aligned_to(logits, dtype == PEQA_LOGITS_F32 ? 4 : 2) || !peqa::aligned_to(targets, 4) || !peqa::aligned_to(logp, 4) ||
         !peqa::aligned_to(entropy, 4) || !peqa::aligned_to(lse, 4) || !peqa::aligned_to(top_logp, 4) || !peqa::aligned_to(top_ids, 4))
         return PEQA_ERR_ALIGN;
@@ -679,7 +679,7 @@ peqa_status peqa_token_logprobs_bwd(const void *logits, int32_t dtype, int32_t T
     const int vectors = (vocab + 7 + 7) / 8;
     const int per_block = 256 * peqa::grad_vectors(dtype == PEQA_LOGITS_F32);
     a.blocks = (vectors + per_block - 1) / per_block;
-    if (a.blocks > INT32_MAX / T) return PEQA_ERR_SHAPE;
+    if ((int64_t)a.blocks * T * 256 > (int64_t)UINT32_MAX) return PEQA_ERR_SHAPE;    // threads of a launch
     hipStream_t s = static_cast<hipStream_t>(stream);
     const unsigned grid = (unsigned)T * (unsigned)a.blocks;
     peqa::trace_before(peqa::KID_LOGPROBS_BWD, s);

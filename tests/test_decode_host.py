@@ -134,3 +134,16 @@ def test_binding_checks(peqa):
     with pytest.raises(AssertionError):
         peqa.paged_attention(c, q.transpose(1, 2), torch.zeros(4, dtype=torch.int32), 64, 1.0, q.clone(), None, 0, stream=0)
     assert ctypes.sizeof(peqa.KVCache) == 104
+
+
+def test_sizes_past_what_the_kernels_index(peqa):
+    """Positions past 2^30, units of a row past 2^30 and launches of more than 2^32 threads are refused."""
+    L = peqa.lib()
+    assert peqa.check_cache(cache(peqa, n_blocks=1 << 26, table_stride=1 << 26)) == peqa.PEQA_OK
+    assert peqa.check_cache(cache(peqa, n_blocks=(1 << 26) + 1, table_stride=1 << 27)) == peqa.PEQA_ERR_SHAPE
+    wide = cache(peqa, n_blocks=1 << 26, table_stride=1 << 26, kv_heads=128, page_stride=128 * 16 * 128)
+    assert peqa.paged_attention_workspace_bytes(wide, 128, 1, 1 << 30) == 0 and peqa.paged_attention_workspace_bytes(wide, 128, 1, 1 << 28) > 0
+    many = cache(peqa, kv_heads=64, n_seqs=1 << 30, page_stride=64 * 16 * 128)
+    assert peqa.paged_attention_workspace_bytes(many, 64, 1 << 20, 16) == 0
+    assert L.peqa_token_logprobs(GOOD, 0, 1 << 24, 100, 100, GOOD, 0, GOOD, None, None, None, None, None, 0, None) == peqa.PEQA_ERR_SHAPE
+    assert L.peqa_token_logprobs_bwd(GOOD, 0, 1 << 20, 1 << 20, 1 << 20, GOOD, GOOD, None, GOOD, None, 2 * GOOD, 1 << 20, None) == peqa.PEQA_ERR_SHAPE
