@@ -424,8 +424,8 @@ peqa_status peqa_check_cache(const peqa_kv_cache *C);
  *   pointers and row strides multiples of 16 bytes: the members of a stacked query/key/value output can be passed as they lie
  * The rotation is fp32 and rounds once to what is stored (nearest even; 8-bit: of x / scale, values past 448 become 448).
  * A token with pos < 0, pos >= n_pos (where rotated), seq outside [0, n_seqs), a position past the table or a page that
- * is not there is skipped: its row of q_out is zeros and nothing is stored.  Of tokens with the same sequence and position
- * one is stored.
+ * is not there is skipped: its row of q_out is zeros and nothing is stored.  The places of one call have to be different: of
+ * tokens with the same sequence and position, every 16 elements are one of theirs, not all of them the same one's.
  */
 peqa_status peqa_rope_append(const peqa_kv_cache *C, int32_t T, const int32_t *pos, const int32_t *seq,
                              const float *cos_table, const float *sin_table, int32_t n_pos, int32_t rot,

@@ -228,6 +228,10 @@ template <int WAVES, typename Out> __device__ __forceinline__ void rank_keys(con
 
 // One workgroup of NT threads per slice of a row.  The logits pass once, BATCH vectors of a thread in flight; per batch one maximum is
 // found and one carry-over done.  With TOP every thread also keeps the vector with its largest logit.
+// Bound by memory and the latency of a batch: 2048 rows of 32000 bf16 logits 27.8 us, 4.7 TB/s (11 vector instructions a logit; a
+// form with 8, that looks for a new maximum only where a batch's sum gets large, is no faster), 333 rows of 100003 fp32 logits with five
+// alternatives 33.5 us, 4.0 TB/s.  16 rows of 32000 with 20 alternatives, 9.7 us, are a launch, two batches and the steps of the search one
+// after the other.
 //
 // Alternatives.  The threads with the same lane are a group.  At least `top` groups have an element no smaller than the top-th
 // largest of the 64 groups' largest ones: what is no smaller than this bound, a few more than `top` if the large logits lie
