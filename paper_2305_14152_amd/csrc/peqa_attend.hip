@@ -46,8 +46,8 @@ struct AttendArgs {
     uint16_t *out;
     float *lse;
     // Parts of items that are in several workgroups: a slot has the heads of one workgroup.
-    float *part;               // [slots, per_wg, head_dim] weighted sums, relative to the maximum
-    float *part_ml;            // [slots, per_wg, 2] maximum (of powers of two) and sum
+    float *part;               // [slots, per_wg, head_dim] weighted sums, relative to the reference
+    float *part_ml;            // [slots, per_wg, 2] reference (the maximum, or 14 below it; of powers of two) and sum
     ItemParts *parts;          // [rows * items of a row], or [shares]: of the item that ends in a share and began before it
     long long q_stride, out_stride;
     float scale;               // times log2 e
@@ -419,6 +419,8 @@ __global__ __launch_bounds__(64 * WAVES, wgs_per_unit(D, FP8)) void attend_kerne
                 top = fmaxf(top, y[i]);
             }
             top = across_groups(top, [](float x, float y) { return fmaxf(x, y); });
+            // relative to 2^14 below the maximum, weights down to 2^-28 of the largest are normal fp16 numbers (scores past 2^24 have no bits for it)
+            if constexpr (FP8) top = fabsf(top) < 16777216.f ? top - 14.f : top;
             const float mn = fmaxf(m[b], top), fall = __builtin_amdgcn_exp2f(m[b] - mn);
             m[b] = mn;
             float p[8], sum = 0.f;

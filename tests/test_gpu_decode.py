@@ -237,6 +237,28 @@ def test_large_scores_and_equal_ones(env):
     check_attention(torch, peqa, cache, q, [700], 700, scale=0.25)
 
 
+@pytest.mark.parametrize("gap", [9.7, 12.1, 17.67])
+@pytest.mark.parametrize("lens", [[100], [700, 3], [20001]])
+def test_small_weights_of_8_bit_values(env, lens, gap):
+    """Some positions `gap` above all others and with values of 0: the result is made of weights of e^-gap, each of which may be
+    off by its own rounding only."""
+    torch, peqa = env
+    gen = torch.Generator().manual_seed(12)
+    cache = make_cache(torch, peqa, gen, lens, 1, 128, 32, True, scales=False)
+    k, v, table, _, _ = cache.tensors
+    k.zero_()
+    v.copy_((torch.rand(v.shape, generator=gen) * 100 + 1).to(torch.float8_e4m3fn))
+    for r, n in enumerate(lens):
+        for j in range(n):
+            if j % 1000 < 256 and j % 32 == 3:
+                page, slot = int(table[r, j // 32]), j % 32
+                k[page, 0, slot, 0] = 16.0
+                v[page, 0, slot] = 0.0
+    q = torch.zeros((len(lens), 4, 128))
+    q[..., 0] = 1.0
+    check_attention(torch, peqa, cache, q.to(torch.bfloat16).cuda(), lens, max(lens), scale=gap / 16, fp8=True)
+
+
 def test_offsets_past_32_bits(env):
     """Pages behind 2^32 bytes and 2^31 elements of a pool."""
     torch, peqa = env
