@@ -127,6 +127,24 @@ def test_hard_rows(env, f32, T, V):
     check(torch, peqa, x[:2], targets[:2], 5)
 
 
+@pytest.mark.parametrize("f32", [False, True])
+@pytest.mark.parametrize("T,V,top", [(40, 700, 32), (40, 1003, 20), (40, 4096, 32), (8, 50257, 32), (3, 200003, 31), (300, 1500, 32)])
+def test_few_words_allowed(env, f32, T, V, top):
+    """Fewer words than alternatives, the rest masked alike: the alternatives end with the first of the masked ones."""
+    torch, peqa = env
+    print("few", f32, T, V, top, flush=True)
+    dtype = torch.float32 if f32 else torch.bfloat16
+    gen = torch.Generator().manual_seed(V + top)
+    x, _ = logits(torch, gen, T, V, dtype)
+    for r in range(T):
+        allowed = torch.randperm(V, generator=gen)[:r % (top + 3)]
+        kept = x[r, allowed.cuda()].clone()
+        x[r] = -math.inf if r % 2 == 0 else torch.finfo(dtype).min
+        x[r, allowed.cuda()] = kept
+    targets = torch.randint(0, V, (T,), generator=gen, dtype=torch.int32)
+    check(torch, peqa, x, targets.cuda(), top)
+
+
 def test_many_distinct_large_logits_in_few_columns(env):
     """More large logits than are gathered at once, all in the elements of few groups of threads."""
     torch, peqa = env
