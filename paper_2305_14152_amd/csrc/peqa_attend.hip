@@ -213,7 +213,7 @@ __global__ __launch_bounds__(64 * WAVES, wgs_per_unit(D, FP8)) void attend_kerne
     constexpr int DS = D / SEG;
     constexpr int VR = FP8 ? W / 4 : W / 2;           // registers of a value's segment
     constexpr int EL = FP8 ? 1 : 2;                   // bytes of an element
-    constexpr bool AHEAD = HB * D <= 128 || wgs_per_unit(D, FP8) == 1;    // registers for two tiles
+    constexpr bool AHEAD = HB * D <= 128 || (HB == 1 && wgs_per_unit(D, FP8) == 1);    // registers for two tiles (of 16 heads of 256: for their queries and sums)
     __shared__ long long page_at[2][CHUNK / 8];             // where a piece's pages begin, in bytes; -1: not there
     __shared__ RowInfo info[SCAN_ROWS];
     __shared__ int scan[WAVES + 6];
@@ -487,6 +487,13 @@ __global__ __launch_bounds__(64 * WAVES, wgs_per_unit(D, FP8)) void attend_kerne
     // The waves' sums: everything goes to LDS as it is, and every thread scales and adds four elements of a head.
     auto join_waves = [&](bool more) __attribute__((always_inline)) {
         const float v_scale = FP8 && C.v_scale ? C.v_scale[cur.kv_head] : 1.f;
+        int tid = threadIdx.x, c = lane & 15, g = lane >> 4;
+        if constexpr (D > 128) {
+            // what follows from the thread's number is found anew, not kept in registers over the tiles
+            asm volatile("" : "+v"(tid));
+            c = tid & 15;
+            g = tid >> 4 & 3;
+        }
 #pragma unroll
         for (int b = 0; b < HB; ++b) {
             l[b] = across_groups(l[b], [](float x, float y) { return x + y; });
@@ -509,7 +516,7 @@ __global__ __launch_bounds__(64 * WAVES, wgs_per_unit(D, FP8)) void attend_kerne
                             if (c >> 3 == half) *reinterpret_cast<f32x4 *>(&joined[wave][c & 7][W * (4 * g + r) + e]) = x;
                         }
                     __syncthreads();
-                    for (int u = threadIdx.x; u < 8 * DS / 4; u += 64 * WAVES) {
+                    for (int u = tid; u < 8 * DS / 4; u += 64 * WAVES) {
                         const int col = u / (DS / 4), at = 4 * (u % (DS / 4)), of_group = first + col;
                         if (of_group >= a.group) break;
                         float top = LOWEST, total = 0.f;
@@ -679,10 +686,10 @@ template <int D, bool FP8>
 hipError_t launch_attend(const AttendArgs &a, const AttendPlan &p, hipStream_t stream)
 {
     auto kernel = p.waves == 1 ? attend_kernel<D, FP8, 1, 1> : attend_kernel<D, FP8, 1, 4>;
-    if constexpr (D <= 128) {
+    if constexpr (D <= 128)
+        if (p.waves == 8) kernel = attend_kernel<D, FP8, 1, 8>;
+    if constexpr (D <= 128 || !FP8)
         if (p.hb == 2) kernel = p.waves == 1 ? attend_kernel<D, FP8, 2, 1> : attend_kernel<D, FP8, 2, 4>;
-        else if (p.waves == 8) kernel = attend_kernel<D, FP8, 1, 8>;
-    }
     trace_before(KID_ATTEND, stream);
     hipLaunchKernelGGL(kernel, dim3((unsigned)p.grid), dim3(64 * p.waves), 0, stream, a);
     trace_after(KID_ATTEND, stream);
@@ -699,7 +706,7 @@ AttendPlan attend_plan(const peqa_kv_cache *C, int rows, int heads, int max_len,
 {
     AttendPlan p{};
     const int group = heads / C->kv_heads, cols = C->dtype == PEQA_CACHE_FP8 ? 16 : 8;
-    p.hb = C->head_dim <= 128 && group > cols ? 2 : 1;
+    p.hb = (C->head_dim <= 128 || C->dtype == PEQA_CACHE_BF16) && group > cols ? 2 : 1;    // (16 heads of 256 with 8 bits fill the registers)
     p.per_wg = cols * p.hb;
     p.blocks = (group + p.per_wg - 1) / p.per_wg;
     const long long span = window > 0 && (long long)window + UNIT - 1 < max_len ? (long long)window + UNIT - 1 : max_len;
@@ -717,17 +724,25 @@ AttendPlan attend_plan(const peqa_kv_cache *C, int rows, int heads, int max_len,
     //   chunks of 128, 256, 512 / whole   8 x 4, 4, 960  10.1, 12.0, 15.4 / 15.4;  1 x 8, 8, 2048  10.3, 11.7, 14.9 / 25.4
     //   chunks of 256, 512 / shares       2 x 8, 8, 8192  18.0, 18.7 / 20.1;  1 x 8, 8, 16384 (8 bits)  16.5, 16.8 / 19.1
     //   chunks of 1024, 512 / shares      16 x 8, 8, 4096  42.6, 42.8 / 37.8;  4 x 8, 8, 32768  70.9, 67.3 / 64.3
+    // "up to": lengths spread, "of": all alike:
+    //   whole items, four waves / one     82 x 64, 1, up to 151 (8 bits)  61.7 / 34.9;  82 x 64, 1, of 200  106.9 / 100.3;  128 x 8, 8, up to 200 (8
+    //                                     bits)  17.1 / 16.1;  63 x 64, 2, up to 250 (256)  154 / 109;  82 x 64, 1, up to 300  87.0 / 82.8;
+    //                                     60 x 40, 1, up to 300  46.6 / 46.5;  but 128 x 8, 8, up to 400  30.5 / 33.2;  82 x 64, 1, up to 500  124 / 132
+    //   of 256 elements: whole / chunks   14 x 1, 8, up to 465  19.1 / 12.1;  4 x 8, 1, of 400 (8 bits)  13.2 / 10.8;  but 100 x 2, 4, of 400
+    //                                     (8 bits)  15.6 / 21.3;  250 x 1, 4, of 500  31.7 / 33.0
+    //   of 256 elements, bf16: chunks / shares  16 x 8, 1, up to 1500  34.8 / 27.8, of 1500  46.4 / 47.6;  20 x 5, 2, of 2000  65.6 / 49.2
+    //   heads of 256, bf16, in two workgroups / one with 16 columns twice  4 x 1, 16, of 66436  102 / 69;  50 x 8, 12, of 488  92.5 / 60.4
     const int fit = wgs_per_unit(C->head_dim, C->dtype == PEQA_CACHE_FP8) * PLAN_UNITS;
     // Of bf16 rows of 256 bytes one workgroup has two tiles of every wave, 128 KB of a unit, in flight, which is enough; where a second one
     // has no more items to pass it only makes everything wait longer.  512 / 256 of them: 32 x 8, 8, 4096 (all that long)  112.1 / 102.5;
     // 16 x 8, 8, 4096  37.5 / 36.3;  8 x 32, 1, 8192  101.9 / 99.7;  but 16 x 32, 1, 2048  60 / 67, and of 8 bits 64 x 8, 8, 8192  118 / 129.
     const int wgs = C->dtype == PEQA_CACHE_BF16 && C->head_dim >= 128 && items <= PLAN_UNITS ? PLAN_UNITS : fit;
     long long slots = 0;
-    if (items >= 2 * fit || (items >= fit && span <= 1024) || span <= 512) {
-        // whole items: many, or of one length, or short.  Of very short ones a wave each; of few all tiles at once, two of each of eight waves
-        if (span <= 128 && items > fit) p.waves = 1;
+    if (items >= 2 * fit || (items >= fit && span <= 1024) || span <= 256 || (span <= 512 && (C->head_dim <= 128 || items > PLAN_UNITS / 2))) {
+        // whole items: many, or of one length, or short.  Of many short ones a wave each; of few all tiles at once, two of each of eight waves
+        if (items > fit && span <= (items >= 4 * fit ? 384 : 256)) p.waves = 1;
         else if (span > 128 && span <= 512 && items <= PLAN_UNITS && p.hb == 1 && C->head_dim <= 128) p.waves = 8;
-    } else if (rows == 1 || rows > SCAN_ROWS || span * items < 960ll * fit || units >= (1ll << 30)) {
+    } else if (rows == 1 || rows > SCAN_ROWS || span * items < (fit == PLAN_UNITS ? 480ll : 960ll) * fit || units >= (1ll << 30)) {
         // chunks: of one row, or as many as there is room for workgroups, of a tile a wave at least
         long long chunk = span * items / wgs;
         chunk = chunk < 128 ? 128 : chunk;

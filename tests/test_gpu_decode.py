@@ -200,6 +200,23 @@ def test_equal_shares(env, fp8, heads, kv_heads, dim, rows, most, window):
     check_attention(torch, peqa, cache, q, [min(n, 5) for n in lens], most, window=window, fp8=fp8)     # nothing but short rows
 
 
+@pytest.mark.parametrize("fp8,heads,kv_heads,dim,rows,most,window", [
+    (False, 16, 1, 256, 7, 130, 0), (False, 24, 2, 256, 9, 500, 0), (False, 18, 1, 256, 3, 9000, 0), (False, 16, 1, 256, 40, 16384, 0),
+    (False, 12, 1, 256, 300, 250, 0), (False, 20, 1, 256, 520, 380, 100), (False, 33, 3, 256, 50, 8192, 3001), (True, 9, 1, 256, 12, 500, 0),
+    (True, 17, 1, 256, 600, 200, 0), (False, 4, 4, 128, 520, 380, 0), (True, 2, 2, 64, 1030, 380, 0), (False, 3, 1, 256, 5, 400, 0),
+])
+def test_wide_heads_and_many_short_rows(env, fp8, heads, kv_heads, dim, rows, most, window):
+    """Heads of 256 with more than eight to a key head, and items by the thousand whose rows one wave walks, in every form of a launch."""
+    torch, peqa = env
+    print("wide", fp8, heads, kv_heads, dim, rows, most, window, flush=True)
+    gen = torch.Generator().manual_seed(rows + heads)
+    lens = [int(n) for n in torch.randint(0, min(most, 300) + 1, (rows,), generator=gen)]
+    lens[0], lens[1], lens[2], lens[rows - 1] = most, 0, 1, min(most, 4200)
+    cache = make_cache(torch, peqa, gen, lens, kv_heads, dim, 32, fp8)
+    q = torch.randn((rows, heads, dim), generator=gen).to(torch.bfloat16).cuda()
+    check_attention(torch, peqa, cache, q, lens, most, window=window, fp8=fp8)
+
+
 def test_rows_of_one_sequence_and_rows_of_none(env):
     """Several query rows of the same sequence (a prompt's tokens), sequences out of range, lengths past max_len and negative."""
     torch, peqa = env
