@@ -29,7 +29,6 @@ typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 
 constexpr int TILE = 32;                 // positions per step of a wave
 constexpr int UNIT = 64;                 // positions that shares are counted in
-constexpr int CHUNK = 4096;              // positions whose pages are in LDS at a time
 constexpr int SCAN_ROWS = 1024;          // rows of a launch of equal shares at most: every workgroup adds up their lengths
 constexpr float LOWEST = -3.0e38f;       // finite stand-in for the maximum of nothing: e^(-inf - LOWEST) is 0, not NaN
 constexpr float LN2 = 0.693147180559945309f, LOG2E = 1.44269504088896341f;
@@ -214,8 +213,11 @@ __global__ __launch_bounds__(64 * WAVES, wgs_per_unit(D, FP8)) void attend_kerne
     constexpr int VR = FP8 ? W / 4 : W / 2;           // registers of a value's segment
     constexpr int EL = FP8 ? 1 : 2;                   // bytes of an element
     constexpr bool AHEAD = HB * D <= 128 || (HB == 1 && wgs_per_unit(D, FP8) == 1);    // registers for two tiles (of 16 heads of 256: for their queries and sums)
+    // Positions of a piece, whose pages are in LDS at a time: few where a wave has an item to itself, whose rows are short (5 KB of LDS for a
+    // workgroup instead of 21: 119 rows x 64 heads of up to 8 positions 25.0 -> 20.6 us, 128 x 8 of up to 200 16.0 -> 13.5).
+    constexpr int CHUNK = WAVES == 1 ? 512 : 4096;
     __shared__ long long page_at[2][CHUNK / 8];             // where a piece's pages begin, in bytes; -1: not there
-    __shared__ RowInfo info[SCAN_ROWS];
+    __shared__ RowInfo info[WAVES == 4 ? SCAN_ROWS : 1];
     __shared__ int scan[WAVES + 6];
     __shared__ float wave_m[WAVES][HB][16], wave_l[WAVES][HB][16];
     __shared__ __attribute__((aligned(16))) float joined[WAVES][8][DS + 4];
