@@ -423,38 +423,46 @@ def check_cache(cache):
     return int(lib().peqa_check_cache(ctypes.byref(cache)))
 
 
-def _rows(x, shape, heads, dim):
-    """(pointer, row stride) of a tensor of bf16 [rows, heads, head_dim] whose rows are contiguous.  (Every attribute of a tensor that is
-    asked for takes some 0.1 us of a call's 5 to 8.)"""
+_ROWS = "tensors [rows, heads, head_dim] of bf16 whose rows are contiguous"
+
+
+def _rows(x, heads, dim):
+    """(pointer, row stride) of such a tensor with more than one row.  (Every attribute of a tensor that is asked for takes some 0.1 us of a
+    call's 6 to 8, and a function called as much.)"""
     s0, s1, s2 = x.stride()
-    assert x.shape == shape and s2 == 1 and (s1 == dim or heads == 1) and x.element_size() == 2, \
-        "tensors [rows, heads, head_dim] of bf16 whose rows are contiguous"
-    return x.data_ptr(), (s0 if shape[0] > 1 else heads * dim)
+    assert s2 == 1 and (s1 == dim or heads == 1) and x.element_size() == 2, _ROWS
+    return x.data_ptr(), s0
 
 
 def rope_append(cache, q, k, v, pos, cos, sin, q_out, seq=None, interleaved=False, stream=None):
     """q, q_out [T, heads, head_dim] or None, k, v [T, kv_heads, head_dim], pos, seq [T] int32, cos, sin [positions, rot / 2] fp32
     or None (no rotation)."""
     T, kv_heads, dim = shape = k.shape
-    assert kv_heads == cache.kv_heads and dim == cache.head_dim, "k and v [T, kv_heads, head_dim] of the cache"
-    kp, ks = _rows(k, shape, kv_heads, dim)
-    vp, vs = _rows(v, shape, kv_heads, dim)
+    assert kv_heads == cache.kv_heads and dim == cache.head_dim and v.shape == shape, "k and v [T, kv_heads, head_dim] of the cache"
+    kp, ks = _rows(k, kv_heads, dim)
+    vp, vs = _rows(v, kv_heads, dim)
     heads, qp, qs, op, os_ = 0, None, 0, None, 0
     if q is not None:
         n, heads, d = shape = q.shape
         assert n == T and d == dim
-        qp, qs = _rows(q, shape, heads, dim)
+        qp, qs = _rows(q, heads, dim)
         if q_out is not None:
-            op, os_ = _rows(q_out, shape, heads, dim)
+            assert q_out.shape == shape
+            op, os_ = _rows(q_out, heads, dim)
     elif q_out is not None:
         op = q_out.data_ptr()                  # (refused by the library)
+    if T == 1:                                 # (a single row may have any stride)
+        ks = vs = kv_heads * dim
+        qs = os_ = heads * dim
     assert pos.numel() == T and (seq is None or seq.numel() == T)
     n_pos = half = 0
     if cos is not None:
-        n_pos, half = cos.shape
-        assert sin is None or sin.shape == (n_pos, half)
-    _check(lib().peqa_rope_append(cache, T, _ptr(pos), _ptr(seq), _ptr(cos), _ptr(sin), n_pos, 2 * half, interleaved,
-                                  heads, qp, qs, kp, ks, vp, vs, op, os_, _stream(stream)), "peqa_rope_append")
+        n_pos, half = shape = cos.shape
+        assert sin is None or sin.shape == shape
+    status = (_lib or lib()).peqa_rope_append(cache, T, _ptr(pos), _ptr(seq), _ptr(cos), _ptr(sin), n_pos, 2 * half, interleaved,
+                                              heads, qp, qs, kp, ks, vp, vs, op, os_, _stream(stream))
+    if status:
+        raise PeqaError(status, "peqa_rope_append")
 
 
 def paged_attention_workspace_bytes(cache, heads, rows, max_len, window=0):
@@ -464,12 +472,16 @@ def paged_attention_workspace_bytes(cache, heads, rows, max_len, window=0):
 def paged_attention(cache, q, lens, max_len, scale, out, workspace, workspace_bytes_, lse=None, seq=None, window=0, stream=None):
     """q, out [rows, heads, head_dim], lens, seq [rows] int32, lse [rows, heads] fp32."""
     rows, heads, dim = shape = q.shape
-    qp, qs = _rows(q, shape, heads, dim)
-    op, os_ = _rows(out, shape, heads, dim)
-    assert dim == cache.head_dim and lens.numel() == rows and (seq is None or seq.numel() == rows)
+    assert out.shape == shape and dim == cache.head_dim and lens.numel() == rows and (seq is None or seq.numel() == rows)
     assert lse is None or lse.shape == (rows, heads)
-    _check(lib().peqa_paged_attention(cache, rows, heads, qp, qs, _ptr(lens), _ptr(seq), max_len, window, scale, op, os_,
-                                      _ptr(lse), _ptr(workspace), workspace_bytes_, _stream(stream)), "peqa_paged_attention")
+    qp, qs = _rows(q, heads, dim)
+    op, os_ = _rows(out, heads, dim)
+    if rows == 1:                              # (a single row may have any stride)
+        qs = os_ = heads * dim
+    status = (_lib or lib()).peqa_paged_attention(cache, rows, heads, qp, qs, _ptr(lens), _ptr(seq), max_len, window, scale, op, os_,
+                                                  _ptr(lse), _ptr(workspace), workspace_bytes_, _stream(stream))
+    if status:
+        raise PeqaError(status, "peqa_paged_attention")
 
 
 def _logits(x):
@@ -491,9 +503,10 @@ def token_logprobs(logits, targets, logp, entropy, lse, top_logp, top_ids, works
         n, top = top_ids.shape
         assert n == T and top_logp.shape == (T, top)
     assert targets is None or targets.numel() == T
-    _check(lib().peqa_token_logprobs(xp, dtype, T, V, stride, _ptr(targets), top, _ptr(logp), _ptr(entropy), _ptr(lse),
-                                     _ptr(top_logp), _ptr(top_ids), _ptr(workspace), workspace_bytes_, _stream(stream)),
-           "peqa_token_logprobs")
+    status = (_lib or lib()).peqa_token_logprobs(xp, dtype, T, V, stride, _ptr(targets), top, _ptr(logp), _ptr(entropy), _ptr(lse),
+                                                 _ptr(top_logp), _ptr(top_ids), _ptr(workspace), workspace_bytes_, _stream(stream))
+    if status:
+        raise PeqaError(status, "peqa_token_logprobs")
 
 
 def token_logprobs_bwd(logits, targets, lse, entropy, d_logp, d_entropy, d_logits, stream=None):
@@ -501,5 +514,7 @@ def token_logprobs_bwd(logits, targets, lse, entropy, d_logp, d_entropy, d_logit
     xp, dtype, T, V, stride = _logits(logits)
     dp, d_dtype, dT, dV, d_stride = _logits(d_logits)
     assert (d_dtype, dT, dV) == (dtype, T, V) and (targets is None or targets.numel() == T)
-    _check(lib().peqa_token_logprobs_bwd(xp, dtype, T, V, stride, _ptr(targets), _ptr(lse), _ptr(entropy), _ptr(d_logp),
-                                         _ptr(d_entropy), dp, d_stride, _stream(stream)), "peqa_token_logprobs_bwd")
+    status = (_lib or lib()).peqa_token_logprobs_bwd(xp, dtype, T, V, stride, _ptr(targets), _ptr(lse), _ptr(entropy), _ptr(d_logp),
+                                                     _ptr(d_entropy), dp, d_stride, _stream(stream))
+    if status:
+        raise PeqaError(status, "peqa_token_logprobs_bwd")
