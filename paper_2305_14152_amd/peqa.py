@@ -411,9 +411,11 @@ def kv_cache(k, v, table, k_scale=None, v_scale=None):
     assert k.shape == v.shape and k.dim() == 4 and k.stride() == v.stride() and k.stride(3) == 1 and k.dtype == v.dtype, \
         "pools [pages, kv_heads, page_size, head_dim] of one type with the same strides, the last 1"
     assert table.dim() == 2 and table.stride(1) == 1 and table.element_size() == 4, "table [sequences, blocks] of int32"
+    n_seqs, n_blocks = table.shape             # (a single row may have any stride)
+    assert n_seqs == 1 or table.stride(0) >= n_blocks, "table [sequences, blocks] whose rows do not overlap"
     assert k.element_size() in (1, 2)
     c = KVCache(k.data_ptr(), v.data_ptr(), table.data_ptr(), _ptr(k_scale), _ptr(v_scale), k.stride(0), k.stride(1), k.stride(2),
-                max(table.stride(0), table.shape[1]), k.shape[0], k.shape[2], k.shape[1], k.shape[3], table.shape[0], table.shape[1],
+                table.stride(0) if n_seqs > 1 else n_blocks, k.shape[0], k.shape[2], k.shape[1], k.shape[3], n_seqs, n_blocks,
                 PEQA_CACHE_FP8 if k.element_size() == 1 else PEQA_CACHE_BF16, 0)
     c.tensors = (k, v, table, k_scale, v_scale)
     return c

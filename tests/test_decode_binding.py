@@ -1,0 +1,32 @@
+"""What the Python side of the decoding and scoring calls refuses before the library is called, and what it lets through.  No tensor's
+memory is read: everything is decided from shapes, strides and types."""
+import pytest
+
+
+@pytest.fixture(scope="module")
+def env():
+    import torch
+    from paper_2305_14152_amd import peqa
+    peqa.lib()
+    return torch, peqa
+
+
+def pools(torch, kind=None):
+    k = torch.zeros((4, 2, 16, 128), dtype=kind or torch.bfloat16)
+    return k, torch.zeros_like(k)
+
+
+def test_tables_whose_rows_overlap(env):
+    """The descriptor's rows are at least a row's entries apart: what is closer would be read past its end."""
+    torch, peqa = env
+    k, v = pools(torch)
+    row = torch.zeros((1, 4), dtype=torch.int32)
+    for table in (row.expand(3, -1), torch.zeros(8, dtype=torch.int32).as_strided((3, 4), (2, 1)),
+                  torch.zeros(8, dtype=torch.int32).as_strided((2, 4), (3, 1))):
+        with pytest.raises(AssertionError, match="table"):
+            peqa.kv_cache(k, v, table)
+    # a single row may have any stride; rows further apart are as they are
+    assert peqa.kv_cache(k, v, row.expand(1, -1)).table_stride == 4
+    assert peqa.kv_cache(k, v, torch.zeros(4, dtype=torch.int32).as_strided((1, 4), (0, 1))).table_stride == 4
+    assert peqa.kv_cache(k, v, torch.zeros((3, 9), dtype=torch.int32)[:, :4]).table_stride == 9
+    assert peqa.kv_cache(k, v, torch.zeros((3, 4), dtype=torch.int32)).table_stride == 4
