@@ -405,18 +405,31 @@ def trace_end(max_kernels=32):
     return {names[i].decode(): (int(launches[i]), float(total_ms[i])) for i in range(n)}
 
 
+class _Kinds(dict):
+    """Names of tensors' types, each formed once: this module takes tensors without importing what they are made by."""
+    def __missing__(self, dtype):
+        self[dtype] = name = str(dtype).rpartition(".")[2]
+        return name
+
+
+_kind = _Kinds()
+_BF16 = ("bfloat16", "int16", "uint16")        # bf16, or its 16-bit pattern
+_FP8 = ("float8_e4m3fn", "uint8")              # the cache's 8-bit floats, or their bytes
+
+
 def kv_cache(k, v, table, k_scale=None, v_scale=None):
-    """The cache of two pools [pages, kv_heads, page_size, head_dim] (any strides, the same of both, the last 1; one byte per
-    element: 8-bit floats, two: bf16) and a table [sequences, blocks] of int32."""
+    """The cache of two pools [pages, kv_heads, page_size, head_dim] (any strides, the same of both, the last 1) of bf16 or
+    torch.float8_e4m3fn, or of their bits as 16- or 8-bit integers, and a table [sequences, blocks] of int32."""
     assert k.shape == v.shape and k.dim() == 4 and k.stride() == v.stride() and k.stride(3) == 1 and k.dtype == v.dtype, \
         "pools [pages, kv_heads, page_size, head_dim] of one type with the same strides, the last 1"
-    assert table.dim() == 2 and table.stride(1) == 1 and table.element_size() == 4, "table [sequences, blocks] of int32"
+    assert table.dim() == 2 and table.stride(1) == 1 and _kind[table.dtype] == "int32", "table [sequences, blocks] of int32"
     n_seqs, n_blocks = table.shape             # (a single row may have any stride)
     assert n_seqs == 1 or table.stride(0) >= n_blocks, "table [sequences, blocks] whose rows do not overlap"
-    assert k.element_size() in (1, 2)
+    fp8 = _kind[k.dtype] in _FP8
+    assert fp8 or _kind[k.dtype] in _BF16, "pools of bf16 or float8_e4m3fn"
     c = KVCache(k.data_ptr(), v.data_ptr(), table.data_ptr(), _ptr(k_scale), _ptr(v_scale), k.stride(0), k.stride(1), k.stride(2),
                 table.stride(0) if n_seqs > 1 else n_blocks, k.shape[0], k.shape[2], k.shape[1], k.shape[3], n_seqs, n_blocks,
-                PEQA_CACHE_FP8 if k.element_size() == 1 else PEQA_CACHE_BF16, 0)
+                PEQA_CACHE_FP8 if fp8 else PEQA_CACHE_BF16, 0)
     c.tensors = (k, v, table, k_scale, v_scale)
     return c
 

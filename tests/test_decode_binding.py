@@ -30,3 +30,18 @@ def test_tables_whose_rows_overlap(env):
     assert peqa.kv_cache(k, v, torch.zeros(4, dtype=torch.int32).as_strided((1, 4), (0, 1))).table_stride == 4
     assert peqa.kv_cache(k, v, torch.zeros((3, 9), dtype=torch.int32)[:, :4]).table_stride == 9
     assert peqa.kv_cache(k, v, torch.zeros((3, 4), dtype=torch.int32)).table_stride == 4
+
+
+def test_types_of_pools_and_table(env):
+    """8-bit pools are e4m3fn (or its bytes), 16-bit ones bf16 (or its 16-bit patterns), tables int32: nothing else of the same width."""
+    torch, peqa = env
+    table = torch.zeros((3, 4), dtype=torch.int32)
+    for kind in (torch.float8_e5m2, torch.float8_e4m3fnuz, torch.float8_e5m2fnuz, torch.int8, torch.bool, torch.float16, torch.float32):
+        with pytest.raises(AssertionError, match="pools"):
+            peqa.kv_cache(*pools(torch, kind), table)
+    for kind in (torch.float32, torch.uint32, torch.int64, torch.int16):
+        with pytest.raises(AssertionError, match="table"):
+            peqa.kv_cache(*pools(torch), torch.zeros((3, 4), dtype=kind))
+    for kind, want in ((torch.bfloat16, 0), (torch.int16, 0), (torch.uint16, 0), (torch.float8_e4m3fn, 1), (torch.uint8, 1)):
+        c = peqa.kv_cache(*pools(torch, kind), table)
+        assert c.dtype == want and peqa.check_cache(c) == peqa.PEQA_OK
