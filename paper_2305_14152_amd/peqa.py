@@ -419,7 +419,8 @@ _FP8 = ("float8_e4m3fn", "uint8")              # the cache's 8-bit floats, or th
 
 def kv_cache(k, v, table, k_scale=None, v_scale=None):
     """The cache of two pools [pages, kv_heads, page_size, head_dim] (any strides, the same of both, the last 1) of bf16 or
-    torch.float8_e4m3fn, or of their bits as 16- or 8-bit integers, and a table [sequences, blocks] of int32."""
+    torch.float8_e4m3fn, or of their bits as 16- or 8-bit integers, and a table [sequences, blocks] of int32.  k_scale, v_scale [kv_heads]
+    fp32 or None."""
     assert k.shape == v.shape and k.dim() == 4 and k.stride() == v.stride() and k.stride(3) == 1 and k.dtype == v.dtype, \
         "pools [pages, kv_heads, page_size, head_dim] of one type with the same strides, the last 1"
     assert table.dim() == 2 and table.stride(1) == 1 and _kind[table.dtype] == "int32", "table [sequences, blocks] of int32"
@@ -427,6 +428,8 @@ def kv_cache(k, v, table, k_scale=None, v_scale=None):
     assert n_seqs == 1 or table.stride(0) >= n_blocks, "table [sequences, blocks] whose rows do not overlap"
     fp8 = _kind[k.dtype] in _FP8
     assert fp8 or _kind[k.dtype] in _BF16, "pools of bf16 or float8_e4m3fn"
+    for scale in (k_scale, v_scale):
+        assert scale is None or (_kind[scale.dtype] == "float32" and scale.numel() == k.shape[1]), "scales [kv_heads] of fp32"
     c = KVCache(k.data_ptr(), v.data_ptr(), table.data_ptr(), _ptr(k_scale), _ptr(v_scale), k.stride(0), k.stride(1), k.stride(2),
                 table.stride(0) if n_seqs > 1 else n_blocks, k.shape[0], k.shape[2], k.shape[1], k.shape[3], n_seqs, n_blocks,
                 PEQA_CACHE_FP8 if fp8 else PEQA_CACHE_BF16, 0)

@@ -45,3 +45,19 @@ def test_types_of_pools_and_table(env):
     for kind, want in ((torch.bfloat16, 0), (torch.int16, 0), (torch.uint16, 0), (torch.float8_e4m3fn, 1), (torch.uint8, 1)):
         c = peqa.kv_cache(*pools(torch, kind), table)
         assert c.dtype == want and peqa.check_cache(c) == peqa.PEQA_OK
+
+
+def test_scales(env):
+    """A scale per key head, fp32, contiguous."""
+    torch, peqa = env
+    k, v = pools(torch, torch.float8_e4m3fn)
+    table = torch.zeros((3, 4), dtype=torch.int32)
+    good = torch.ones(2)
+    for bad in (torch.ones(1), torch.ones(()), torch.ones(2, dtype=torch.float64), torch.ones(2, dtype=torch.bfloat16), torch.ones(4)[::2],
+                torch.ones(1).expand(2), torch.ones(3)):
+        for args in ((bad, good), (good, bad)):
+            with pytest.raises(AssertionError):
+                peqa.kv_cache(k, v, table, *args)
+    assert peqa.check_cache(peqa.kv_cache(k, v, table, good, good.clone())) == peqa.PEQA_OK
+    assert peqa.check_cache(peqa.kv_cache(k, v, table, None, good)) == peqa.PEQA_OK
+    assert peqa.check_cache(peqa.kv_cache(k, v, table, good.view(2, 1), None)) == peqa.PEQA_OK
