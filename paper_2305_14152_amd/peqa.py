@@ -429,7 +429,8 @@ def kv_cache(k, v, table, k_scale=None, v_scale=None):
     fp8 = _kind[k.dtype] in _FP8
     assert fp8 or _kind[k.dtype] in _BF16, "pools of bf16 or float8_e4m3fn"
     for scale in (k_scale, v_scale):
-        assert scale is None or (_kind[scale.dtype] == "float32" and scale.numel() == k.shape[1]), "scales [kv_heads] of fp32"
+        assert scale is None or isinstance(scale, int) or (_kind[scale.dtype] == "float32" and scale.numel() == k.shape[1]), \
+            "scales [kv_heads] of fp32"
     c = KVCache(k.data_ptr(), v.data_ptr(), table.data_ptr(), _ptr(k_scale), _ptr(v_scale), k.stride(0), k.stride(1), k.stride(2),
                 table.stride(0) if n_seqs > 1 else n_blocks, k.shape[0], k.shape[2], k.shape[1], k.shape[3], n_seqs, n_blocks,
                 PEQA_CACHE_FP8 if fp8 else PEQA_CACHE_BF16, 0)

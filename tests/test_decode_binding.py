@@ -61,3 +61,11 @@ def test_scales(env):
     assert peqa.check_cache(peqa.kv_cache(k, v, table, good, good.clone())) == peqa.PEQA_OK
     assert peqa.check_cache(peqa.kv_cache(k, v, table, None, good)) == peqa.PEQA_OK
     assert peqa.check_cache(peqa.kv_cache(k, v, table, good.view(2, 1), None)) == peqa.PEQA_OK
+
+
+def test_scales_may_be_addresses(env):
+    """As elsewhere in the binding, an integer is taken for a device address."""
+    torch, peqa = env
+    k, v = pools(torch, torch.float8_e4m3fn)
+    c = peqa.kv_cache(k, v, torch.zeros((3, 4), dtype=torch.int32), 0x10000, 0x20000)
+    assert (c.k_scale, c.v_scale) == (0x10000, 0x20000) and peqa.check_cache(c) == peqa.PEQA_OK
