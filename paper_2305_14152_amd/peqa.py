@@ -453,6 +453,14 @@ def _rows(x, heads, dim):
     return x.data_ptr(), s0
 
 
+def _index(t, n):
+    """Pointer of n positions, lengths, sequences or words; None -> NULL."""
+    if t is None:
+        return None
+    assert _kind[t.dtype] == "int32" and t.numel() == n and t.is_contiguous(), "a contiguous tensor of %d int32" % n
+    return t.data_ptr()
+
+
 def rope_append(cache, q, k, v, pos, cos, sin, q_out, seq=None, interleaved=False, stream=None):
     """q, q_out [T, heads, head_dim] or None, k, v [T, kv_heads, head_dim], pos, seq [T] int32, cos, sin [positions, rot / 2] fp32
     or None (no rotation)."""
@@ -473,12 +481,11 @@ def rope_append(cache, q, k, v, pos, cos, sin, q_out, seq=None, interleaved=Fals
     if T == 1:                                 # (a single row may have any stride)
         ks = vs = kv_heads * dim
         qs = os_ = heads * dim
-    assert pos.numel() == T and (seq is None or seq.numel() == T)
     n_pos = half = 0
     if cos is not None:
         n_pos, half = shape = cos.shape
         assert sin is None or sin.shape == shape
-    status = (_lib or lib()).peqa_rope_append(cache, T, _ptr(pos), _ptr(seq), _ptr(cos), _ptr(sin), n_pos, 2 * half, interleaved,
+    status = (_lib or lib()).peqa_rope_append(cache, T, _index(pos, T), _index(seq, T), _ptr(cos), _ptr(sin), n_pos, 2 * half, interleaved,
                                               heads, qp, qs, kp, ks, vp, vs, op, os_, _stream(stream))
     if status:
         raise PeqaError(status, "peqa_rope_append")
@@ -491,13 +498,13 @@ def paged_attention_workspace_bytes(cache, heads, rows, max_len, window=0):
 def paged_attention(cache, q, lens, max_len, scale, out, workspace, workspace_bytes_, lse=None, seq=None, window=0, stream=None):
     """q, out [rows, heads, head_dim], lens, seq [rows] int32, lse [rows, heads] fp32."""
     rows, heads, dim = shape = q.shape
-    assert out.shape == shape and dim == cache.head_dim and lens.numel() == rows and (seq is None or seq.numel() == rows)
+    assert out.shape == shape and dim == cache.head_dim
     assert lse is None or lse.shape == (rows, heads)
     qp, qs = _rows(q, heads, dim)
     op, os_ = _rows(out, heads, dim)
     if rows == 1:                              # (a single row may have any stride)
         qs = os_ = heads * dim
-    status = (_lib or lib()).peqa_paged_attention(cache, rows, heads, qp, qs, _ptr(lens), _ptr(seq), max_len, window, scale, op, os_,
+    status = (_lib or lib()).peqa_paged_attention(cache, rows, heads, qp, qs, _index(lens, rows), _index(seq, rows), max_len, window, scale, op, os_,
                                                   _ptr(lse), _ptr(workspace), workspace_bytes_, _stream(stream))
     if status:
         raise PeqaError(status, "peqa_paged_attention")
@@ -521,8 +528,7 @@ def token_logprobs(logits, targets, logp, entropy, lse, top_logp, top_ids, works
     if top_ids is not None:
         n, top = top_ids.shape
         assert n == T and top_logp.shape == (T, top)
-    assert targets is None or targets.numel() == T
-    status = (_lib or lib()).peqa_token_logprobs(xp, dtype, T, V, stride, _ptr(targets), top, _ptr(logp), _ptr(entropy), _ptr(lse),
+    status = (_lib or lib()).peqa_token_logprobs(xp, dtype, T, V, stride, _index(targets, T), top, _ptr(logp), _ptr(entropy), _ptr(lse),
                                                  _ptr(top_logp), _ptr(top_ids), _ptr(workspace), workspace_bytes_, _stream(stream))
     if status:
         raise PeqaError(status, "peqa_token_logprobs")
@@ -532,8 +538,8 @@ def token_logprobs_bwd(logits, targets, lse, entropy, d_logp, d_entropy, d_logit
     """d_logits [T, vocab], the gradient of sum(d_logp * logp + d_entropy * entropy); may be `logits` itself."""
     xp, dtype, T, V, stride = _logits(logits)
     dp, d_dtype, dT, dV, d_stride = _logits(d_logits)
-    assert (d_dtype, dT, dV) == (dtype, T, V) and (targets is None or targets.numel() == T)
-    status = (_lib or lib()).peqa_token_logprobs_bwd(xp, dtype, T, V, stride, _ptr(targets), _ptr(lse), _ptr(entropy), _ptr(d_logp),
+    assert (d_dtype, dT, dV) == (dtype, T, V)
+    status = (_lib or lib()).peqa_token_logprobs_bwd(xp, dtype, T, V, stride, _index(targets, T), _ptr(lse), _ptr(entropy), _ptr(d_logp),
                                                      _ptr(d_entropy), dp, d_stride, _stream(stream))
     if status:
         raise PeqaError(status, "peqa_token_logprobs_bwd")

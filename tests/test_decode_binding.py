@@ -69,3 +69,63 @@ def test_scales_may_be_addresses(env):
     k, v = pools(torch, torch.float8_e4m3fn)
     c = peqa.kv_cache(k, v, torch.zeros((3, 4), dtype=torch.int32), 0x10000, 0x20000)
     assert (c.k_scale, c.v_scale) == (0x10000, 0x20000) and peqa.check_cache(c) == peqa.PEQA_OK
+
+
+def bound(torch, peqa):
+    """A cache, its inputs for three tokens, and logits with all that the scoring calls take."""
+    k, v = pools(torch)
+    cache = peqa.kv_cache(k, v, torch.zeros((3, 4), dtype=torch.int32))
+    bf16 = lambda *shape: torch.zeros(shape, dtype=torch.bfloat16)  # noqa: E731
+    ints = lambda n: torch.zeros(n, dtype=torch.int32)  # noqa: E731
+    append = dict(q=bf16(3, 4, 128), k=bf16(3, 2, 128), v=bf16(3, 2, 128), pos=ints(3), cos=torch.zeros(64, 64), sin=torch.zeros(64, 64),
+                  q_out=bf16(3, 4, 128), seq=ints(3))
+    attend = dict(q=bf16(3, 4, 128), lens=ints(3), max_len=64, scale=1.0, out=bf16(3, 4, 128), workspace=None, workspace_bytes_=0,
+                  lse=torch.zeros(3, 4), seq=ints(3))
+    score = dict(logits=bf16(3, 100), targets=ints(3), logp=torch.zeros(3), entropy=torch.zeros(3), lse=torch.zeros(3), top_logp=torch.zeros(3, 5),
+                 top_ids=torch.zeros((3, 5), dtype=torch.int32), workspace=None, workspace_bytes_=0)
+    back = dict(logits=bf16(3, 100), targets=ints(3), lse=torch.zeros(3), entropy=torch.zeros(3), d_logp=torch.zeros(3), d_entropy=torch.zeros(3),
+                d_logits=bf16(3, 100))
+    return cache, append, attend, score, back
+
+
+class Called(Exception):
+    pass
+
+
+@pytest.fixture()
+def calls(env, monkeypatch):
+    """The four calls with good arguments, and a library that says that it was reached instead of launching anything."""
+    torch, peqa = env
+    cache, append, attend, score, back = bound(torch, peqa)
+
+    class Library:
+        def __getattr__(self, name):
+            def reached(*args):
+                raise Called(name)
+            return reached
+    monkeypatch.setattr(peqa, "_lib", Library())
+
+    def call(name, **changes):
+        first, good = {"rope_append": ((cache,), append), "paged_attention": ((cache,), attend), "token_logprobs": ((), score),
+                       "token_logprobs_bwd": ((), back)}[name]
+        return getattr(peqa, name)(*first, stream=0, **{**good, **changes})
+
+    for name in ("rope_append", "paged_attention", "token_logprobs", "token_logprobs_bwd"):
+        with pytest.raises(Called):
+            call(name)
+    return call
+
+
+INDEXES = [("rope_append", "pos"), ("rope_append", "seq"), ("paged_attention", "lens"), ("paged_attention", "seq"), ("token_logprobs", "targets"),
+           ("token_logprobs_bwd", "targets")]
+
+
+@pytest.mark.parametrize("name,argument", INDEXES)
+def test_positions_lengths_sequences_and_words_are_int32(env, calls, name, argument):
+    torch, _ = env
+    for bad in (torch.zeros(3, dtype=torch.int64), torch.zeros(3), torch.zeros(3, dtype=torch.int16), torch.zeros(3, dtype=torch.uint32),
+                torch.zeros(2, dtype=torch.int32), torch.zeros(4, dtype=torch.int32), torch.zeros(6, dtype=torch.int32)[::2]):
+        with pytest.raises(AssertionError):
+            calls(name, **{argument: bad})
+    with pytest.raises(Called):
+        calls(name, **{argument: torch.zeros((3, 1), dtype=torch.int32)})
