@@ -449,7 +449,7 @@ def _rows(x, heads, dim):
     """(pointer, row stride) of such a tensor with more than one row.  (Every attribute of a tensor that is asked for takes some 0.1 us of a
     call's 6 to 8, and a function called as much.)"""
     s0, s1, s2 = x.stride()
-    assert s2 == 1 and (s1 == dim or heads == 1) and x.element_size() == 2, _ROWS
+    assert s2 == 1 and (s1 == dim or heads == 1) and _kind[x.dtype] in _BF16, _ROWS
     return x.data_ptr(), s0
 
 
@@ -512,9 +512,9 @@ def paged_attention(cache, q, lens, max_len, scale, out, workspace, workspace_by
 
 def _logits(x):
     """(pointer, type, rows, words, row stride) of logits [T, vocab]."""
-    (T, V), (s0, s1), size = x.shape, x.stride(), x.element_size()
-    assert (s1 == 1 or V == 1) and size in (2, 4), "logits [T, vocab] of bf16 or fp32 with contiguous rows"
-    return x.data_ptr(), PEQA_LOGITS_F32 if size == 4 else PEQA_LOGITS_BF16, T, V, s0 if T > 1 else V
+    (T, V), (s0, s1), kind = x.shape, x.stride(), _kind[x.dtype]
+    assert (s1 == 1 or V == 1) and (kind == "float32" or kind in _BF16), "logits [T, vocab] of bf16 or fp32 with contiguous rows"
+    return x.data_ptr(), PEQA_LOGITS_F32 if kind == "float32" else PEQA_LOGITS_BF16, T, V, s0 if T > 1 else V
 
 
 def token_logprobs_workspace_bytes(T, vocab, top=0):

@@ -129,3 +129,21 @@ def test_positions_lengths_sequences_and_words_are_int32(env, calls, name, argum
             calls(name, **{argument: bad})
     with pytest.raises(Called):
         calls(name, **{argument: torch.zeros((3, 1), dtype=torch.int32)})
+
+
+@pytest.mark.parametrize("name,arguments", [("rope_append", ("q",)), ("rope_append", ("k",)), ("rope_append", ("v",)), ("rope_append", ("q_out",)),
+                                            ("paged_attention", ("q",)), ("paged_attention", ("out",)), ("token_logprobs", ("logits",)),
+                                            ("token_logprobs_bwd", ("logits", "d_logits")), ("token_logprobs_bwd", ("d_logits",))])
+def test_queries_keys_values_and_logits_are_bf16(env, calls, name, arguments):
+    """bf16 or its 16-bit pattern, logits also fp32: nothing else of the same width."""
+    torch, peqa = env
+    shape = {"k": (3, 2, 128), "v": (3, 2, 128), "logits": (3, 100), "d_logits": (3, 100)}.get(arguments[0], (3, 4, 128))
+    for kind in (torch.float16, torch.int32, torch.uint8, torch.float64):
+        with pytest.raises(AssertionError, match="bf16"):
+            calls(name, **{a: torch.zeros(shape, dtype=kind) for a in arguments})
+    for kind in (torch.bfloat16, torch.int16, torch.uint16):
+        with pytest.raises(Called):
+            calls(name, **{a: torch.zeros(shape, dtype=kind) for a in arguments})
+    good = {a: torch.zeros(shape, dtype=torch.float32) for a in arguments}
+    with pytest.raises(Called if "logits" in arguments else AssertionError):
+        calls(name, **good)
