@@ -461,6 +461,14 @@ def _index(t, n):
     return t.data_ptr()
 
 
+def _floats(t, n):
+    """Pointer of n fp32 numbers at least; None -> NULL, a device address as it is."""
+    if t is None or isinstance(t, int):
+        return t
+    assert _kind[t.dtype] == "float32" and t.numel() >= n and t.is_contiguous(), "a contiguous tensor of %d float32" % n
+    return t.data_ptr()
+
+
 def rope_append(cache, q, k, v, pos, cos, sin, q_out, seq=None, interleaved=False, stream=None):
     """q, q_out [T, heads, head_dim] or None, k, v [T, kv_heads, head_dim], pos, seq [T] int32, cos, sin [positions, rot / 2] fp32
     or None (no rotation)."""
@@ -485,8 +493,9 @@ def rope_append(cache, q, k, v, pos, cos, sin, q_out, seq=None, interleaved=Fals
     if cos is not None:
         n_pos, half = shape = cos.shape
         assert sin is None or sin.shape == shape
-    status = (_lib or lib()).peqa_rope_append(cache, T, _index(pos, T), _index(seq, T), _ptr(cos), _ptr(sin), n_pos, 2 * half, interleaved,
-                                              heads, qp, qs, kp, ks, vp, vs, op, os_, _stream(stream))
+    status = (_lib or lib()).peqa_rope_append(cache, T, _index(pos, T), _index(seq, T), _floats(cos, n_pos * half),
+                                              _floats(sin, n_pos * half), n_pos, 2 * half, interleaved, heads, qp, qs, kp, ks, vp, vs, op,
+                                              os_, _stream(stream))
     if status:
         raise PeqaError(status, "peqa_rope_append")
 

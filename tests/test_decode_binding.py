@@ -147,3 +147,19 @@ def test_queries_keys_values_and_logits_are_bf16(env, calls, name, arguments):
     good = {a: torch.zeros(shape, dtype=torch.float32) for a in arguments}
     with pytest.raises(Called if "logits" in arguments else AssertionError):
         calls(name, **good)
+
+
+@pytest.mark.parametrize("argument", ["cos", "sin"])
+def test_rotation_tables_are_fp32(env, calls, argument):
+    """bf16 tables, as models often keep them, would be read as half as many fp32 numbers and past their end."""
+    torch, peqa = env
+    for kind in (torch.bfloat16, torch.float16, torch.float64, torch.int32):
+        with pytest.raises(AssertionError, match="float32"):
+            calls("rope_append", **{argument: torch.zeros((64, 64), dtype=kind)})
+    for bad in (torch.zeros((64, 128))[:, ::2], torch.zeros((64, 65))[:, :64], torch.zeros((64, 64)).T, torch.zeros((1, 64)).expand(64, -1)):
+        with pytest.raises(AssertionError):
+            calls("rope_append", **{argument: bad})
+    with pytest.raises(Called):
+        calls("rope_append", cos=None, sin=None)
+    with pytest.raises(Called):
+        calls("rope_append", cos=torch.zeros((64, 128))[:32, :64].contiguous(), sin=torch.zeros((32, 64)))
