@@ -454,7 +454,7 @@ def _rows(x, heads, dim):
 
 
 def _index(t, n):
-    """Pointer of n positions, lengths, sequences or words; None -> NULL."""
+    """Pointer of n positions, lengths, sequences, words or alternatives; None -> NULL."""
     if t is None:
         return None
     assert _kind[t.dtype] == "int32" and t.numel() == n and t.is_contiguous(), "a contiguous tensor of %d int32" % n
@@ -514,7 +514,7 @@ def paged_attention(cache, q, lens, max_len, scale, out, workspace, workspace_by
     if rows == 1:                              # (a single row may have any stride)
         qs = os_ = heads * dim
     status = (_lib or lib()).peqa_paged_attention(cache, rows, heads, qp, qs, _index(lens, rows), _index(seq, rows), max_len, window, scale, op, os_,
-                                                  _ptr(lse), _ptr(workspace), workspace_bytes_, _stream(stream))
+                                                  _floats(lse, rows * heads), _ptr(workspace), workspace_bytes_, _stream(stream))
     if status:
         raise PeqaError(status, "peqa_paged_attention")
 
@@ -537,8 +537,9 @@ def token_logprobs(logits, targets, logp, entropy, lse, top_logp, top_ids, works
     if top_ids is not None:
         n, top = top_ids.shape
         assert n == T and top_logp.shape == (T, top)
-    status = (_lib or lib()).peqa_token_logprobs(xp, dtype, T, V, stride, _index(targets, T), top, _ptr(logp), _ptr(entropy), _ptr(lse),
-                                                 _ptr(top_logp), _ptr(top_ids), _ptr(workspace), workspace_bytes_, _stream(stream))
+    status = (_lib or lib()).peqa_token_logprobs(xp, dtype, T, V, stride, _index(targets, T), top, _floats(logp, T), _floats(entropy, T),
+                                                 _floats(lse, T), _floats(top_logp, T * top), _index(top_ids, T * top), _ptr(workspace),
+                                                 workspace_bytes_, _stream(stream))
     if status:
         raise PeqaError(status, "peqa_token_logprobs")
 
@@ -548,7 +549,7 @@ def token_logprobs_bwd(logits, targets, lse, entropy, d_logp, d_entropy, d_logit
     xp, dtype, T, V, stride = _logits(logits)
     dp, d_dtype, dT, dV, d_stride = _logits(d_logits)
     assert (d_dtype, dT, dV) == (dtype, T, V)
-    status = (_lib or lib()).peqa_token_logprobs_bwd(xp, dtype, T, V, stride, _index(targets, T), _ptr(lse), _ptr(entropy), _ptr(d_logp),
-                                                     _ptr(d_entropy), dp, d_stride, _stream(stream))
+    status = (_lib or lib()).peqa_token_logprobs_bwd(xp, dtype, T, V, stride, _index(targets, T), _floats(lse, T), _floats(entropy, T),
+                                                     _floats(d_logp, T), _floats(d_entropy, T), dp, d_stride, _stream(stream))
     if status:
         raise PeqaError(status, "peqa_token_logprobs_bwd")

@@ -163,3 +163,31 @@ def test_rotation_tables_are_fp32(env, calls, argument):
         calls("rope_append", cos=None, sin=None)
     with pytest.raises(Called):
         calls("rope_append", cos=torch.zeros((64, 128))[:32, :64].contiguous(), sin=torch.zeros((32, 64)))
+
+
+FLOATS = [("paged_attention", "lse"), ("token_logprobs", "logp"), ("token_logprobs", "entropy"), ("token_logprobs", "lse"), ("token_logprobs", "top_logp"),
+          ("token_logprobs_bwd", "lse"), ("token_logprobs_bwd", "entropy"), ("token_logprobs_bwd", "d_logp"), ("token_logprobs_bwd", "d_entropy")]
+
+
+@pytest.mark.parametrize("name,argument", FLOATS)
+def test_numbers_of_rows_are_fp32_and_as_many(env, calls, name, argument):
+    torch, _ = env
+    shape = {"paged_attention": (3, 4)}.get(name, (3, 5) if argument == "top_logp" else (3,))
+    for kind in (torch.bfloat16, torch.float16, torch.float64, torch.int32):
+        with pytest.raises(AssertionError, match="float32"):
+            calls(name, **{argument: torch.zeros(shape, dtype=kind)})
+    for bad in (torch.zeros((2,) + shape[1:]), torch.zeros(()), torch.zeros((1,) + shape[1:]).expand(shape), torch.zeros((6,) + shape[1:])[::2]):
+        with pytest.raises(AssertionError):
+            calls(name, **{argument: bad})
+    if len(shape) == 1:                            # buffers made for more rows, and device addresses
+        for good in (torch.zeros(8), 0x10000):
+            with pytest.raises(Called):
+                calls(name, **{argument: good})
+
+
+def test_alternatives_are_int32(env, calls):
+    torch, _ = env
+    for bad in (torch.zeros((3, 5), dtype=torch.int64), torch.zeros((3, 5)), torch.zeros((3, 10), dtype=torch.int32)[:, ::2],
+                torch.zeros((2, 5), dtype=torch.int32), torch.zeros((3, 4), dtype=torch.int32)):
+        with pytest.raises(AssertionError):
+            calls("token_logprobs", top_ids=bad)
