@@ -480,6 +480,9 @@ peqa_status peqa_token_logprobs(const void *logits, int32_t dtype, int32_t T, in
  *   lse, and entropy where d_entropy is given, as peqa_token_logprobs left them;  d_logp or d_entropy may be NULL (= 0)
  *   d_logits: rows d_stride elements apart, may be logits itself with the same stride; only the first `vocab` elements of
  *   a row are written.  Rows whose two factors are 0 (logits not read), or whose lse is -inf, are zeros.
+ * An fp32 lse is rounded, to 2^-24 of itself: p_j is off by 2^-17 of itself at most for |lse| < 256.  Of rows whose lse is larger, those of
+ * the type's lowest value only among them, the rest is found from the row first (they take two to three times as long), unless lse differs
+ * from the row's own by more than 2^-22 of itself: it is then taken to be of more words than these, and used as it is.
  */
 peqa_status peqa_token_logprobs_bwd(const void *logits, int32_t dtype, int32_t T, int32_t vocab, int64_t stride,
                                     const int32_t *targets, const float *lse, const float *entropy, const float *d_logp,

@@ -520,6 +520,13 @@ __global__ __launch_bounds__(256) void logprobs_join_kernel(LogprobArgs a)
 // logits, a tenth of them ignored and not read, at 5.7 TB/s.  A thread has 32 bytes of a row, one vector of eight or two (fp32: 1000 rows
 // of 32000 48 us with one, 52 with two; bf16: the 2048 rows 51.9 and 46.1).  The target's place is looked for a vector at a time and the
 // entropy's terms are left out where there are none, else it is 19.5 vector instructions a logit and 47.7 us.
+//
+// p_j = e^(x_j - lse) is off by the rounding of lse to fp32, 2^-17 of p_j for an lse under 256.  Of a row whose lse is further from zero
+// (all words masked with the lowest value: nothing is left of log V in it) one workgroup first adds up the row: r = log sum e^(x - lse) is
+// what the rounding left, p_j = e^((x_j - lse) - r).  It reads the whole row before it writes any of it, so the gradient may still
+// replace the logits.  Such rows cost two to three times as much (2048 of 32000 bf16 logits 134 us, 1000 of 50257 fp32 ones 140 for 74), the
+// others the code's weight (4000 of 2000 7.6 -> 7.9 us).
+constexpr float LSE_FAR = 256.f;
 constexpr int grad_vectors(bool f32) { return f32 ? 1 : 2; }
 template <bool F32, bool ENTROPY>
 __global__ __launch_bounds__(256) void logprobs_bwd_kernel(GradArgs a)
@@ -535,20 +542,18 @@ __global__ __launch_bounds__(256) void logprobs_bwd_kernel(GradArgs a)
     const bool none = (g == 0.f && h == 0.f) || lse == -__builtin_inff();
     E *out = static_cast<E *>(a.d_logits) + row * a.d_stride;
     const bool aligned = (int)((reinterpret_cast<uintptr_t>(out) & 15u) / sizeof(E)) == r.off;
-    const int all = r.vectors(a.V), v0 = block * GRAD_VECTORS * 256 + (int)threadIdx.x;
-#pragma unroll
-    for (int k = 0; k < GRAD_VECTORS; ++k) {
-        const int v = v0 + k * 256;
-        if (v >= all) return;
+    const int all = r.vectors(a.V);
+    // vector v of the row, whose logits are `raw`; rest: what lse lacks (REST), else 0
+    auto write = [&](int v, const Raw &raw, float rest, auto REST) __attribute__((always_inline)) {
         float x[8];
         if (none) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) x[i] = 0.f;
         } else {
-            floats<F32>(read_vector<F32>(r, v, a.V), x);
+            floats<F32>(raw, x);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const float logp = x[i] - lse, p = exp_of(logp);
+                const float logp = REST ? (x[i] - lse) - rest : x[i] - lse, p = exp_of(logp);
                 x[i] = ENTROPY ? -p * (g + h * (fmaxf(logp, FAR) + H)) : -p * g;
             }
             const int target = t + r.off - 8 * v;              // its place in this vector
@@ -574,6 +579,47 @@ __global__ __launch_bounds__(256) void logprobs_bwd_kernel(GradArgs a)
                 else out[j] = (uint16_t)float_to_bf16_bits(x[i]);
             }
         }
+    };
+    if (__builtin_expect(!none && fabsf(lse) >= LSE_FAR && fabsf(lse) < __builtin_inff(), 0)) {
+        // (the same for all workgroups of the row; not the first of every one, which can all be on one die)
+        if (block != (int)((unsigned)row % (unsigned)a.blocks)) return;
+        __shared__ float wave_s[4];
+        constexpr int FLIGHT = 4;
+        auto walk = [&](auto each) __attribute__((always_inline)) {
+#pragma unroll 1
+            for (int v0 = (int)threadIdx.x; v0 < all; v0 += FLIGHT * 256) {
+                Raw w[FLIGHT];
+#pragma unroll
+                for (int k = 0; k < FLIGHT; ++k) w[k] = v0 + k * 256 < all ? read_vector<F32>(r, v0 + k * 256, a.V) : nothing<F32>();
+#pragma unroll
+                for (int k = 0; k < FLIGHT; ++k) each(v0 + k * 256, w[k]);
+            }
+        };
+        float s = 0.f;
+        walk([&](int, const Raw &raw) {
+            float x[8], sum = 0.f;
+            floats<F32>(raw, x);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sum += exp_of(x[i] - lse);
+            s += sum;
+        });
+        s = wave_sum(s);
+        if ((threadIdx.x & 63) == 0) wave_s[threadIdx.x >> 6] = s;
+        __syncthreads();
+        float rest = logf(wave_s[0] + wave_s[1] + wave_s[2] + wave_s[3]);
+        // an lse that is off by more than rounding is not this row's alone (words in several pieces), and is taken as it is
+        if (!(fabsf(rest) <= fabsf(lse) * 0x1p-22f)) rest = 0.f;
+        walk([&](int v, const Raw &raw) {
+            if (v < all) write(v, raw, rest, std::true_type{});
+        });
+        return;
+    }
+    const int v0 = block * GRAD_VECTORS * 256 + (int)threadIdx.x;
+#pragma unroll
+    for (int k = 0; k < GRAD_VECTORS; ++k) {
+        if (v0 + k * 256 >= all) return;
+        const int v = v0 + k * 256;
+        write(v, none ? Raw{} : read_vector<F32>(r, v, a.V), 0.f, std::false_type{});
     }
 }
 
