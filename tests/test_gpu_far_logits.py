@@ -130,3 +130,68 @@ def test_an_lse_over_more_words_is_taken_as_it_is(env, far):
         y, d = x[:, part * 1500:part * 1500 + 1500], torch.empty((T, 1500), device="cuda")
         peqa.token_logprobs_bwd(y, t, lse, None, g, None, d)
         close(torch, d, *gradient64(host(y), t.tolist(), host(g), zero, host(lse)))
+
+
+# ---- the forward ------------------------------------------------------------------------------------------------------
+# logp, the alternatives' and the entropy do not depend on where a row lies: (x - m) - log s, with m the row's largest, x - m rounded to
+# 2^-24 of itself, and sums of positive terms (taken: 2^-18).  2^-17 (1 + |value|) bounds each, whatever m is; lse alone has m's rounding.
+
+def check_forward(torch, peqa, x, targets, top):
+    T, V = x.shape
+    logp, H, lse, best, ids = forward(torch, peqa, x, targets, top)
+    near = lambda got, want: got == want if not math.isfinite(want) else abs(got - want) <= 2.0 ** -17 * (1 + abs(want))  # noqa: E731
+    d, t = host(x), targets.tolist()
+    for r in range(T):
+        m = d[r].max()
+        e = np.exp(d[r] - m)
+        log_s = math.log(e.sum())
+        p = e / e.sum()
+        assert abs(float(lse[r]) - (m + log_s)) <= 2.0 ** -17 * (1 + log_s) + 2.0 ** -24 * abs(m + log_s), r
+        assert near(float(H[r]), log_s - float((p * np.where(e > 0, d[r] - m, 0.0)).sum())), (r, float(H[r]))
+        assert near(float(logp[r]), d[r, t[r]] - m - log_s if 0 <= t[r] < V else 0.0), (r, float(logp[r]))
+        if top:
+            order = np.argsort(-d[r], kind="stable")[:top]
+            assert ids[r].tolist() == order.tolist(), r
+            assert all(near(got, d[r, j] - m - log_s) for got, j in zip(best[r].tolist(), order)), r
+
+
+@pytest.mark.parametrize("f32", [False, True])
+@pytest.mark.parametrize("T,V,top", [(9, 7, 7), (9, 1000, 32), (9, 32003, 5), (9, 50257, 0), (300, 1500, 20), (9, 200003, 32)])
+def test_forward_far_from_zero(env, f32, T, V, top):
+    """Rows around +-1000 and +-10000, of the lowest value only (log probabilities -log V, entropy log V), of one word more, of half of them."""
+    torch, peqa = env
+    print("forward far", f32, T, V, top, flush=True)
+    dtype = torch.float32 if f32 else torch.bfloat16
+    gen = torch.Generator().manual_seed(V + T)
+    x, _ = rows(torch, gen, T, V, dtype)
+    low = torch.finfo(dtype).min
+    for r, far in enumerate((1000, -1000, 10000, -10000)):
+        x[r] = (x[r].float() + far).to(dtype)
+    x[4] = low
+    x[5] = low
+    x[5, V // 2] = 3.0
+    x[6, ::2] = low
+    x[6, 1::2] = -math.inf
+    x[7, 3:] = low
+    targets = torch.randint(0, V, (T,), generator=gen, dtype=torch.int32)
+    targets[1], targets[6] = -100, 2
+    check_forward(torch, peqa, x, targets.cuda(), top)
+
+
+@pytest.mark.parametrize("f32", [False, True])
+def test_more_large_logits_in_a_slice_than_are_gathered(env, f32):
+    """A row that is cut into slices, each with more than 1024 logits no smaller than its bound: large ones in eight of every 64 vectors of
+    eight, so that with 32 alternatives the bound is among the small ones.  They are then found one by one within a slice."""
+    torch, peqa = env
+    V, top = 200000, 32
+    slices = (V + 14) // 8 // 2048
+    round256 = lambda n: (n + 255) // 256 * 256  # noqa: E731
+    assert slices > 8 and peqa.token_logprobs_workspace_bytes(1, V, top) == round256(slices * 16) + round256(slices * top * 8)
+    x, _ = rows(torch, torch.Generator().manual_seed(3), 1, V, torch.float32 if f32 else torch.bfloat16)
+    large = (torch.arange(V) // 8) % 64 < 8
+    assert int(large.sum()) // slices > 1500
+    order = torch.randperm(int(large.sum()), generator=torch.Generator().manual_seed(4))
+    x[0, large.cuda()] = (1000 + 0.001 * order).to(x.dtype).cuda()
+    check_forward(torch, peqa, x, torch.tensor([9], dtype=torch.int32).cuda(), top)
+    x[0, large.cuda()] = (1000 + 0.001 * torch.arange(len(order))).to(x.dtype).cuda()          # the last slice has the answer
+    check_forward(torch, peqa, x, torch.tensor([V - 1], dtype=torch.int32).cuda(), top)
