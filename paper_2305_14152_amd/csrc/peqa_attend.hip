@@ -22,6 +22,14 @@ using namespace peqa::host;
 
 namespace peqa {
 
+// How a call is cut: column blocks of a workgroup, workgroups' worth of heads per key head, heads of a workgroup, chunks or shares.
+struct AttendPlan {
+    int hb, waves, blocks, per_wg, splits, chunk_units, shares, entries;
+    long long grid;
+    size_t part_bytes, ml_bytes, parts_bytes;
+};
+AttendPlan attend_plan(const peqa_kv_cache *C, int rows, int heads, int max_len, int window);
+
 namespace {
 
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
@@ -703,13 +711,6 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a)
     if (a.lse && at == 0) a.lse[(size_t)item.row * a.heads + head] = any ? (top + __builtin_amdgcn_logf(total)) * LN2 : -__builtin_inff();
 }
 
-// How a call is cut: column blocks of a workgroup, workgroups' worth of heads per key head, heads of a workgroup, chunks or shares.
-struct AttendPlan {
-    int hb, waves, blocks, per_wg, splits, chunk_units, shares, entries;
-    long long grid;
-    size_t part_bytes, ml_bytes, parts_bytes;
-};
-
 template <int D, bool FP8>
 hipError_t launch_attend(const AttendArgs &a, const AttendPlan &p, hipStream_t stream)
 {
@@ -729,6 +730,8 @@ hipError_t launch_attend(const AttendArgs &a, const AttendPlan &p, hipStream_t s
     trace_after(KID_ATTEND_JOIN, stream);
     return hipGetLastError();
 }
+
+}  // namespace
 
 AttendPlan attend_plan(const peqa_kv_cache *C, int rows, int heads, int max_len, int window)
 {
@@ -794,6 +797,8 @@ AttendPlan attend_plan(const peqa_kv_cache *C, int rows, int heads, int max_len,
     }
     return p;
 }
+
+namespace {
 
 peqa_status check_attend(const peqa_kv_cache *C, int32_t rows, int32_t heads, int32_t max_len, int32_t window)
 {
