@@ -444,9 +444,11 @@ peqa_status peqa_rope_append(const peqa_kv_cache *C, int32_t T, const int32_t *p
  *   max_len: the host's bound of lens, at most n_blocks * page_size (PEQA_ERR_SHAPE); longer rows are cut to it.  The work
  *            is split for it, so a tight bound is faster.  heads: a multiple of kv_heads.
  *   workspace: peqa_paged_attention_workspace_bytes(C, rows, heads, max_len, window).
- * Products and sums are fp32.  The softmax weights are rounded for the matrix instructions: against bf16 values in two
- * bf16 parts (16 bits), against 8-bit values to fp16 (11 bits; of weights under 2^-28 of the row's largest to 2^-39 of it).  The same call gives the same bits; the order in which a
- * row's positions are added depends on max_len, window, the number of rows and, with many long rows, their lengths.
+ * Products and sums are fp32.  The softmax weights are rounded for the matrix instructions: against bf16 values in two bf16 parts (16
+ * bits), against 8-bit values in two fp16 parts (22 bits) where up to eight heads share a key head, else to fp16 (11 bits; of weights
+ * under 2^-28 of the row's largest to 2^-39 of it).
+ * The same call gives the same bits; the order in which a row's positions are added depends on max_len, window, the number of rows and,
+ * with many long rows, their lengths.
  */
 size_t peqa_paged_attention_workspace_bytes(const peqa_kv_cache *C, int32_t rows, int32_t heads, int32_t max_len,
                                             int32_t window);

@@ -207,12 +207,15 @@ template <bool HI> __device__ __forceinline__ uint32_t fp8_f16(uint32_t v)
 // alone are as many, one with up to 512.
 constexpr int wgs_per_unit(int D, bool fp8) { return D > 128 && !fp8 ? 1 : 2; }
 
-template <int D, bool FP8, int HB, int WAVES>
+template <int D, bool FP8, int HB, int WAVES, bool TWICE>
 __global__ __launch_bounds__(64 * WAVES, wgs_per_unit(D, FP8)) void attend_kernel(AttendArgs a)
 {
-    // Columns of the matrix instructions: 16 heads with 8-bit values, whose weights are fp16; with bf16 values eight heads twice,
-    // the upper ones with what rounding the weights to bf16 leaves, so that they have 16 bits.
-    constexpr int COLS = FP8 ? 16 : 8;
+    // Columns of the matrix instructions: eight heads twice, the upper ones with what rounding the weights leaves, so that they have 16 bits
+    // against bf16 values and 22, as fp16, against 8-bit ones (64 rows of up to 8192 with eight heads to a key head 115.5 us with one part,
+    // 115.9 with two, three caches in turn).  More than eight heads on 8-bit values have a column each and weights of 11 bits: with eight at
+    // a time 12 heads take 132 us for 120, 128 rows of up to 200 with 8 x 12 heads 19.7 for 14.5.
+    static_assert(TWICE || FP8);
+    constexpr int COLS = TWICE ? 8 : 16;
     constexpr int QK = D / 32;                        // steps of the scores' product
     constexpr int SEG = D > 128 ? D / 128 : 1;        // segments of 128 elements of a value
     constexpr int W = D / 16 / SEG;                   // neighbouring elements of a segment that a lane has: 4 or 8
@@ -444,8 +447,15 @@ __global__ __launch_bounds__(64 * WAVES, wgs_per_unit(D, FP8)) void attend_kerne
             for (int e = 0; e < SEG * W; ++e) acc[b][e] *= fall;
             if constexpr (FP8) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    weight[b][i] = __builtin_bit_cast(uint32_t, f16x2{(_Float16)p[2 * i], (_Float16)p[2 * i + 1]});
+                for (int i = 0; i < 4; ++i) {
+                    const f16x2 near = {(_Float16)p[2 * i], (_Float16)p[2 * i + 1]};
+                    if constexpr (TWICE) {
+                        const f16x2 rest = {(_Float16)(p[2 * i] - (float)near[0]), (_Float16)(p[2 * i + 1] - (float)near[1])};
+                        weight[b][i] = __builtin_bit_cast(uint32_t, c < 8 ? near : rest);
+                    } else {
+                        weight[b][i] = __builtin_bit_cast(uint32_t, near);
+                    }
+                }
             } else {
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
@@ -547,7 +557,7 @@ __global__ __launch_bounds__(64 * WAVES, wgs_per_unit(D, FP8)) void attend_kerne
                         for (int e = 0; e < W; e += 4) {
                             f32x4 x;
 #pragma unroll
-                            for (int i = 0; i < 4; ++i) x[i] = FP8 ? acc[b][s * W + e + i][r] : add_halves(acc[b][s * W + e + i][r]);
+                            for (int i = 0; i < 4; ++i) x[i] = TWICE ? add_halves(acc[b][s * W + e + i][r]) : acc[b][s * W + e + i][r];
                             // this lane: elements 128 s + W (4 g + r) + e
                             if (c >> 3 == half) *reinterpret_cast<f32x4 *>(&joined[wave][c & 7][W * (4 * g + r) + e]) = x;
                         }
@@ -714,11 +724,20 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a)
 template <int D, bool FP8>
 hipError_t launch_attend(const AttendArgs &a, const AttendPlan &p, hipStream_t stream)
 {
-    auto kernel = p.waves == 1 ? attend_kernel<D, FP8, 1, 1> : attend_kernel<D, FP8, 1, 4>;
+    auto kernel = p.waves == 1 ? attend_kernel<D, FP8, 1, 1, true> : attend_kernel<D, FP8, 1, 4, true>;
     if constexpr (D <= 128)
-        if (p.waves == 8) kernel = attend_kernel<D, FP8, 1, 8>;
-    if constexpr (D <= 128 || !FP8)
-        if (p.hb == 2) kernel = p.waves == 1 ? attend_kernel<D, FP8, 2, 1> : attend_kernel<D, FP8, 2, 4>;
+        if (p.waves == 8) kernel = attend_kernel<D, FP8, 1, 8, true>;
+    if constexpr (FP8) {
+        if (p.per_wg > 8) {
+            kernel = p.waves == 1 ? attend_kernel<D, true, 1, 1, false> : attend_kernel<D, true, 1, 4, false>;
+            if constexpr (D <= 128) {
+                if (p.waves == 8) kernel = attend_kernel<D, true, 1, 8, false>;
+                if (p.hb == 2) kernel = p.waves == 1 ? attend_kernel<D, true, 2, 1, false> : attend_kernel<D, true, 2, 4, false>;
+            }
+        }
+    } else {
+        if (p.hb == 2) kernel = p.waves == 1 ? attend_kernel<D, false, 2, 1, true> : attend_kernel<D, false, 2, 4, true>;
+    }
     trace_before(KID_ATTEND, stream);
     hipLaunchKernelGGL(kernel, dim3((unsigned)p.grid), dim3(64 * p.waves), 0, stream, a);
     trace_after(KID_ATTEND, stream);
@@ -736,7 +755,7 @@ hipError_t launch_attend(const AttendArgs &a, const AttendPlan &p, hipStream_t s
 AttendPlan attend_plan(const peqa_kv_cache *C, int rows, int heads, int max_len, int window)
 {
     AttendPlan p{};
-    const int group = heads / C->kv_heads, cols = C->dtype == PEQA_CACHE_FP8 ? 16 : 8;
+    const int group = heads / C->kv_heads, cols = C->dtype == PEQA_CACHE_FP8 && group > 8 ? 16 : 8;
     p.hb = (C->head_dim <= 128 || C->dtype == PEQA_CACHE_BF16) && group > cols ? 2 : 1;    // (16 heads of 256 with 8 bits fill the registers)
     p.per_wg = cols * p.hb;
     p.blocks = (group + p.per_wg - 1) / p.per_wg;

@@ -110,8 +110,8 @@ FORMS = {
 }
 
 
-HEADS = [(64, False, 5), (64, False, 11), (64, False, 17), (64, True, 16), (64, True, 19), (128, False, 8), (128, False, 16), (128, True, 3), (128, True, 32),
-         (256, False, 7), (256, False, 9), (256, True, 12), (256, True, 18)]
+HEADS = [(64, False, 5), (64, False, 11), (64, False, 17), (64, True, 6), (64, True, 16), (64, True, 19), (128, False, 8), (128, False, 16), (128, True, 3),
+         (128, True, 9), (128, True, 32), (256, False, 7), (256, False, 9), (256, True, 8), (256, True, 12), (256, True, 18)]
 
 
 def two_blocks(dim, fp8, group):
