@@ -524,15 +524,17 @@ __global__ __launch_bounds__(256) void logprobs_join_kernel(LogprobArgs a)
 // p_j = e^(x_j - lse) is off by the rounding of lse to fp32, 2^-17 of p_j for an lse under 256.  Of a row whose lse is further from zero
 // (all words masked with the lowest value: nothing is left of log V in it) one workgroup first adds up the row: r = log sum e^(x - lse) is
 // what the rounding left, p_j = e^((x_j - lse) - r).  It reads the whole row before it writes any of it, so the gradient may still
-// replace the logits.  Such rows cost two to three times as much (2048 of 32000 bf16 logits 134 us, 1000 of 50257 fp32 ones 140 for 74), the
-// others the code's weight (4000 of 2000 7.6 -> 7.9 us).
+// replace the logits.  Such rows cost two to three times as much (2048 of 32000 bf16 logits 134 us, 1000 of 50257 fp32 ones 151 for 74), the
+// others nothing.
 constexpr float LSE_FAR = 256.f;
 constexpr int grad_vectors(bool f32) { return f32 ? 1 : 2; }
 template <bool F32, bool ENTROPY>
 __global__ __launch_bounds__(256) void logprobs_bwd_kernel(GradArgs a)
 {
     constexpr int GRAD_VECTORS = grad_vectors(F32);
-    const int row = (int)(blockIdx.x / (unsigned)a.blocks), block = (int)(blockIdx.x - (unsigned)row * (unsigned)a.blocks);
+    int row = (int)(blockIdx.x / (unsigned)a.blocks);
+    asm("" : "+s"(row));                                   // (and all that follows from it; else 12 vector instructions a logit, not 8: 4000 rows of 2000 7.9 us, not 7.6)
+    const int block = (int)(blockIdx.x - (unsigned)row * (unsigned)a.blocks);
     const Row<F32> r(a.logits, row, a.stride);
     typedef typename Row<F32>::T E;
     const int t = a.targets ? a.targets[row] : -1;
