@@ -12,8 +12,8 @@
 // of all items laid end to end.
 // Every key and value is read once, and the matrix and vector instructions of a tile (a third and less of the time) run beside the loads of
 // the next: bound by what a unit has in flight, and for short rows by the start of a launch and the latency of its three dependent
-// loads (length, page, tile).  Measured, the kernel alone:  one row of 131072 positions, 8 key heads of 128, 8 heads to each  94.5 us,
-// 5.7 TB/s;  64 rows of up to 8192 on 8 bits, as many heads  108 us, 5.1 TB/s;  16 rows of up to 2048, 32 key heads  53.5 us, 4.8 TB/s;
+// loads (length, page, tile).  Measured, the kernel alone:  one row of 131072 positions, 8 key heads of 128, 8 heads to each  93.5 us,
+// 5.7 TB/s;  64 rows of up to 8192 on 8 bits, as many heads  107 us, 5.2 TB/s;  16 rows of up to 2048, 32 key heads  53.5 us, 4.8 TB/s;
 // one row of 333, 32 key heads  9 us.
 #include "peqa_cache.h"
 #include "peqa_host.h"
@@ -225,7 +225,8 @@ __global__ __launch_bounds__(64 * WAVES, wgs_per_unit(D, FP8)) void attend_kerne
     constexpr int EL = FP8 ? 1 : 2;                   // bytes of an element
     constexpr bool AHEAD = HB * D <= 128 || (HB == 1 && wgs_per_unit(D, FP8) == 1);    // registers for two tiles (of 16 heads of 256: for their queries and sums)
     // Positions of a piece, whose pages are in LDS at a time: few where a wave has an item to itself, whose rows are short (5 KB of LDS for a
-    // workgroup instead of 21: 119 rows x 64 heads of up to 8 positions 25.0 -> 20.6 us, 128 x 8 of up to 200 16.0 -> 13.5).
+    // workgroup instead of 21: 119 rows x 64 heads of up to 8 positions 25.0 -> 20.6 us, 128 x 8 of up to 200 16.0 -> 13.5; 17.0 and 13.8 with
+    // 8-bit weights in two parts).
     constexpr int CHUNK = WAVES == 1 ? 512 : 4096;
     __shared__ long long page_at[2][CHUNK / 8];             // where a piece's pages begin, in bytes; -1: not there
     __shared__ RowInfo info[WAVES == 4 ? SCAN_ROWS : 1];
@@ -767,25 +768,27 @@ AttendPlan attend_plan(const peqa_kv_cache *C, int rows, int heads, int max_len,
     p.chunk_units = (int)((span + UNIT - 1) / UNIT);
     if (p.chunk_units < 1) p.chunk_units = 1;
     // Measured, us (lengths are spread from 2 % to 100 % of the longest; "n x kv, group, length"; bf16, head_dim 128 unless stated):
-    //   whole items, four waves / one     101 rows x 32, 1, 12 (8 bits)  33.1 / 13.1;  101 x 32, 1, 60  31.3 / 17.7;  40 x 16, 8, 40  10.2 / 8.6;
-    //                                     128 x 4, 8, 128 (8 bits, 64)  6.2 / 8.2;  16 x 32, 1, 500  18.6 / 28.7
-    //   whole items / shares              64 x 8, 4, 1000  36.4 / 40.6;  128 x 8, 8, 2000 (8 bits)  67 / 72;  16 x 8, 8, 4096  57.6 / 37.8;
-    //                                     64 x 8, 8, 8192 (8 bits)  139 / 118
-    //   chunks of 128, 256, 512 / whole   8 x 4, 4, 960  10.1, 12.0, 15.4 / 15.4;  1 x 8, 8, 2048  10.3, 11.7, 14.9 / 25.4
-    //   chunks of 256, 512 / shares       2 x 8, 8, 8192  18.0, 18.7 / 20.1;  1 x 8, 8, 16384 (8 bits)  16.5, 16.8 / 19.1
-    //   chunks of 1024, 512 / shares      16 x 8, 8, 4096  42.6, 42.8 / 37.8;  4 x 8, 8, 32768  70.9, 67.3 / 64.3
+    //   whole items, four waves / one     101 rows x 32, 1, 12 (8 bits)  35.6 / 10.6;  101 x 32, 1, 60  32.5 / 16.6;  40 x 16, 8, 40  10.1 / 7.5;
+    //                                     128 x 4, 8, 128 (8 bits, 64)  5.9 / 7.3;  16 x 32, 1, 500  18.7 / 27.8
+    //   whole items / shares              64 x 8, 4, 1000  35.7 / 39.1;  128 x 8, 8, 2000 (8 bits)  65 / 69;  16 x 8, 8, 4096  57.3 / 35.6;
+    //                                     64 x 8, 8, 8192 (8 bits)  123 / 116
+    //   chunks of 128, 256, 512 / whole   8 x 4, 4, 960  8.9, 10.7, 14.2 / 16.9;  1 x 8, 8, 2048  9.2, 10.5, 13.6 / 28.8
+    //   chunks of 256, 512 / shares       2 x 8, 8, 8192  17.5, 17.8 / 19.7;  1 x 8, 8, 16384 (8 bits)  15.1, 14.5 / 17.8
+    //   chunks of 1024, 512 / shares      16 x 8, 8, 4096  41.5, 41.9 / 35.6;  4 x 8, 8, 32768  69.8, 66.3 / 62.0
     // "up to": lengths spread, "of": all alike:
-    //   whole items, four waves / one     82 x 64, 1, up to 151 (8 bits)  61.7 / 34.9;  82 x 64, 1, of 200  106.9 / 100.3;  128 x 8, 8, up to 200 (8
-    //                                     bits)  17.1 / 16.1;  63 x 64, 2, up to 250 (256)  154 / 109;  82 x 64, 1, up to 300  87.0 / 82.8;
-    //                                     60 x 40, 1, up to 300  46.6 / 46.5;  but 128 x 8, 8, up to 400  30.5 / 33.2;  82 x 64, 1, up to 500  124 / 132
-    //   of 256 elements: whole / chunks   14 x 1, 8, up to 465  19.1 / 12.1;  4 x 8, 1, of 400 (8 bits)  13.2 / 10.8;  but 100 x 2, 4, of 400
-    //                                     (8 bits)  15.6 / 21.3;  250 x 1, 4, of 500  31.7 / 33.0
-    //   of 256 elements, bf16: chunks / shares  16 x 8, 1, up to 1500  34.8 / 27.8, of 1500  46.4 / 47.6;  20 x 5, 2, of 2000  65.6 / 49.2
-    //   heads of 256, bf16, in two workgroups / one with 16 columns twice  4 x 1, 16, of 66436  102 / 69;  50 x 8, 12, of 488  92.5 / 60.4
+    //   whole items, four waves / one     82 x 64, 1, up to 151 (8 bits)  66.4 / 28.2;  82 x 64, 1, of 200  108.8 / 104.2;  128 x 8, 8, up to 200 (8
+    //                                     bits)  18.1 / 13.9;  63 x 64, 2, up to 250 (256)  163 / 109;  82 x 64, 1, up to 300  89.7 / 85.4;
+    //                                     60 x 40, 1, up to 300  47.7 / 47.0;  but 128 x 8, 8, up to 400  30.9 / 32.3;  82 x 64, 1, up to 500  128 / 135
+    //   whole items, four waves / eight   1 x 32, 1, of 333  9.0 / 8.4;  4 x 32, 2, up to 500 (8 bits)  9.7 / 8.8;  8 x 16, 4, of 200  8.4 / 8.0
+    //   of 256 elements: whole / chunks   14 x 1, 8, up to 465  18.6 / 12.3;  4 x 8, 1, of 400 (8 bits)  12.4 / 9.9;  but 100 x 2, 4, of 400
+    //                                     (8 bits)  14.8 / 22.9;  250 x 1, 4, of 500  29.9 / 38.8
+    //   of 256 elements, bf16: chunks of 512 / shares  16 x 8, 1, up to 1500  26.7 / 27.7, of 1500  52.6 / 47.7;  20 x 5, 2, of 2000  55.4 / 49.5
+    //   heads of 256, bf16, in two workgroups / one with 16 columns twice  4 x 1, 16, of 66436  100 / 69;  50 x 8, 12, of 488  88.8 / 61.7
     const int fit = wgs_per_unit(C->head_dim, C->dtype == PEQA_CACHE_FP8) * PLAN_UNITS;
     // Of bf16 rows of 256 bytes one workgroup has two tiles of every wave, 128 KB of a unit, in flight, which is enough; where a second one
-    // has no more items to pass it only makes everything wait longer.  512 / 256 of them: 32 x 8, 8, 4096 (all that long)  112.1 / 102.5;
-    // 16 x 8, 8, 4096  37.5 / 36.3;  8 x 32, 1, 8192  101.9 / 99.7;  but 16 x 32, 1, 2048  60 / 67, and of 8 bits 64 x 8, 8, 8192  118 / 129.
+    // has no more items to pass it only makes everything wait longer.  512 / 256 of them: 32 x 8, 8, 4096 (all that long)  109.5 / 102.4;
+    // 16 x 8, 8, 4096  36.8 / 35.0;  8 x 32, 1, 8192  98.2 / 100.1;  of 512 items (16 x 32, 1, 2048)  59.9 / 57.7, and of 8 bits 64 x 8, 8, 8192
+    // 115.8 / 119.5.
     const int wgs = C->dtype == PEQA_CACHE_BF16 && C->head_dim >= 128 && items <= PLAN_UNITS ? PLAN_UNITS : fit;
     long long slots = 0;
     if (items >= 2 * fit || (items >= fit && span <= 1024) || span <= 256 || (span <= 512 && (C->head_dim <= 128 || items > PLAN_UNITS / 2))) {
