@@ -469,6 +469,14 @@ def _floats(t, n):
     return t.data_ptr()
 
 
+def _room(t, n):
+    """Pointer of a workspace of n bytes; None -> NULL (refused where one is needed), a device address as it is."""
+    if t is None or isinstance(t, int):
+        return t
+    assert t.nbytes >= n and t.is_contiguous(), "a contiguous workspace of %d bytes" % n
+    return t.data_ptr()
+
+
 def rope_append(cache, q, k, v, pos, cos, sin, q_out, seq=None, interleaved=False, stream=None):
     """q, q_out [T, heads, head_dim] or None, k, v [T, kv_heads, head_dim], pos, seq [T] int32, cos, sin [positions, rot / 2] fp32
     or None (no rotation)."""
@@ -514,7 +522,7 @@ def paged_attention(cache, q, lens, max_len, scale, out, workspace, workspace_by
     if rows == 1:                              # (a single row may have any stride)
         qs = os_ = heads * dim
     status = (_lib or lib()).peqa_paged_attention(cache, rows, heads, qp, qs, _index(lens, rows), _index(seq, rows), max_len, window, scale, op, os_,
-                                                  _floats(lse, rows * heads), _ptr(workspace), workspace_bytes_, _stream(stream))
+                                                  _floats(lse, rows * heads), _room(workspace, workspace_bytes_), workspace_bytes_, _stream(stream))
     if status:
         raise PeqaError(status, "peqa_paged_attention")
 
@@ -538,8 +546,8 @@ def token_logprobs(logits, targets, logp, entropy, lse, top_logp, top_ids, works
         n, top = top_ids.shape
         assert n == T and top_logp.shape == (T, top)
     status = (_lib or lib()).peqa_token_logprobs(xp, dtype, T, V, stride, _index(targets, T), top, _floats(logp, T), _floats(entropy, T),
-                                                 _floats(lse, T), _floats(top_logp, T * top), _index(top_ids, T * top), _ptr(workspace),
-                                                 workspace_bytes_, _stream(stream))
+                                                 _floats(lse, T), _floats(top_logp, T * top), _index(top_ids, T * top),
+                                                 _room(workspace, workspace_bytes_), workspace_bytes_, _stream(stream))
     if status:
         raise PeqaError(status, "peqa_token_logprobs")
 

@@ -191,3 +191,14 @@ def test_alternatives_are_int32(env, calls):
                 torch.zeros((2, 5), dtype=torch.int32), torch.zeros((3, 4), dtype=torch.int32)):
         with pytest.raises(AssertionError):
             calls("token_logprobs", top_ids=bad)
+
+
+@pytest.mark.parametrize("name", ["paged_attention", "token_logprobs"])
+def test_workspaces_are_as_large_as_they_are_said_to_be(env, calls, name):
+    torch, _ = env
+    for room, said in ((torch.zeros(255, dtype=torch.uint8), 256), (torch.zeros(63), 256), (torch.zeros(512, dtype=torch.uint8)[::2], 256)):
+        with pytest.raises(AssertionError):
+            calls(name, workspace=room, workspace_bytes_=said)
+    for room, said in ((torch.zeros(256, dtype=torch.uint8), 256), (torch.zeros(64), 256), (torch.zeros(1000, dtype=torch.uint8), 256), (0x10000, 256)):
+        with pytest.raises(Called):
+            calls(name, workspace=room, workspace_bytes_=said)
