@@ -453,19 +453,19 @@ def _rows(x, heads, dim):
     return x.data_ptr(), s0
 
 
-def _index(t, n):
-    """Pointer of n positions, lengths, sequences, words or alternatives; None -> NULL."""
+def _index(t, n=None):
+    """Pointer of n positions, lengths, sequences, words or alternatives (of a shape that was compared: n is left out); None -> NULL."""
     if t is None:
         return None
-    assert _kind[t.dtype] == "int32" and t.numel() == n and t.is_contiguous(), "a contiguous tensor of %d int32" % n
+    assert _kind[t.dtype] == "int32" and t.is_contiguous() and (n is None or t.numel() == n), "a contiguous tensor of int32, one of each"
     return t.data_ptr()
 
 
-def _floats(t, n):
-    """Pointer of n fp32 numbers at least; None -> NULL, a device address as it is."""
+def _floats(t, n=0):
+    """Pointer of n fp32 numbers at least (of a shape that was compared: n is left out); None -> NULL, a device address as it is."""
     if t is None or isinstance(t, int):
         return t
-    assert _kind[t.dtype] == "float32" and t.numel() >= n and t.is_contiguous(), "a contiguous tensor of %d float32" % n
+    assert _kind[t.dtype] == "float32" and t.is_contiguous() and (n == 0 or t.numel() >= n), "a contiguous tensor of float32, one of each"
     return t.data_ptr()
 
 
@@ -501,9 +501,8 @@ def rope_append(cache, q, k, v, pos, cos, sin, q_out, seq=None, interleaved=Fals
     if cos is not None:
         n_pos, half = shape = cos.shape
         assert sin is None or sin.shape == shape
-    status = (_lib or lib()).peqa_rope_append(cache, T, _index(pos, T), _index(seq, T), _floats(cos, n_pos * half),
-                                              _floats(sin, n_pos * half), n_pos, 2 * half, interleaved, heads, qp, qs, kp, ks, vp, vs, op,
-                                              os_, _stream(stream))
+    status = (_lib or lib()).peqa_rope_append(cache, T, _index(pos, T), _index(seq, T), _floats(cos), _floats(sin), n_pos,
+                                              2 * half, interleaved, heads, qp, qs, kp, ks, vp, vs, op, os_, _stream(stream))
     if status:
         raise PeqaError(status, "peqa_rope_append")
 
@@ -522,7 +521,7 @@ def paged_attention(cache, q, lens, max_len, scale, out, workspace, workspace_by
     if rows == 1:                              # (a single row may have any stride)
         qs = os_ = heads * dim
     status = (_lib or lib()).peqa_paged_attention(cache, rows, heads, qp, qs, _index(lens, rows), _index(seq, rows), max_len, window, scale, op, os_,
-                                                  _floats(lse, rows * heads), _room(workspace, workspace_bytes_), workspace_bytes_, _stream(stream))
+                                                  _floats(lse), _room(workspace, workspace_bytes_), workspace_bytes_, _stream(stream))
     if status:
         raise PeqaError(status, "peqa_paged_attention")
 
@@ -546,8 +545,8 @@ def token_logprobs(logits, targets, logp, entropy, lse, top_logp, top_ids, works
         n, top = top_ids.shape
         assert n == T and top_logp.shape == (T, top)
     status = (_lib or lib()).peqa_token_logprobs(xp, dtype, T, V, stride, _index(targets, T), top, _floats(logp, T), _floats(entropy, T),
-                                                 _floats(lse, T), _floats(top_logp, T * top), _index(top_ids, T * top),
-                                                 _room(workspace, workspace_bytes_), workspace_bytes_, _stream(stream))
+                                                 _floats(lse, T), _floats(top_logp), _index(top_ids), _room(workspace, workspace_bytes_),
+                                                 workspace_bytes_, _stream(stream))
     if status:
         raise PeqaError(status, "peqa_token_logprobs")
 
