@@ -434,6 +434,46 @@ peqa_status peqa_rope_append(const peqa_kv_cache *C, int32_t T, const int32_t *p
                              int64_t q_out_stride, void *stream);
 
 /*
+ * peqa_rope_append for decoders that normalise the heads of queries and keys before the rotation, and for caches that positions have left
+ * (peqa_cache_evict), where a token's place is not its position.  Of every head of q and k
+ *   r = (mean_d x_d^2 + eps)^(-1/2),   y_d = r x_d w_d,
+ * y is rotated by pos[t] and goes to q_out, or to place[t] of the sequence; v is stored as it is.
+ *   place [T] int32, or NULL: pos;  q_weight, k_weight [head_dim] fp32 (16-byte aligned), each or NULL: ones;  eps > 0 (PEQA_ERR_PARAM)
+ * Sums and rotation are fp32 and what is stored is rounded once.  A head whose sum of squares passes fp32's range is zeros.
+ * Everything else as in peqa_rope_append: tokens with place < 0 or past the table are skipped too, and the places of a call are
+ * different.
+ */
+peqa_status peqa_norm_rope_append(const peqa_kv_cache *C, int32_t T, const int32_t *pos, const int32_t *place, const int32_t *seq,
+                                  const float *cos_table, const float *sin_table, int32_t n_pos, int32_t rot, int32_t interleaved,
+                                  const float *q_weight, const float *k_weight, float eps, int32_t heads, const uint16_t *q,
+                                  int64_t q_stride, const uint16_t *k, int64_t k_stride, const uint16_t *v, int64_t v_stride,
+                                  uint16_t *q_out, int64_t q_out_stride, void *stream);
+
+/*
+ * The same norms and rotation without a cache, for training, and their gradients.
+ *   y = R(pos[t]) (r x w);   with g = R^T dy, z = r x, u = g w:   dx = r (u - z mean_d(u z)),   dw_d = sum over tokens and heads of g_d z_d
+ *   q, q_out, d_q_out, dq [T, heads, head_dim], k, k_out, d_k_out, dk [T, kv_heads, head_dim] bf16, rows strides apart (multiples of 8,
+ *   pointers 16-byte aligned: members of a stacked query/key/value output, and of its gradient, can be passed as they lie)
+ *   head_dim 64, 128 or 256;  q_out may be q itself, dq d_q_out itself (with the same stride), k likewise
+ *   d_q_weight, d_k_weight [head_dim] fp32 out (overwritten), each or NULL (PEQA's training leaves norms as they are: with both NULL no
+ *   workspace is needed)
+ *   workspace: peqa_norm_rope_bwd_workspace_bytes(T, heads, kv_heads, head_dim).
+ * A token with pos < 0, or pos >= n_pos (where rotated), has zeros for outputs and gradients and no part in dw.  Sums are fp32 in a fixed
+ * order: the same call gives the same bits.
+ */
+peqa_status peqa_norm_rope(int32_t T, const int32_t *pos, const float *cos_table, const float *sin_table, int32_t n_pos, int32_t rot,
+                           int32_t interleaved, const float *q_weight, const float *k_weight, float eps, int32_t head_dim, int32_t heads,
+                           int32_t kv_heads, const uint16_t *q, int64_t q_stride, const uint16_t *k, int64_t k_stride, uint16_t *q_out,
+                           int64_t q_out_stride, uint16_t *k_out, int64_t k_out_stride, void *stream);
+size_t peqa_norm_rope_bwd_workspace_bytes(int32_t T, int32_t heads, int32_t kv_heads, int32_t head_dim);
+peqa_status peqa_norm_rope_bwd(int32_t T, const int32_t *pos, const float *cos_table, const float *sin_table, int32_t n_pos, int32_t rot,
+                               int32_t interleaved, const float *q_weight, const float *k_weight, float eps, int32_t head_dim, int32_t heads,
+                               int32_t kv_heads, const uint16_t *q, int64_t q_stride, const uint16_t *k, int64_t k_stride,
+                               const uint16_t *d_q_out, int64_t d_q_out_stride, const uint16_t *d_k_out, int64_t d_k_out_stride,
+                               uint16_t *dq, int64_t dq_stride, uint16_t *dk, int64_t dk_stride, float *d_q_weight, float *d_k_weight,
+                               void *workspace, size_t workspace_bytes, void *stream);
+
+/*
  * Attention of one query token per row over its sequence's cache: for row r (sequence seq[r]; NULL: r), head h and
  * its key head h / (heads / kv_heads), over the positions j in [max(0, len - window), len), len = lens[r] (window 0: all)
  *   x_j = scale * <q[r,h], k_j>;   out[r,h] = sum_j exp(x_j) v_j / sum_j exp(x_j);   lse[r,h] = log sum_j exp(x_j)

@@ -1036,7 +1036,8 @@ const char *const kKernelNames[peqa::KID_COUNT] = {
     "quantize", "rowsum", "gemm_y", "gemm_dds", "gemm_dx", "scale_dy", "reduce_partials", "adamw", "gemv",
     "gemv_finish", "group_table", "dds_kept", "dz_partial", "dz_finish", "transpose_pad", "gemm_dw", "gemm_bwd", "gemm_multi_y",
     "gemm_multi_dds", "gemm_multi_dx", "gemm_finish", "rope_append", "attend", "attend_join", "logprobs", "logprobs_join",
-    "logprobs_bwd"};
+    "logprobs_bwd", "norm_rope_append", "norm_rope", "norm_rope_bwd", "norm_weights", "shared", "shared_join", "attend_weights",
+    "evict_select", "evict_move"};
 
 }  // namespace
 namespace {

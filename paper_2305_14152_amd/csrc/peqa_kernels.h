@@ -387,6 +387,8 @@ enum {
     KID_REDUCE, KID_ADAMW, KID_GEMV, KID_GEMV_FINISH, KID_GROUP_TABLE, KID_DDS_KEPT, KID_DZ_PARTIAL, KID_DZ_FINISH,
     KID_TRANSPOSE, KID_GEMM_DW, KID_GEMM_BWD, KID_GEMM_MULTI_Y, KID_GEMM_MULTI_DDS, KID_GEMM_MULTI_DX, KID_GEMM_FINISH,
     KID_ROPE_APPEND, KID_ATTEND, KID_ATTEND_JOIN, KID_LOGPROBS, KID_LOGPROBS_JOIN, KID_LOGPROBS_BWD,
+    KID_NORM_ROPE_APPEND, KID_NORM_ROPE, KID_NORM_ROPE_BWD, KID_NORM_WEIGHTS, KID_SHARED, KID_SHARED_JOIN, KID_ATTEND_WEIGHTS,
+    KID_EVICT_SELECT, KID_EVICT_MOVE,
     KID_COUNT
 };
 

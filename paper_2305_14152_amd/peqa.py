@@ -24,7 +24,8 @@ EXPORTS = ["peqa_check_layout", "peqa_packed_words", "peqa_num_scales", "peqa_wo
            "peqa_set_option", "peqa_get_option", "peqa_linear_fwd_static",
            "peqa_block_workspace_bytes", "peqa_block_fwd", "peqa_block_bwd", "peqa_trace_select",
            "peqa_check_cache", "peqa_rope_append", "peqa_paged_attention_workspace_bytes", "peqa_paged_attention",
-           "peqa_token_logprobs_workspace_bytes", "peqa_token_logprobs", "peqa_token_logprobs_bwd"]
+           "peqa_token_logprobs_workspace_bytes", "peqa_token_logprobs", "peqa_token_logprobs_bwd",
+           "peqa_norm_rope_append", "peqa_norm_rope", "peqa_norm_rope_bwd_workspace_bytes", "peqa_norm_rope_bwd"]
 
 
 class Layout(ctypes.Structure):
@@ -150,6 +151,16 @@ def lib():
         L.peqa_token_logprobs.restype = i32
         L.peqa_token_logprobs_bwd.argtypes = [vp, i32, i32, i32, i64, vp, vp, vp, vp, vp, vp, i64, vp]
         L.peqa_token_logprobs_bwd.restype = i32
+        f32, sides = ctypes.c_float, [vp, i64, vp, i64]
+        norms = [i32, vp, vp, vp, i32, i32, i32, vp, vp, f32, i32, i32, i32]
+        L.peqa_norm_rope_append.argtypes = [CP, i32, vp, vp, vp, vp, vp, i32, i32, i32, vp, vp, f32, i32, *sides, *sides, vp]
+        L.peqa_norm_rope_append.restype = i32
+        L.peqa_norm_rope.argtypes = [*norms, *sides, *sides, vp]
+        L.peqa_norm_rope.restype = i32
+        L.peqa_norm_rope_bwd_workspace_bytes.argtypes = [i32, i32, i32, i32]
+        L.peqa_norm_rope_bwd_workspace_bytes.restype = sz
+        L.peqa_norm_rope_bwd.argtypes = [*norms, *sides, *sides, *sides, vp, vp, vp, sz, vp]
+        L.peqa_norm_rope_bwd.restype = i32
         _lib = L
     return _lib
 
@@ -477,9 +488,8 @@ def _room(t, n):
     return t.data_ptr()
 
 
-def rope_append(cache, q, k, v, pos, cos, sin, q_out, seq=None, interleaved=False, stream=None):
-    """q, q_out [T, heads, head_dim] or None, k, v [T, kv_heads, head_dim], pos, seq [T] int32, cos, sin [positions, rot / 2] fp32
-    or None (no rotation)."""
+def _append_rows(cache, q, k, v, q_out):
+    """(tokens, heads, pointers and row strides of q, k, v, q_out) of new tokens."""
     T, kv_heads, dim = shape = k.shape
     assert kv_heads == cache.kv_heads and dim == cache.head_dim and v.shape == shape, "k and v [T, kv_heads, head_dim] of the cache"
     kp, ks = _rows(k, kv_heads, dim)
@@ -497,14 +507,80 @@ def rope_append(cache, q, k, v, pos, cos, sin, q_out, seq=None, interleaved=Fals
     if T == 1:                                 # (a single row may have any stride)
         ks = vs = kv_heads * dim
         qs = os_ = heads * dim
-    n_pos = half = 0
-    if cos is not None:
-        n_pos, half = shape = cos.shape
-        assert sin is None or sin.shape == shape
-    status = (_lib or lib()).peqa_rope_append(cache, T, _index(pos, T), _index(seq, T), _floats(cos), _floats(sin), n_pos,
-                                              2 * half, interleaved, heads, qp, qs, kp, ks, vp, vs, op, os_, _stream(stream))
+    return T, heads, qp, qs, kp, ks, vp, vs, op, os_
+
+
+def _angles(cos, sin):
+    """(positions, rotated elements) of the tables."""
+    if cos is None:
+        return 0, 0
+    n_pos, half = shape = cos.shape
+    assert sin is None or sin.shape == shape
+    return n_pos, 2 * half
+
+
+def rope_append(cache, q, k, v, pos, cos, sin, q_out, seq=None, interleaved=False, stream=None):
+    """q, q_out [T, heads, head_dim] or None, k, v [T, kv_heads, head_dim], pos, seq [T] int32, cos, sin [positions, rot / 2] fp32
+    or None (no rotation)."""
+    T, heads, *rows = _append_rows(cache, q, k, v, q_out)
+    n_pos, rot = _angles(cos, sin)
+    status = (_lib or lib()).peqa_rope_append(cache, T, _index(pos, T), _index(seq, T), _floats(cos), _floats(sin), n_pos, rot, interleaved, heads,
+                                              *rows, _stream(stream))
     if status:
         raise PeqaError(status, "peqa_rope_append")
+
+
+def norm_rope_append(cache, q, k, v, pos, cos, sin, q_weight, k_weight, eps, q_out, place=None, seq=None, interleaved=False, stream=None):
+    """rope_append of heads that are normalised first, to places of their own: q_weight, k_weight [head_dim] fp32 or None (ones), place [T]
+    int32 or None (pos)."""
+    T, heads, *rows = _append_rows(cache, q, k, v, q_out)
+    n_pos, rot = _angles(cos, sin)
+    dim = cache.head_dim
+    status = (_lib or lib()).peqa_norm_rope_append(cache, T, _index(pos, T), _index(place, T), _index(seq, T), _floats(cos), _floats(sin), n_pos, rot,
+                                                   interleaved, _floats(q_weight, dim), _floats(k_weight, dim), eps, heads, *rows, _stream(stream))
+    if status:
+        raise PeqaError(status, "peqa_norm_rope_append")
+
+
+def _side(x, shape):
+    """(pointer, row stride) of queries, keys or their gradients of this shape."""
+    assert x.shape == shape, "tensors of the same shape"
+    T, heads, dim = shape
+    p, s = _rows(x, heads, dim)
+    return p, (s if T > 1 else heads * dim)    # (a single row may have any stride)
+
+
+def norm_rope(q, k, pos, cos, sin, q_weight, k_weight, eps, q_out, k_out, interleaved=False, stream=None):
+    """q, q_out [T, heads, head_dim], k, k_out [T, kv_heads, head_dim], pos [T] int32, cos, sin [positions, rot / 2] fp32 or None (no
+    rotation), q_weight, k_weight [head_dim] fp32 or None (ones)."""
+    T, heads, dim = q.shape
+    assert k.dim() == 3 and k.shape[0] == T and k.shape[2] == dim, "q [T, heads, head_dim] and k [T, kv_heads, head_dim]"
+    n_pos, rot = _angles(cos, sin)
+    status = (_lib or lib()).peqa_norm_rope(T, _index(pos, T), _floats(cos), _floats(sin), n_pos, rot, interleaved, _floats(q_weight, dim),
+                                            _floats(k_weight, dim), eps, dim, heads, k.shape[1], *_side(q, q.shape), *_side(k, k.shape),
+                                            *_side(q_out, q.shape), *_side(k_out, k.shape), _stream(stream))
+    if status:
+        raise PeqaError(status, "peqa_norm_rope")
+
+
+def norm_rope_bwd_workspace_bytes(T, heads, kv_heads, head_dim):
+    return int(lib().peqa_norm_rope_bwd_workspace_bytes(int(T), int(heads), int(kv_heads), int(head_dim)))
+
+
+def norm_rope_bwd(q, k, pos, cos, sin, q_weight, k_weight, eps, d_q_out, d_k_out, dq, dk, d_q_weight, d_k_weight, workspace, workspace_bytes_,
+                  interleaved=False, stream=None):
+    """The inputs of norm_rope, the gradients of its outputs, and those that it gives: dq as q, dk as k, d_q_weight, d_k_weight [head_dim] fp32
+    or None."""
+    T, heads, dim = q.shape
+    assert k.dim() == 3 and k.shape[0] == T and k.shape[2] == dim, "q [T, heads, head_dim] and k [T, kv_heads, head_dim]"
+    n_pos, rot = _angles(cos, sin)
+    status = (_lib or lib()).peqa_norm_rope_bwd(T, _index(pos, T), _floats(cos), _floats(sin), n_pos, rot, interleaved, _floats(q_weight, dim),
+                                                _floats(k_weight, dim), eps, dim, heads, k.shape[1], *_side(q, q.shape), *_side(k, k.shape),
+                                                *_side(d_q_out, q.shape), *_side(d_k_out, k.shape), *_side(dq, q.shape), *_side(dk, k.shape),
+                                                _floats(d_q_weight, dim), _floats(d_k_weight, dim), _room(workspace, workspace_bytes_),
+                                                workspace_bytes_, _stream(stream))
+    if status:
+        raise PeqaError(status, "peqa_norm_rope_bwd")
 
 
 def paged_attention_workspace_bytes(cache, heads, rows, max_len, window=0):
