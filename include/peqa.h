@@ -498,6 +498,49 @@ peqa_status peqa_paged_attention(const peqa_kv_cache *C, int32_t rows, int32_t h
                                  void *stream);
 
 /*
+ * peqa_paged_attention that also says what every position was given, for caches that are cut to what is looked at (peqa_cache_evict): for every
+ * row r, its sequence s, key head h and position j < lens[r]
+ *   weights_out[s, h, j] = weights[s, h, j] + sum over the sequence's rows and the heads i of h of exp(x_j - lse[r, i])
+ * (0 of positions outside the window and of pages that are not there; nothing else of weights_out is written).  out and lse are
+ * peqa_paged_attention's, bit for bit.
+ *   weights [n_seqs, kv_heads, max_len or more] fp32, sequences and heads strides apart (multiples of 4, at least max_len; 16-byte aligned), or
+ *   NULL: zeros;  weights_out the same, may be weights itself
+ *   workspace: peqa_paged_attention_weights_workspace_bytes(C, rows, heads, max_len, window): 4 bytes a row, head and position beside
+ *   the attention's own.
+ * Sums are fp32 in a fixed order: rows of one sequence after one another.
+ */
+size_t peqa_paged_attention_weights_workspace_bytes(const peqa_kv_cache *C, int32_t rows, int32_t heads, int32_t max_len,
+                                                    int32_t window);
+peqa_status peqa_paged_attention_weights(const peqa_kv_cache *C, int32_t rows, int32_t heads, const uint16_t *q, int64_t q_stride,
+                                         const int32_t *lens, const int32_t *seq, int32_t max_len, int32_t window, float scale,
+                                         uint16_t *out, int64_t out_stride, float *lse, const float *weights, float *weights_out,
+                                         int64_t weights_seq_stride, int64_t weights_head_stride, void *workspace,
+                                         size_t workspace_bytes, void *stream);
+
+/*
+ * Eviction.  Of each of n sequences (entry i: sequence seq[i], lens[i] positions long; seq NULL: sequence i) and each key head by itself: where
+ * there are more than `keep` positions, the first `sinks`, the last `recent` and, of those between, the keep - sinks - recent with the
+ * largest weights stay (equal ones: the lowest positions; NaN is less than everything), in order, at places 0 .. keep - 1: keys, values and
+ * weights.  Every head then has its own positions at a sequence's places, so that a token's place is no longer its position
+ * (peqa_norm_rope_append).  Shorter sequences keep everything.
+ *   to: the cache that keys and values go to, at the same sequences' places: of as many sequences, the same heads, head_dim, dtype and scales,
+ *   any page size; its pages of these places are none that C's sequences have.  NULL, or one with C's own pools and table: in place.  In
+ *   place a sequence's pages are its own: what another sequence shares with it would change.
+ *   lens [n] int32, cut to max_len (as in the attention);  1 <= keep,  0 <= sinks, recent,  sinks + recent <= keep (PEQA_ERR_PARAM)
+ *   weights, weights_out as in peqa_paged_attention_weights; places behind what stays, up to max_len, become 0
+ *   kept [n, kv_heads, keep] int32 out or NULL: the position that each place's was, -1 behind what stays
+ *   new_lens [n] int32 out or NULL: min(lens[i], keep); not lens itself (the layers of a model have the same lens)
+ * A sequence outside [0, n_seqs) has none; one that an earlier entry has is left out (kept -1, that entry's length).  What lies on a page that is
+ * not there arrives as zeros; nothing is stored to one.  Weights are compared as they are: every choice is exact.
+ *   workspace: peqa_cache_evict_workspace_bytes(C, n, max_len, keep).
+ */
+size_t peqa_cache_evict_workspace_bytes(const peqa_kv_cache *C, int32_t n, int32_t max_len, int32_t keep);
+peqa_status peqa_cache_evict(const peqa_kv_cache *C, const peqa_kv_cache *to, int32_t n, const int32_t *seq, const int32_t *lens,
+                             int32_t max_len, const float *weights, float *weights_out, int64_t weights_seq_stride,
+                             int64_t weights_head_stride, int32_t keep, int32_t sinks, int32_t recent, int32_t *kept,
+                             int32_t *new_lens, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
  * Log probabilities.  Of every row x = logits[t, 0 .. vocab-1] (bf16 or fp32, rows `stride` elements apart), in fp32:
  *   lse[t] = log sum_j exp(x_j);  logp[t] = x[targets[t]] - lse[t];  entropy[t] = -sum_j p_j log p_j,  p_j = exp(x_j - lse[t])
  *   top_ids[t, i], top_logp[t, i], i < top: the `top` largest x_j in falling order (equal ones: the lowest index first) and

@@ -1,4 +1,5 @@
-// Attention of single query tokens over the paged cache (peqa_paged_attention).
+// Attention of single query tokens over the paged cache (peqa_paged_attention), and with what every position was given of it
+// (peqa_paged_attention_weights).
 //
 // For a row and one of its key heads, with the heads that share it as columns:
 //   x[j][h] = scale <k_j, q_h>;   out[h] = sum_j e^(x[j][h]) v_j / sum_j e^(x[j][h])
@@ -56,7 +57,8 @@ struct AttendArgs {
     float *part;               // [slots, per_wg, head_dim] weighted sums, relative to the reference
     float *part_ml;            // [slots, per_wg, 2] reference (the maximum, or 14 below it; of powers of two) and sum
     ItemParts *parts;          // [rows * items of a row], or [shares]: of the item that ends in a share and began before it
-    long long q_stride, out_stride;
+    float *scores;             // [rows, heads, score_stride] of powers of two, for the positions' weights; or null
+    long long q_stride, out_stride, score_stride;
     float scale;               // times log2 e
     int rows, heads, group;    // heads per key head
     int max_len, window;
@@ -207,7 +209,7 @@ template <bool HI> __device__ __forceinline__ uint32_t fp8_f16(uint32_t v)
 // alone are as many, one with up to 512.
 constexpr int wgs_per_unit(int D, bool fp8) { return D > 128 && !fp8 ? 1 : 2; }
 
-template <int D, bool FP8, int HB, int WAVES, bool TWICE>
+template <int D, bool FP8, int HB, int WAVES, bool TWICE, bool SCORES>
 __global__ __launch_bounds__(64 * WAVES, wgs_per_unit(D, FP8)) void attend_kernel(AttendArgs a)
 {
     // Columns of the matrix instructions: eight heads twice, the upper ones with what rounding the weights leaves, so that they have 16 bits
@@ -431,6 +433,15 @@ __global__ __launch_bounds__(64 * WAVES, wgs_per_unit(D, FP8)) void attend_kerne
                 y[i] = x[i >> 2][i & 3] * scale;
                 if (!full) y[i] = seen(i) ? y[i] : -__builtin_inff();
                 top = fmaxf(top, y[i]);
+            }
+            if constexpr (SCORES) {
+                // (the columns of a head's remainders have the same scores)
+                const int of_group = cur.first_head + b * COLS + c;
+                if (c < COLS && of_group < a.group) {
+                    float *o = a.scores + ((size_t)cur.row * a.heads + cur.kv_head * a.group + of_group) * a.score_stride + t0 + 4 * g;
+                    if (t0 + 4 * g < cur.end) *reinterpret_cast<f32x4 *>(o) = f32x4{y[0], y[1], y[2], y[3]};
+                    if (t0 + 16 + 4 * g < cur.end) *reinterpret_cast<f32x4 *>(o + 16) = f32x4{y[4], y[5], y[6], y[7]};
+                }
             }
             top = across_groups(top, [](float x, float y) { return fmaxf(x, y); });
             // relative to 2^14 below the maximum, weights down to 2^-28 of the largest are normal fp16 numbers (scores past 2^24 have no bits for it)
@@ -722,22 +733,22 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a)
     if (a.lse && at == 0) a.lse[(size_t)item.row * a.heads + head] = any ? (top + __builtin_amdgcn_logf(total)) * LN2 : -__builtin_inff();
 }
 
-template <int D, bool FP8>
+template <int D, bool FP8, bool SCORES>
 hipError_t launch_attend(const AttendArgs &a, const AttendPlan &p, hipStream_t stream)
 {
-    auto kernel = p.waves == 1 ? attend_kernel<D, FP8, 1, 1, true> : attend_kernel<D, FP8, 1, 4, true>;
+    auto kernel = p.waves == 1 ? attend_kernel<D, FP8, 1, 1, true, SCORES> : attend_kernel<D, FP8, 1, 4, true, SCORES>;
     if constexpr (D <= 128)
-        if (p.waves == 8) kernel = attend_kernel<D, FP8, 1, 8, true>;
+        if (p.waves == 8) kernel = attend_kernel<D, FP8, 1, 8, true, SCORES>;
     if constexpr (FP8) {
         if (p.per_wg > 8) {
-            kernel = p.waves == 1 ? attend_kernel<D, true, 1, 1, false> : attend_kernel<D, true, 1, 4, false>;
+            kernel = p.waves == 1 ? attend_kernel<D, true, 1, 1, false, SCORES> : attend_kernel<D, true, 1, 4, false, SCORES>;
             if constexpr (D <= 128) {
-                if (p.waves == 8) kernel = attend_kernel<D, true, 1, 8, false>;
-                if (p.hb == 2) kernel = p.waves == 1 ? attend_kernel<D, true, 2, 1, false> : attend_kernel<D, true, 2, 4, false>;
+                if (p.waves == 8) kernel = attend_kernel<D, true, 1, 8, false, SCORES>;
+                if (p.hb == 2) kernel = p.waves == 1 ? attend_kernel<D, true, 2, 1, false, SCORES> : attend_kernel<D, true, 2, 4, false, SCORES>;
             }
         }
     } else {
-        if (p.hb == 2) kernel = p.waves == 1 ? attend_kernel<D, false, 2, 1, true> : attend_kernel<D, false, 2, 4, true>;
+        if (p.hb == 2) kernel = p.waves == 1 ? attend_kernel<D, false, 2, 1, true, SCORES> : attend_kernel<D, false, 2, 4, true, SCORES>;
     }
     trace_before(KID_ATTEND, stream);
     hipLaunchKernelGGL(kernel, dim3((unsigned)p.grid), dim3(64 * p.waves), 0, stream, a);
@@ -749,6 +760,81 @@ hipError_t launch_attend(const AttendArgs &a, const AttendPlan &p, hipStream_t s
                        dim3(256), 0, stream, a);
     trace_after(KID_ATTEND_JOIN, stream);
     return hipGetLastError();
+}
+
+template <bool SCORES> hipError_t launch_attend(const peqa_kv_cache *C, const AttendArgs &a, const AttendPlan &p, hipStream_t s)
+{
+    const bool fp8 = C->dtype == PEQA_CACHE_FP8;
+    switch (C->head_dim) {
+    case 64: return fp8 ? launch_attend<64, true, SCORES>(a, p, s) : launch_attend<64, false, SCORES>(a, p, s);
+    case 128: return fp8 ? launch_attend<128, true, SCORES>(a, p, s) : launch_attend<128, false, SCORES>(a, p, s);
+    default: return fp8 ? launch_attend<256, true, SCORES>(a, p, s) : launch_attend<256, false, SCORES>(a, p, s);
+    }
+}
+
+// What the positions were given: weights_out = weights + the sum over a row's heads of a key head, and over the rows of a sequence, of
+// 2^(score - log2 of the sum of powers).  A workgroup has 1024 positions of a key head, four a thread, of the first row with its sequence, and
+// adds the others' after one another, so that no sum depends on an order of workgroups.
+struct WeightArgs {
+    const int32_t *lens, *seq;
+    const float *scores, *lse, *weights;
+    float *weights_out;
+    long long score_stride, seq_stride, head_stride;
+    int rows, heads, kv_heads, group, n_seqs, max_len, window, chunks;
+};
+constexpr int WEIGHT_POSITIONS = 1024;
+
+__global__ __launch_bounds__(256) void attend_weights_kernel(WeightArgs a)
+{
+    unsigned b = blockIdx.x;
+    const int chunk = (int)(b % (unsigned)a.chunks);
+    b /= (unsigned)a.chunks;
+    const int row = (int)(b / (unsigned)a.kv_heads), h = (int)(b - (unsigned)row * (unsigned)a.kv_heads);
+    const int seq = a.seq ? a.seq[row] : row, lane = threadIdx.x & 63;
+    if (seq < 0 || seq >= a.n_seqs) return;
+    if (a.seq) {
+        for (int r0 = 0; r0 < row; r0 += 64) {
+            const int r = r0 + lane;
+            if (__ballot(r < row && a.seq[r < row ? r : 0] == seq) != 0) return;
+        }
+    }
+    const int pos = chunk * WEIGHT_POSITIONS + 4 * (int)threadIdx.x;
+    f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+    int longest = 0;
+    auto add_row = [&](int r) {
+        int len = a.lens[r];
+        len = len < a.max_len ? len : a.max_len;
+        if (len > longest) longest = len;
+        const int lo = a.window > 0 && len > a.window ? len - a.window : 0;
+        if (pos >= len || pos + 4 <= lo) return;
+        for (int i = 0; i < a.group; ++i) {
+            const size_t head = (size_t)r * a.heads + (size_t)h * a.group + i;
+            const float lse = a.lse[head] * LOG2E;
+            if (lse == -__builtin_inff()) continue;        // (a row without positions)
+            const f32x4 x = *reinterpret_cast<const f32x4 *>(a.scores + head * a.score_stride + pos);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) sum[k] += pos + k >= lo && pos + k < len ? __builtin_amdgcn_exp2f(x[k] - lse) : 0.f;
+        }
+    };
+    add_row(row);
+    if (a.seq) {
+        for (int r0 = row + 1; r0 < a.rows; r0 += 64) {
+            const int r = r0 + lane;
+            uint64_t same = __ballot(r < a.rows && a.seq[r < a.rows ? r : row] == seq);
+            while (same) {
+                add_row(r0 + __builtin_ctzll(same));
+                same &= same - 1;
+            }
+        }
+    }
+    if (pos >= longest) return;
+    const size_t at = (size_t)(seq * a.seq_stride + h * a.head_stride) + pos;
+    if (pos + 4 <= longest) {
+        if (a.weights) sum += *reinterpret_cast<const f32x4 *>(a.weights + at);
+        *reinterpret_cast<f32x4 *>(a.weights_out + at) = sum;
+    } else {
+        for (int k = 0; k < longest - pos; ++k) a.weights_out[at + k] = (a.weights ? a.weights[at + k] : 0.f) + sum[k];
+    }
 }
 
 }  // namespace
@@ -835,6 +921,57 @@ peqa_status check_attend(const peqa_kv_cache *C, int32_t rows, int32_t heads, in
     return PEQA_OK;
 }
 
+// The arguments that both calls have, checked and, where they are right, in `a`; part_bytes: what the parts of split items need.
+peqa_status attend_args(const peqa_kv_cache *C, int32_t rows, int32_t heads, const uint16_t *q, int64_t q_stride, const int32_t *lens,
+                        const int32_t *seq, int32_t max_len, int32_t window, float scale, uint16_t *out, int64_t out_stride, float *lse,
+                        void *workspace, size_t workspace_bytes, AttendArgs &a, AttendPlan &p)
+{
+    const peqa_status st = check_attend(C, rows, heads, max_len, window);
+    if (st != PEQA_OK) return st;
+    if (!q || !lens || !out) return PEQA_ERR_NULL;
+    if (!seq && rows > C->n_seqs) return PEQA_ERR_SHAPE;
+    const int64_t width = (int64_t)heads * C->head_dim;
+    if (q_stride < width || out_stride < width) return PEQA_ERR_SHAPE;
+    if (!aligned16(q) || !aligned16(out) || q_stride % 8 || out_stride % 8) return PEQA_ERR_ALIGN;
+    if ((reinterpret_cast<uintptr_t>(lens) | reinterpret_cast<uintptr_t>(seq) | reinterpret_cast<uintptr_t>(lse)) & 3) return PEQA_ERR_ALIGN;
+    p = attend_plan(C, rows, heads, max_len, window);
+    if (p.entries > 0) {
+        if (!workspace || workspace_bytes < p.part_bytes + p.ml_bytes + p.parts_bytes) return PEQA_ERR_WORKSPACE;
+        if (!aligned16(workspace)) return PEQA_ERR_ALIGN;
+    }
+    a.cache = cache_args(C);
+    a.q = q; a.lens = lens; a.seq = seq; a.out = out; a.lse = lse;
+    if (p.entries > 0) {
+        char *w = static_cast<char *>(workspace);
+        a.part = reinterpret_cast<float *>(w);
+        a.part_ml = reinterpret_cast<float *>(w + p.part_bytes);
+        a.parts = reinterpret_cast<ItemParts *>(w + p.part_bytes + p.ml_bytes);
+    }
+    a.q_stride = q_stride; a.out_stride = out_stride;
+    a.scale = scale * LOG2E;
+    a.rows = rows; a.heads = heads; a.group = heads / C->kv_heads;
+    a.max_len = max_len; a.window = window;
+    a.blocks = p.blocks; a.per_wg = p.per_wg;
+    a.splits = p.splits; a.chunk_units = p.chunk_units; a.shares = p.shares;
+    return PEQA_OK;
+}
+
+// Room of a call that says what the positions were given, behind the parts' own: scores, and what the rows' sums were.
+struct ScoreRoom {
+    size_t parts, scores, lse;
+    long long stride;
+};
+ScoreRoom score_room(const peqa_kv_cache *C, int rows, int heads, int max_len, int window)
+{
+    const AttendPlan p = attend_plan(C, rows, heads, max_len, window);
+    ScoreRoom r{};
+    r.stride = ((long long)max_len + 3) & ~3ll;
+    r.parts = p.part_bytes + p.ml_bytes + p.parts_bytes;
+    r.scores = round256((size_t)rows * (size_t)heads * (size_t)r.stride * sizeof(float));
+    r.lse = round256((size_t)rows * (size_t)heads * sizeof(float));
+    return r;
+}
+
 }  // namespace
 }  // namespace peqa
 
@@ -852,43 +989,57 @@ peqa_status peqa_paged_attention(const peqa_kv_cache *C, int32_t rows, int32_t h
                                  const int32_t *lens, const int32_t *seq, int32_t max_len, int32_t window, float scale, uint16_t *out,
                                  int64_t out_stride, float *lse, void *workspace, size_t workspace_bytes, void *stream)
 {
-    const peqa_status st = peqa::check_attend(C, rows, heads, max_len, window);
-    if (st != PEQA_OK) return st;
-    if (!q || !lens || !out) return PEQA_ERR_NULL;
-    if (!seq && rows > C->n_seqs) return PEQA_ERR_SHAPE;
-    const int64_t width = (int64_t)heads * C->head_dim;
-    if (q_stride < width || out_stride < width) return PEQA_ERR_SHAPE;
-    if (!aligned16(q) || !aligned16(out) || q_stride % 8 || out_stride % 8) return PEQA_ERR_ALIGN;
-    if ((reinterpret_cast<uintptr_t>(lens) | reinterpret_cast<uintptr_t>(seq) | reinterpret_cast<uintptr_t>(lse)) & 3) return PEQA_ERR_ALIGN;
-    const peqa::AttendPlan p = peqa::attend_plan(C, rows, heads, max_len, window);
-    if (p.entries > 0) {
-        if (!workspace || workspace_bytes < p.part_bytes + p.ml_bytes + p.parts_bytes) return PEQA_ERR_WORKSPACE;
-        if (!aligned16(workspace)) return PEQA_ERR_ALIGN;
-    }
     peqa::AttendArgs a{};
-    a.cache = peqa::cache_args(C);
-    a.q = q; a.lens = lens; a.seq = seq; a.out = out; a.lse = lse;
-    if (p.entries > 0) {
-        char *w = static_cast<char *>(workspace);
-        a.part = reinterpret_cast<float *>(w);
-        a.part_ml = reinterpret_cast<float *>(w + p.part_bytes);
-        a.parts = reinterpret_cast<peqa::ItemParts *>(w + p.part_bytes + p.ml_bytes);
-    }
-    a.q_stride = q_stride; a.out_stride = out_stride;
-    a.scale = scale * peqa::LOG2E;
-    a.rows = rows; a.heads = heads; a.group = heads / C->kv_heads;
-    a.max_len = max_len; a.window = window;
-    a.blocks = p.blocks; a.per_wg = p.per_wg;
-    a.splits = p.splits; a.chunk_units = p.chunk_units; a.shares = p.shares;
+    peqa::AttendPlan p{};
+    const peqa_status st = peqa::attend_args(C, rows, heads, q, q_stride, lens, seq, max_len, window, scale, out, out_stride, lse, workspace,
+                                             workspace_bytes, a, p);
+    if (st != PEQA_OK) return st;
+    return dev_status(peqa::launch_attend<false>(C, a, p, static_cast<hipStream_t>(stream)));
+}
+
+size_t peqa_paged_attention_weights_workspace_bytes(const peqa_kv_cache *C, int32_t rows, int32_t heads, int32_t max_len, int32_t window)
+{
+    if (peqa::check_attend(C, rows, heads, max_len, window) != PEQA_OK) return 0;
+    const peqa::ScoreRoom r = peqa::score_room(C, rows, heads, max_len, window);
+    return r.parts + r.scores + r.lse;
+}
+
+peqa_status peqa_paged_attention_weights(const peqa_kv_cache *C, int32_t rows, int32_t heads, const uint16_t *q, int64_t q_stride,
+                                         const int32_t *lens, const int32_t *seq, int32_t max_len, int32_t window, float scale, uint16_t *out,
+                                         int64_t out_stride, float *lse, const float *weights, float *weights_out,
+                                         int64_t weights_seq_stride, int64_t weights_head_stride, void *workspace, size_t workspace_bytes,
+                                         void *stream)
+{
+    peqa_status st = peqa::check_attend(C, rows, heads, max_len, window);
+    if (st != PEQA_OK) return st;
+    if (!weights_out) return PEQA_ERR_NULL;
+    if (weights_head_stride < max_len || weights_seq_stride < max_len) return PEQA_ERR_SHAPE;
+    if (!aligned16(weights) || !aligned16(weights_out) || weights_head_stride % 4 || weights_seq_stride % 4) return PEQA_ERR_ALIGN;
+    const peqa::ScoreRoom r = peqa::score_room(C, rows, heads, max_len, window);
+    const long long chunks = ((long long)max_len + peqa::WEIGHT_POSITIONS - 1) / peqa::WEIGHT_POSITIONS;
+    if (chunks * rows * C->kv_heads > (1 << 23)) return PEQA_ERR_SHAPE;       // workgroups of a launch
+    if (!workspace || workspace_bytes < r.parts + r.scores + r.lse) return PEQA_ERR_WORKSPACE;
+    if (!aligned16(workspace)) return PEQA_ERR_ALIGN;
+    char *w = static_cast<char *>(workspace);
+    if (!lse) lse = reinterpret_cast<float *>(w + r.parts + r.scores);
+    peqa::AttendArgs a{};
+    peqa::AttendPlan p{};
+    st = peqa::attend_args(C, rows, heads, q, q_stride, lens, seq, max_len, window, scale, out, out_stride, lse, workspace, workspace_bytes, a, p);
+    if (st != PEQA_OK) return st;
+    a.scores = reinterpret_cast<float *>(w + r.parts);
+    a.score_stride = r.stride;
     hipStream_t s = static_cast<hipStream_t>(stream);
-    const bool fp8 = C->dtype == PEQA_CACHE_FP8;
-    hipError_t e;
-    switch (C->head_dim) {
-    case 64: e = fp8 ? peqa::launch_attend<64, true>(a, p, s) : peqa::launch_attend<64, false>(a, p, s); break;
-    case 128: e = fp8 ? peqa::launch_attend<128, true>(a, p, s) : peqa::launch_attend<128, false>(a, p, s); break;
-    default: e = fp8 ? peqa::launch_attend<256, true>(a, p, s) : peqa::launch_attend<256, false>(a, p, s); break;
-    }
-    return dev_status(e);
+    const hipError_t e = peqa::launch_attend<true>(C, a, p, s);
+    if (e != hipSuccess || chunks == 0) return dev_status(e);
+    peqa::WeightArgs g{};
+    g.lens = lens; g.seq = seq; g.scores = a.scores; g.lse = lse; g.weights = weights; g.weights_out = weights_out;
+    g.score_stride = r.stride; g.seq_stride = weights_seq_stride; g.head_stride = weights_head_stride;
+    g.rows = rows; g.heads = heads; g.kv_heads = C->kv_heads; g.group = a.group; g.n_seqs = C->n_seqs;
+    g.max_len = max_len; g.window = window; g.chunks = (int)chunks;
+    peqa::trace_before(peqa::KID_ATTEND_WEIGHTS, s);
+    hipLaunchKernelGGL(peqa::attend_weights_kernel, dim3((unsigned)(chunks * rows * C->kv_heads)), dim3(256), 0, s, g);
+    peqa::trace_after(peqa::KID_ATTEND_WEIGHTS, s);
+    return dev_status(hipGetLastError());
 }
 
 }  // extern "C"

@@ -25,7 +25,8 @@ EXPORTS = ["peqa_check_layout", "peqa_packed_words", "peqa_num_scales", "peqa_wo
            "peqa_block_workspace_bytes", "peqa_block_fwd", "peqa_block_bwd", "peqa_trace_select",
            "peqa_check_cache", "peqa_rope_append", "peqa_paged_attention_workspace_bytes", "peqa_paged_attention",
            "peqa_token_logprobs_workspace_bytes", "peqa_token_logprobs", "peqa_token_logprobs_bwd",
-           "peqa_norm_rope_append", "peqa_norm_rope", "peqa_norm_rope_bwd_workspace_bytes", "peqa_norm_rope_bwd"]
+           "peqa_norm_rope_append", "peqa_norm_rope", "peqa_norm_rope_bwd_workspace_bytes", "peqa_norm_rope_bwd",
+           "peqa_paged_attention_weights_workspace_bytes", "peqa_paged_attention_weights", "peqa_cache_evict_workspace_bytes", "peqa_cache_evict"]
 
 
 class Layout(ctypes.Structure):
@@ -161,6 +162,14 @@ def lib():
         L.peqa_norm_rope_bwd_workspace_bytes.restype = sz
         L.peqa_norm_rope_bwd.argtypes = [*norms, *sides, *sides, *sides, vp, vp, vp, sz, vp]
         L.peqa_norm_rope_bwd.restype = i32
+        L.peqa_paged_attention_weights_workspace_bytes.argtypes = [CP, i32, i32, i32, i32]
+        L.peqa_paged_attention_weights_workspace_bytes.restype = sz
+        L.peqa_paged_attention_weights.argtypes = [CP, i32, i32, vp, i64, vp, vp, i32, i32, f32, vp, i64, vp, vp, vp, i64, i64, vp, sz, vp]
+        L.peqa_paged_attention_weights.restype = i32
+        L.peqa_cache_evict_workspace_bytes.argtypes = [CP, i32, i32, i32]
+        L.peqa_cache_evict_workspace_bytes.restype = sz
+        L.peqa_cache_evict.argtypes = [CP, CP, i32, vp, vp, i32, vp, vp, i64, i64, i32, i32, i32, vp, vp, vp, sz, vp]
+        L.peqa_cache_evict.restype = i32
         _lib = L
     return _lib
 
@@ -600,6 +609,62 @@ def paged_attention(cache, q, lens, max_len, scale, out, workspace, workspace_by
                                                   _floats(lse), _room(workspace, workspace_bytes_), workspace_bytes_, _stream(stream))
     if status:
         raise PeqaError(status, "peqa_paged_attention")
+
+
+def _weights(cache, weights, weights_out, most):
+    """Pointers and strides of a cache's weights [sequences, kv_heads, most or more] fp32 before and after a call."""
+    n, heads, room = shape = weights_out.shape
+    assert n == cache.n_seqs and heads == cache.kv_heads and room >= most, "weights [sequences, kv_heads, max_len or more]"
+    s0, s1, s2 = strides = weights_out.stride()
+    assert s2 == 1 and _kind[weights_out.dtype] == "float32", "weights of fp32 with contiguous positions"
+    wp = None
+    if weights is not None:
+        assert weights.shape == shape and weights.stride() == strides and _kind[weights.dtype] == "float32", "weights of the same shape and strides"
+        wp = weights.data_ptr()
+    s1 = s1 if heads > 1 else -(-room // 4) * 4              # (a single one may have any stride)
+    assert s1 >= room and (n == 1 or s0 >= room), "weights whose rows do not overlap"
+    return wp, weights_out.data_ptr(), s0 if n > 1 else heads * s1, s1
+
+
+def paged_attention_weights_workspace_bytes(cache, heads, rows, max_len, window=0):
+    return int(lib().peqa_paged_attention_weights_workspace_bytes(ctypes.byref(cache), int(rows), int(heads), int(max_len), int(window)))
+
+
+def paged_attention_weights(cache, q, lens, max_len, scale, out, weights, weights_out, workspace, workspace_bytes_, lse=None, seq=None, window=0,
+                            stream=None):
+    """paged_attention, and weights_out = weights + what every position was given: [sequences, kv_heads, max_len or more] fp32, weights None for
+    zeros or weights_out itself."""
+    rows, heads, dim = shape = q.shape
+    assert out.shape == shape and dim == cache.head_dim
+    assert lse is None or lse.shape == (rows, heads)
+    qp, qs = _rows(q, heads, dim)
+    op, os_ = _rows(out, heads, dim)
+    if rows == 1:                              # (a single row may have any stride)
+        qs = os_ = heads * dim
+    status = (_lib or lib()).peqa_paged_attention_weights(cache, rows, heads, qp, qs, _index(lens, rows), _index(seq, rows), max_len, window, scale, op,
+                                                          os_, _floats(lse), *_weights(cache, weights, weights_out, max_len),
+                                                          _room(workspace, workspace_bytes_), workspace_bytes_, _stream(stream))
+    if status:
+        raise PeqaError(status, "peqa_paged_attention_weights")
+
+
+def cache_evict_workspace_bytes(cache, n, max_len, keep):
+    return int(lib().peqa_cache_evict_workspace_bytes(ctypes.byref(cache), int(n), int(max_len), int(keep)))
+
+
+def cache_evict(cache, lens, max_len, weights, weights_out, keep, sinks, recent, kept, new_lens, workspace, workspace_bytes_, seq=None, to=None,
+                stream=None):
+    """lens, seq [n] int32, weights, weights_out as in paged_attention_weights (the same one will do), kept [n, kv_heads, keep] and new_lens [n]
+    int32 or None, to: the cache that the positions go to, or None (in place)."""
+    n = lens.numel()
+    assert kept is None or kept.shape == (n, cache.kv_heads, keep), "kept [n, kv_heads, keep]"
+    assert weights is not None and new_lens is not lens
+    assert to is None or (to.k_scale is None) == (cache.k_scale is None) and (to.v_scale is None) == (cache.v_scale is None), "caches of the same scales"
+    status = (_lib or lib()).peqa_cache_evict(cache, to, n, _index(seq, n), _index(lens), max_len, *_weights(cache, weights, weights_out, max_len), keep,
+                                              sinks, recent, _index(kept), _index(new_lens, n), _room(workspace, workspace_bytes_),
+                                              workspace_bytes_, _stream(stream))
+    if status:
+        raise PeqaError(status, "peqa_cache_evict")
 
 
 def _logits(x):
