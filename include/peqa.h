@@ -498,6 +498,25 @@ peqa_status peqa_paged_attention(const peqa_kv_cache *C, int32_t rows, int32_t h
                                  void *stream);
 
 /*
+ * peqa_paged_attention for rows whose sequences begin with the same positions (samples of one prompt, questions about one document, a system
+ * prompt): the first `shared` positions of every row are those of sequence `prefix`, which are read once for all rows; those behind
+ * them are the row's own sequence's.  With K_r = positions [0, shared) of sequence `prefix`, then [shared, lens[r]) of sequence seq[r]
+ * (NULL: r), out and lse are those of peqa_paged_attention over K_r; a row with lens[r] < shared sees the first lens[r] of the
+ * shared positions.  The table's entries of a row's blocks before position `shared` are not used: a page in which the
+ * shared positions end is there twice, in `prefix` and, with the row's own positions behind, in the row's.
+ *   max_len: the host's bound of lens, shared positions included;  shared, max_len at most n_blocks * page_size (PEQA_ERR_SHAPE)
+ *   prefix: 0 .. n_seqs - 1;  the other arguments as in peqa_paged_attention
+ *   workspace: peqa_shared_attention_workspace_bytes(C, rows, heads, max_len, shared).
+ * Products and sums are fp32; weights are rounded to two bf16 parts (16 bits) against bf16 values, to fp16 (11 bits; of weights under 2^-28
+ * of the row's largest to 2^-39 of it) against 8-bit ones.  The same call gives the same bits.
+ */
+size_t peqa_shared_attention_workspace_bytes(const peqa_kv_cache *C, int32_t rows, int32_t heads, int32_t max_len, int32_t shared);
+peqa_status peqa_shared_attention(const peqa_kv_cache *C, int32_t rows, int32_t heads, const uint16_t *q, int64_t q_stride,
+                                  const int32_t *lens, const int32_t *seq, int32_t max_len, int32_t prefix, int32_t shared,
+                                  float scale, uint16_t *out, int64_t out_stride, float *lse, void *workspace,
+                                  size_t workspace_bytes, void *stream);
+
+/*
  * peqa_paged_attention that also says what every position was given, for caches that are cut to what is looked at (peqa_cache_evict): for every
  * row r, its sequence s, key head h and position j < lens[r]
  *   weights_out[s, h, j] = weights[s, h, j] + sum over the sequence's rows and the heads i of h of exp(x_j - lse[r, i])

@@ -16,6 +16,7 @@
 // loads (length, page, tile).  Measured, the kernel alone:  one row of 131072 positions, 8 key heads of 128, 8 heads to each  93.5 us,
 // 5.7 TB/s;  64 rows of up to 8192 on 8 bits, as many heads  107 us, 5.2 TB/s;  16 rows of up to 2048, 32 key heads  53.5 us, 4.8 TB/s;
 // one row of 333, 32 key heads  9 us.
+#include "peqa_attend.h"
 #include "peqa_cache.h"
 #include "peqa_host.h"
 
@@ -33,14 +34,9 @@ AttendPlan attend_plan(const peqa_kv_cache *C, int rows, int heads, int max_len,
 
 namespace {
 
-typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
-typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
-
 constexpr int TILE = 32;                 // positions per step of a wave
 constexpr int UNIT = 64;                 // positions that shares are counted in
 constexpr int SCAN_ROWS = 1024;          // rows of a launch of equal shares at most: every workgroup adds up their lengths
-constexpr float LOWEST = -3.0e38f;       // finite stand-in for the maximum of nothing: e^(-inf - LOWEST) is 0, not NaN
-constexpr float LN2 = 0.693147180559945309f, LOG2E = 1.44269504088896341f;
 
 // An item in several workgroups, for the join (n < 2: none): the slots of its n parts are first, next, next + step, ...
 struct ItemParts {
@@ -172,37 +168,10 @@ struct Piece {
     bool first, last, alone;                               // of its segment; alone: the segment is the whole item
 };
 
-__device__ __forceinline__ f32x4 mfma_bf16(u32x4 x, u32x4 y, f32x4 c)
-{
-    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x), __builtin_bit_cast(bf16x8, y), c, 0, 0, 0);
-}
-__device__ __forceinline__ f32x4 mfma_f16(u32x4 x, u32x4 y, f32x4 c)
-{
-    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, x), __builtin_bit_cast(f16x8, y), c, 0, 0, 0);
-}
-
-// f over the four lanes of a wave with the same lane % 16, in all of them: rows of 16 lanes change places, then halves.
-template <typename F> __device__ __forceinline__ float across_groups(float v, F f)
-{
-    auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-    v = f(__uint_as_float(a[0]), __uint_as_float(a[1]));
-    auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-    return f(__uint_as_float(b[0]), __uint_as_float(b[1]));
-}
 // The sum of lanes c and c + 8 of every 16, in both.
 __device__ __forceinline__ float add_halves(float v)
 {
     return v + __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(v), 0x128 /* row_ror:8 */, 0xF, 0xF, true));
-}
-
-// Four 8-bit floats as bf16, or two as fp16: exact.
-template <bool HI> __device__ __forceinline__ uint32_t fp8_bf16(uint32_t v)
-{
-    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(v, 1.f, HI));
-}
-template <bool HI> __device__ __forceinline__ uint32_t fp8_f16(uint32_t v)
-{
-    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(v, 1.f, HI));
 }
 
 // Workgroups of a unit: two, of one wave per SIMD each, with up to 256 registers a lane; of the widest heads, whose two tiles

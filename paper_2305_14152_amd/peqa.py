@@ -26,7 +26,8 @@ EXPORTS = ["peqa_check_layout", "peqa_packed_words", "peqa_num_scales", "peqa_wo
            "peqa_check_cache", "peqa_rope_append", "peqa_paged_attention_workspace_bytes", "peqa_paged_attention",
            "peqa_token_logprobs_workspace_bytes", "peqa_token_logprobs", "peqa_token_logprobs_bwd",
            "peqa_norm_rope_append", "peqa_norm_rope", "peqa_norm_rope_bwd_workspace_bytes", "peqa_norm_rope_bwd",
-           "peqa_paged_attention_weights_workspace_bytes", "peqa_paged_attention_weights", "peqa_cache_evict_workspace_bytes", "peqa_cache_evict"]
+           "peqa_paged_attention_weights_workspace_bytes", "peqa_paged_attention_weights", "peqa_cache_evict_workspace_bytes", "peqa_cache_evict",
+           "peqa_shared_attention_workspace_bytes", "peqa_shared_attention"]
 
 
 class Layout(ctypes.Structure):
@@ -170,6 +171,10 @@ def lib():
         L.peqa_cache_evict_workspace_bytes.restype = sz
         L.peqa_cache_evict.argtypes = [CP, CP, i32, vp, vp, i32, vp, vp, i64, i64, i32, i32, i32, vp, vp, vp, sz, vp]
         L.peqa_cache_evict.restype = i32
+        L.peqa_shared_attention_workspace_bytes.argtypes = [CP, i32, i32, i32, i32]
+        L.peqa_shared_attention_workspace_bytes.restype = sz
+        L.peqa_shared_attention.argtypes = [CP, i32, i32, vp, i64, vp, vp, i32, i32, i32, f32, vp, i64, vp, vp, sz, vp]
+        L.peqa_shared_attention.restype = i32
         _lib = L
     return _lib
 
@@ -609,6 +614,26 @@ def paged_attention(cache, q, lens, max_len, scale, out, workspace, workspace_by
                                                   _floats(lse), _room(workspace, workspace_bytes_), workspace_bytes_, _stream(stream))
     if status:
         raise PeqaError(status, "peqa_paged_attention")
+
+
+def shared_attention_workspace_bytes(cache, heads, rows, max_len, shared):
+    return int(lib().peqa_shared_attention_workspace_bytes(ctypes.byref(cache), int(rows), int(heads), int(max_len), int(shared)))
+
+
+def shared_attention(cache, q, lens, max_len, prefix, shared, scale, out, workspace, workspace_bytes_, lse=None, seq=None, stream=None):
+    """paged_attention of rows whose first `shared` positions are those of sequence `prefix`: q, out [rows, heads, head_dim], lens, seq [rows]
+    int32, lse [rows, heads] fp32."""
+    rows, heads, dim = shape = q.shape
+    assert out.shape == shape and dim == cache.head_dim
+    assert lse is None or lse.shape == (rows, heads)
+    qp, qs = _rows(q, heads, dim)
+    op, os_ = _rows(out, heads, dim)
+    if rows == 1:                              # (a single row may have any stride)
+        qs = os_ = heads * dim
+    status = (_lib or lib()).peqa_shared_attention(cache, rows, heads, qp, qs, _index(lens, rows), _index(seq, rows), max_len, prefix, shared, scale, op,
+                                                   os_, _floats(lse), _room(workspace, workspace_bytes_), workspace_bytes_, _stream(stream))
+    if status:
+        raise PeqaError(status, "peqa_shared_attention")
 
 
 def _weights(cache, weights, weights_out, most):
