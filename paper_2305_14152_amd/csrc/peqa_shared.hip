@@ -16,7 +16,8 @@ namespace peqa {
 
 namespace {
 
-constexpr int TILE = 32, WAVES = 4, STEP = TILE * WAVES;   // positions of a wave's step, and of a workgroup's
+constexpr int TILE = 32;       // positions of a wave's step
+constexpr int UNIT = 128;      // that chunks are counted in
 
 struct SharedArgs {
     CacheArgs cache;
@@ -62,7 +63,7 @@ __device__ __forceinline__ OwnChunks own_chunks(const SharedArgs &a, const RowIn
     OwnChunks o;
     o.from = r.lo & ~(TILE - 1);
     const int span = r.len > r.lo ? r.len - o.from : 0;
-    o.length = ((span + a.own_splits - 1) / a.own_splits + STEP - 1) & ~(STEP - 1);
+    o.length = ((span + a.own_splits - 1) / a.own_splits + UNIT - 1) & ~(UNIT - 1);
     o.length = o.length > a.own_chunk ? o.length : a.own_chunk;
     o.n = (span + o.length - 1) / o.length;
     return o;
@@ -76,22 +77,214 @@ struct Item {
     long long slot;            // of the first column
 };
 
-// The pages of a tile of 32 positions: four at most, neighbouring entries of the table (the last ones of an item again past its end).
+typedef const __attribute__((address_space(4))) int32_t *scalar_ints;
+
+// The pages of a tile of 32 positions: four at most, neighbouring entries of the table.  They are read (scalar loads) a step before they
+// are used, the last one of the positions up to `last` again past its end.
+struct Entries {
+    int page[4];
+};
+__device__ __forceinline__ Entries read_entries(const CacheArgs &C, const int32_t *row, int last, int t0)
+{
+    scalar_ints table = (scalar_ints)(uintptr_t)row;
+    const int block = t0 >> C.page_shift, last_block = last >> C.page_shift, next = C.page_shift < 5 ? 1 : 0;
+    Entries e;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) e.page[i] = table[block + i * next < last_block ? block + i * next : last_block];
+    return e;
+}
 struct Pages {
     long long at[4];           // in bytes
     uint32_t there;            // bit i: the page is there
 };
+__device__ __forceinline__ Pages pages_of(const CacheArgs &C, const Entries &e, int el)
+{
+    Pages p;
+    p.there = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const bool ok = (unsigned)e.page[i] < (unsigned)C.n_pages;
+        p.at[i] = (ok ? e.page[i] : 0) * C.page_stride * el;
+        p.there |= (ok ? 1u : 0u) << i;
+    }
+    return p;
+}
+__device__ __forceinline__ long long page_of(const Pages &p, int which)
+{
+    const long long low = which & 1 ? p.at[1] : p.at[0], high = which & 1 ? p.at[3] : p.at[2];
+    return which & 2 ? high : low;
+}
+// Where a position of a tile is: the last one's place past the end.
+__device__ __forceinline__ long long place_of(const CacheArgs &C, const Pages &p, int t0, int pos, int last, int slot_bytes)
+{
+    const int at = pos < last ? pos : last;
+    return page_of(p, (at >> C.page_shift) - (t0 >> C.page_shift)) + (uint32_t)((at & C.page_mask) * slot_bytes);
+}
+// Whether a position of the tile at t0 is in [lo, end) and its page there.
+__device__ __forceinline__ bool seen_at(const CacheArgs &C, uint32_t there, int t0, int pos, int lo, int end)
+{
+    return pos >= lo && pos < end && (there >> ((pos >> C.page_shift) - (t0 >> C.page_shift) & 3) & 1u);
+}
+// What the scores' sums begin with: 0, or of positions that are not seen -inf.  (Score i of a lane is of position t0 + 16 (i / 4) + 4 g + i % 4.)
+struct Start {
+    f32x4 x[2];
+};
+__device__ __forceinline__ Start start_of(const CacheArgs &C, uint32_t there, int t0, int g, int lo, int end)
+{
+    Start s;
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        s.x[i >> 2][i & 3] = seen_at(C, there, t0, t0 + 16 * (i >> 2) + 4 * g + (i & 3), lo, end) ? 0.f : -__builtin_inff();
+    return s;
+}
 
-typedef const __attribute__((address_space(4))) int32_t *scalar_ints;
+// Values of eight positions, 2 VR or 4 VR elements each (bf16; 8 bits), turned: operand e has element e of all eight, 8-bit ones as fp16 (exact).
+template <bool FP8, int VR> __device__ __forceinline__ void turn_values(const uint32_t (&v)[8][VR], u32x4 *vt)
+{
+#pragma unroll
+    for (int r = 0; r < VR; ++r)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if constexpr (FP8) {
+                // bytes of two positions next to each other, then to fp16
+                const uint32_t lo = __builtin_amdgcn_perm(v[2 * i + 1][r], v[2 * i][r], 0x05010400u);
+                const uint32_t hi = __builtin_amdgcn_perm(v[2 * i + 1][r], v[2 * i][r], 0x07030602u);
+                vt[4 * r][i] = fp8_f16<false>(lo);
+                vt[4 * r + 1][i] = fp8_f16<true>(lo);
+                vt[4 * r + 2][i] = fp8_f16<false>(hi);
+                vt[4 * r + 3][i] = fp8_f16<true>(hi);
+            } else {
+                vt[2 * r][i] = __builtin_amdgcn_perm(v[2 * i + 1][r], v[2 * i][r], 0x05040100u);
+                vt[2 * r + 1][i] = __builtin_amdgcn_perm(v[2 * i + 1][r], v[2 * i][r], 0x07060302u);
+            }
+        }
+}
+
+// Weights of 8 positions and a column as operands: bf16 in two parts, fp16 in one.
+template <bool FP8> struct Weights {
+    u32x4 near, rest;
+};
+// The reference of a column follows the maximum of its scores only when that is 2^GROWTH past it, so that the sums are seldom carried over; weights are
+// then up to that, and as fp16 (relative to 2^6 below the maximum that was met) up to 2^14.  x: a lane's eight scores, to be multiplied with
+// scale > 0; m, l and acc: the reference, the lane's sum of weights, and what is carried over.
+template <bool FP8, int ACC> __device__ __forceinline__ void follow(const f32x4 (&x)[2], float scale, float &m, float &l, f32x4 (&acc)[ACC])
+{
+    constexpr float GROWTH = 8.f;
+    float top = x[0][0];
+#pragma unroll
+    for (int i = 1; i < 8; ++i) top = fmaxf(top, x[i >> 2][i & 3]);
+    top *= scale;
+    if (__ballot(top > m + (FP8 ? GROWTH + 6.f : GROWTH)) != 0) {
+        top = across_groups(top, [](float x, float y) { return fmaxf(x, y); });
+        if constexpr (FP8) top -= 6.f;
+        const float mn = fmaxf(m, top), fall = __builtin_amdgcn_exp2f(m - mn);
+        m = mn;
+        l *= fall;
+#pragma unroll
+        for (int e = 0; e < ACC; ++e) acc[e] *= fall;
+    }
+}
+// The weights of eight scores; their sum is added to l.
+struct Eights {
+    float p[8];
+};
+__device__ __forceinline__ Eights powers(const f32x4 (&x)[2], float scale, float m, float &l)
+{
+    Eights e;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        e.p[i] = __builtin_amdgcn_exp2f(fmaf(x[i >> 2][i & 3], scale, -m));
+        l += e.p[i];
+    }
+    return e;
+}
+// As operands.  Two bf16 parts have 16 bits: the first is cut, so that the second is not negative, and not 0: an infinite value then gives
+// infinities of one sign.
+template <bool FP8> __device__ __forceinline__ Weights<FP8> operands(const Eights &e)
+{
+    const auto &p = e.p;
+    Weights<FP8> w;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if constexpr (FP8) {
+            const f16x2 h = {(_Float16)p[2 * i], (_Float16)p[2 * i + 1]};
+            w.near[i] = __builtin_bit_cast(uint32_t, h);
+        } else {
+            const uint32_t p0 = __float_as_uint(p[2 * i]), p1 = __float_as_uint(p[2 * i + 1]);
+            w.near[i] = __builtin_amdgcn_perm(p1, p0, 0x07060302u);
+            w.rest[i] = pack_bf16x2(fmaxf(p[2 * i] - __uint_as_float(p0 & 0xFFFF0000u), 1.2e-38f),
+                                    fmaxf(p[2 * i + 1] - __uint_as_float(p1 & 0xFFFF0000u), 1.2e-38f));
+        }
+    }
+    return w;
+}
+// acc[e] += values' operand e x weights, for COUNT operands: no two neighbouring instructions add to the same sums.
+template <bool FP8, int COUNT> __device__ __forceinline__ void add_weighted(const u32x4 *vt, const Weights<FP8> &w, f32x4 *acc)
+{
+#pragma unroll
+    for (int e = 0; e < COUNT; ++e) acc[e] = FP8 ? mfma_f16(vt[e], w.near, acc[e]) : mfma_bf16(vt[e], w.near, acc[e]);
+    if constexpr (!FP8) {
+#pragma unroll
+        for (int e = 0; e < COUNT; ++e) acc[e] = mfma_bf16(vt[e], w.rest, acc[e]);
+    }
+}
+
+// What the products of a key head's queries and keys are multiplied with, made positive: a negative one turns the queries' signs, so that the largest
+// score is that of the largest product, and for 0 a number stands that no product makes anything of (and -inf stays).
+template <bool FP8> __device__ __forceinline__ float scale_of(const SharedArgs &a, int kv_head, uint32_t &turn)
+{
+    const float scale = a.scale * (FP8 && a.cache.k_scale ? a.cache.k_scale[kv_head] : 1.f);
+    turn = scale < 0.f ? 0x80008000u : 0u;
+    return fmaxf(fabsf(scale), 1e-36f);
+}
+
+// A piece of the query of a column: 16 bytes of step s of the scores' product, whose elements the keys' pieces decide.
+template <int D, bool FP8> __device__ __forceinline__ u32x4 query_piece(const SharedArgs &a, const Item &it, int column, int s, int g, uint32_t turn)
+{
+    const int i = it.first + (column < it.n ? column : 0);
+    const int row = i / a.group, head = it.kv_head * a.group + (i - row * a.group);
+    const int at = FP8 ? 64 * (s >> 1) + 16 * g + 8 * (s & 1) : 32 * s + 8 * g;
+    u32x4 x = *reinterpret_cast<const u32x4 *>(a.q + row * a.q_stride + (long long)head * D + at);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) x[k] ^= turn;
+    return x;
+}
+// Eight elements of a key for step j, of the pieces that were loaded.
+template <bool FP8, int KB> __device__ __forceinline__ u32x4 key_piece(const u32x4 (&k)[KB], int j)
+{
+    if constexpr (FP8) {
+        const uint32_t lo = k[j >> 1][2 * (j & 1)], hi = k[j >> 1][2 * (j & 1) + 1];
+        return u32x4{fp8_bf16<false>(lo), fp8_bf16<true>(lo), fp8_bf16<false>(hi), fp8_bf16<true>(hi)};
+    } else {
+        return k[j];
+    }
+}
+// VR registers from memory.
+template <int VR> __device__ __forceinline__ void load_value(const uint8_t *src, uint32_t (&v)[VR])
+{
+    if constexpr (VR == 4) {
+        const u32x4 x = *reinterpret_cast<const u32x4 *>(src);
+#pragma unroll
+        for (int r = 0; r < VR; ++r) v[r] = x[r];
+    } else if constexpr (VR == 2) {
+        const u32x2 x = *reinterpret_cast<const u32x2 *>(src);
+#pragma unroll
+        for (int r = 0; r < VR; ++r) v[r] = x[r];
+    } else {
+        v[0] = *reinterpret_cast<const uint32_t *>(src);
+    }
+}
 
 template <int D> struct Shape {
     static constexpr int SEG = D > 128 ? D / 128 : 1, DS = D / SEG;
 };
 
-template <int D, bool FP8, int HB>
+// All columns in every wave, which take the tiles in turn.
+template <int D, bool FP8, int HB, int WAVES>
 __device__ __forceinline__ void attend_item(const SharedArgs &a, const Item &it, u32x4 *lds_q, float (*wave_m)[16], float (*wave_l)[16],
                                             float (*joined)[16][Shape<D>::DS + 4])
 {
+    constexpr int STEP = TILE * WAVES;                // positions of a workgroup's step
     constexpr int QK = D / 32;                        // steps of the scores' product
     constexpr int SEG = Shape<D>::SEG, DS = Shape<D>::DS;
     constexpr int W = D / 16 / SEG;                   // neighbouring elements of a segment that a lane has: 4 or 8
@@ -105,101 +298,50 @@ __device__ __forceinline__ void attend_item(const SharedArgs &a, const Item &it,
     const int c = lane & 15, g = lane >> 4;
     const int slot_bytes = (int)C.slot_stride * EL;
 
-    // a negative scale turns the queries' sign, so that the largest score is that of the largest product
-    float scale = a.scale * (FP8 && C.k_scale ? C.k_scale[it.kv_head] : 1.f);
-    const uint32_t turn = scale < 0.f ? 0x80008000u : 0u;
-    scale = fabsf(scale);
-    auto query = [&](int b, int s) __attribute__((always_inline)) {
-        int i = 16 * b + c;
-        i = it.first + (i < it.n ? i : 0);
-        const int row = i / a.group, head = it.kv_head * a.group + (i - row * a.group);
-        // the keys' pieces decide which elements a step has
-        const int at = FP8 ? 64 * (s >> 1) + 16 * g + 8 * (s & 1) : 32 * s + 8 * g;
-        u32x4 x = *reinterpret_cast<const u32x4 *>(a.q + row * a.q_stride + (long long)head * D + at);
-#pragma unroll
-        for (int k = 0; k < 4; ++k) x[k] ^= turn;
-        return x;
-    };
+    uint32_t turn;
+    const float scale = scale_of<FP8>(a, it.kv_head, turn);
     u32x4 q[QUERIES_IN_LDS ? 1 : HB][QUERIES_IN_LDS ? 1 : QK];
     if constexpr (QUERIES_IN_LDS) {
 #pragma unroll
         for (int b = 0; b < HB / WAVES; ++b)
 #pragma unroll
-            for (int s = 0; s < QK; ++s) lds_q[((b * WAVES + wave) * QK + s) * 64 + lane] = query(b * WAVES + wave, s);
+            for (int s = 0; s < QK; ++s)
+                lds_q[((b * WAVES + wave) * QK + s) * 64 + lane] = query_piece<D, FP8>(a, it, 16 * (b * WAVES + wave) + c, s, g, turn);
         __syncthreads();
     } else {
 #pragma unroll
         for (int b = 0; b < HB; ++b)
 #pragma unroll
-            for (int s = 0; s < QK; ++s) q[b][s] = query(b, s);
+            for (int s = 0; s < QK; ++s) q[b][s] = query_piece<D, FP8>(a, it, 16 * b + c, s, g, turn);
     }
 
-    const int last = it.end - 1, last_block = last >> C.page_shift;
-    scalar_ints table = (scalar_ints)(uintptr_t)it.table;
-    auto read_pages = [&](int t0) __attribute__((always_inline)) {
-        Pages p;
-        p.there = 0;
-        const int block = t0 >> C.page_shift;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            int entry;
-            if (i > 0 && C.page_shift >= 5) {
-                p.at[i] = p.at[0];
-                p.there |= (p.there & 1u) << i;
-                continue;
-            }
-            entry = table[block + i < last_block ? block + i : last_block];
-            const bool ok = entry >= 0 && entry < C.n_pages;
-            p.at[i] = ok ? entry * C.page_stride * EL : 0ll;
-            p.there |= ok ? 1u << i : 0u;
-        }
-        return p;
-    };
-    auto page_of = [&](const Pages &p, int which) __attribute__((always_inline)) {
-        long long at = which & 1 ? p.at[1] : p.at[0];
-        const long long high = which & 1 ? p.at[3] : p.at[2];
-        return which & 2 ? high : at;
-    };
+    const int last = it.end - 1;
     // A tile in registers: pieces of the keys at t0 + c and t0 + 16 + c, of the values at t0 + 4 g .. + 3 and t0 + 16 + 4 g .. + 3 (a page
     // has whole quads of positions).  Positions past the end are read from the last one's place, quads from the last one's.
     struct Tile {
         u32x4 k[2][KB];
-        uint32_t v[8][SEG][VR];
+        uint32_t v[SEG][8][VR];
         uint32_t there;
     };
     const uint8_t *kbase = static_cast<const uint8_t *>(C.k) + it.kv_head * C.head_stride * EL + 16 * g;
     const uint8_t *vbase = static_cast<const uint8_t *>(C.v) + it.kv_head * C.head_stride * EL + W * EL * c;
-    auto load = [&](Tile &t, const Pages &p, int t0) __attribute__((always_inline)) {
-        const int block = t0 >> C.page_shift;
+    auto entries_at = [&](int t0) __attribute__((always_inline)) { return read_entries(C, it.table, last, t0); };
+    auto load = [&](Tile &t, const Entries &e, int t0) __attribute__((always_inline)) {
+        const Pages p = pages_of(C, e, EL);
         t.there = p.there;
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
-            const int pos = t0 + 16 * s + c, at = pos < last ? pos : last;
-            const uint8_t *src = kbase + page_of(p, (at >> C.page_shift) - block) + (uint32_t)((at & C.page_mask) * slot_bytes);
+            const uint8_t *src = kbase + place_of(C, p, t0, t0 + 16 * s + c, last, slot_bytes);
 #pragma unroll
             for (int j = 0; j < KB; ++j) t.k[s][j] = *reinterpret_cast<const u32x4 *>(src + 64 * j);
         }
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
-            const int pos = t0 + 16 * s + 4 * g, quad = last & ~3, at = pos < quad ? pos : quad;
-            const uint8_t *src = vbase + page_of(p, (at >> C.page_shift) - block) + (uint32_t)((at & C.page_mask) * slot_bytes);
+            const uint8_t *src = vbase + place_of(C, p, t0, t0 + 16 * s + 4 * g, last & ~3, slot_bytes);
 #pragma unroll
             for (int i = 0; i < 4; ++i, src += slot_bytes)
 #pragma unroll
-                for (int e = 0; e < SEG; ++e) {
-                    uint32_t *v = t.v[4 * s + i][e];
-                    if constexpr (VR == 4) {
-                        const u32x4 x = *reinterpret_cast<const u32x4 *>(src + 128 * EL * e);
-#pragma unroll
-                        for (int r = 0; r < VR; ++r) v[r] = x[r];
-                    } else if constexpr (VR == 2) {
-                        const u32x2 x = *reinterpret_cast<const u32x2 *>(src + 128 * EL * e);
-#pragma unroll
-                        for (int r = 0; r < VR; ++r) v[r] = x[r];
-                    } else {
-                        v[0] = *reinterpret_cast<const uint32_t *>(src + 128 * EL * e);
-                    }
-                }
+                for (int e = 0; e < SEG; ++e) load_value<VR>(src + 128 * EL * e, t.v[e][4 * s + i]);
         }
     };
 
@@ -213,63 +355,35 @@ __device__ __forceinline__ void attend_item(const SharedArgs &a, const Item &it,
         for (int e = 0; e < SEG * W; ++e) acc[b][e] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
     auto step = [&](Tile &t, int t0) __attribute__((always_inline)) {
-        const bool full = t0 >= it.lo && t0 + TILE <= it.end && t.there == 15u;
-        auto seen = [&](int i) {
-            const int pos = t0 + 16 * (i >> 2) + 4 * g + (i & 3);
-            return pos >= it.lo && pos < it.end && (t.there >> ((pos >> C.page_shift) - (t0 >> C.page_shift) & 3) & 1u);
-        };
-        if (!full) {
-            // what masked positions hold must not meet a weight of 0: NaN and infinities would stay
+        Start start{};
+        if (!(t0 >= it.lo && t0 + TILE <= it.end && t.there == 15u)) {
+            // what positions that are not seen hold must not meet a 0 or -inf: NaN and infinities would stay
+            start = start_of(C, t.there, t0, g, it.lo, it.end);
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                const bool in = seen_at(C, t.there, t0, t0 + 16 * s + c, it.lo, it.end);
+#pragma unroll
+                for (int j = 0; j < KB; ++j) t.k[s][j] = in ? t.k[s][j] : u32x4{0, 0, 0, 0};
+            }
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const bool in = seen(i);
+                const bool in = seen_at(C, t.there, t0, t0 + 16 * (i >> 2) + 4 * g + (i & 3), it.lo, it.end);
 #pragma unroll
                 for (int s = 0; s < SEG; ++s)
 #pragma unroll
-                    for (int r = 0; r < VR; ++r) t.v[i][s][r] = in ? t.v[i][s][r] : 0u;
+                    for (int r = 0; r < VR; ++r) t.v[s][i][r] = in ? t.v[s][i][r] : 0u;
             }
         }
-        // the values' operands: element W (lane's row) + e of eight positions
-        u32x4 vt[SEG][W];
+        u32x4 vt[SEG * W], key[2][QK];                         // (element W (lane's row) + e of eight positions)
 #pragma unroll
-        for (int s = 0; s < SEG; ++s)
-#pragma unroll
-            for (int r = 0; r < VR; ++r) {
-                auto &v = t.v;
-                if constexpr (FP8) {
-                    // elements 4 r .. 4 r + 3: bytes of two positions next to each other, then to fp16
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const uint32_t lo = __builtin_amdgcn_perm(v[2 * i + 1][s][r], v[2 * i][s][r], 0x05010400u);
-                        const uint32_t hi = __builtin_amdgcn_perm(v[2 * i + 1][s][r], v[2 * i][s][r], 0x07030602u);
-                        vt[s][4 * r][i] = fp8_f16<false>(lo);
-                        vt[s][4 * r + 1][i] = fp8_f16<true>(lo);
-                        vt[s][4 * r + 2][i] = fp8_f16<false>(hi);
-                        vt[s][4 * r + 3][i] = fp8_f16<true>(hi);
-                    }
-                } else {
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        vt[s][2 * r][i] = __builtin_amdgcn_perm(v[2 * i + 1][s][r], v[2 * i][s][r], 0x05040100u);
-                        vt[s][2 * r + 1][i] = __builtin_amdgcn_perm(v[2 * i + 1][s][r], v[2 * i][s][r], 0x07060302u);
-                    }
-                }
-            }
-        u32x4 key[2][QK];
+        for (int s = 0; s < SEG; ++s) turn_values<FP8, VR>(t.v[s], vt + s * W);
 #pragma unroll
         for (int s = 0; s < 2; ++s)
 #pragma unroll
-            for (int j = 0; j < QK; ++j) {
-                if constexpr (FP8) {
-                    const uint32_t lo = t.k[s][j >> 1][2 * (j & 1)], hi = t.k[s][j >> 1][2 * (j & 1) + 1];
-                    key[s][j] = u32x4{fp8_bf16<false>(lo), fp8_bf16<true>(lo), fp8_bf16<false>(hi), fp8_bf16<true>(hi)};
-                } else {
-                    key[s][j] = t.k[s][j];
-                }
-            }
+            for (int j = 0; j < QK; ++j) key[s][j] = key_piece<FP8, KB>(t.k[s], j);
 #pragma unroll
         for (int b = 0; b < HB; ++b) {
-            f32x4 x[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
+            f32x4 x[2] = {start.x[0], start.x[1]};
 #pragma unroll
             for (int j = 0; j < QK; ++j) {
                 u32x4 qj;
@@ -278,80 +392,24 @@ __device__ __forceinline__ void attend_item(const SharedArgs &a, const Item &it,
 #pragma unroll
                 for (int s = 0; s < 2; ++s) x[s] = mfma_bf16(key[s][j], qj, x[s]);
             }
-            float y[8], top = -__builtin_inff();
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                y[i] = x[i >> 2][i & 3];
-                if (!full) y[i] = seen(i) ? y[i] : -__builtin_inff();
-                top = fmaxf(top, y[i]);
-            }
-            // The reference follows the maximum only when that is 2^GROWTH past it, so that the sums are seldom carried over; weights are then up to
-            // that, and as fp16 (relative to 2^6 below the maximum that was met) up to 2^14.
-            constexpr float GROWTH = 8.f;
-            top *= scale;
-            if (__ballot(top > m[b] + (FP8 ? GROWTH + 6.f : GROWTH)) != 0) {
-                top = across_groups(top, [](float x, float y) { return fmaxf(x, y); });
-                if constexpr (FP8) top -= 6.f;
-                const float mn = fmaxf(m[b], top), fall = __builtin_amdgcn_exp2f(m[b] - mn);
-                m[b] = mn;
-                l[b] *= fall;
-#pragma unroll
-                for (int e = 0; e < SEG * W; ++e) acc[b][e] *= fall;
-            }
-            float p[8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                p[i] = __builtin_amdgcn_exp2f(fmaf(y[i], scale, -m[b]));
-                if (!full) p[i] = seen(i) ? p[i] : 0.f;        // (a scale of 0 times -inf)
-                l[b] += p[i];
-            }
-            if constexpr (FP8) {
-                u32x4 w;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const f16x2 h = {(_Float16)p[2 * i], (_Float16)p[2 * i + 1]};
-                    w[i] = __builtin_bit_cast(uint32_t, h);
-                }
-#pragma unroll
-                for (int s = 0; s < SEG; ++s)
-#pragma unroll
-                    for (int e = 0; e < W; ++e) acc[b][s * W + e] = mfma_f16(vt[s][e], w, acc[b][s * W + e]);
-            } else {
-                // Weights in two bf16 parts, 16 bits.  The first is cut, so that the second is not negative, and not 0: an infinite value then
-                // gives infinities of one sign.
-                u32x4 near, rest;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const uint32_t p0 = __float_as_uint(p[2 * i]), p1 = __float_as_uint(p[2 * i + 1]);
-                    near[i] = __builtin_amdgcn_perm(p1, p0, 0x07060302u);
-                    rest[i] = pack_bf16x2(fmaxf(p[2 * i] - __uint_as_float(p0 & 0xFFFF0000u), 1.2e-38f),
-                                          fmaxf(p[2 * i + 1] - __uint_as_float(p1 & 0xFFFF0000u), 1.2e-38f));
-                }
-#pragma unroll
-                for (int s = 0; s < SEG; ++s)
-#pragma unroll
-                    for (int e = 0; e < W; ++e) {
-                        acc[b][s * W + e] = mfma_bf16(vt[s][e], near, acc[b][s * W + e]);
-                        acc[b][s * W + e] = mfma_bf16(vt[s][e], rest, acc[b][s * W + e]);
-                    }
-            }
+            follow<FP8>(x, scale, m[b], l[b], acc[b]);
+            add_weighted<FP8, SEG * W>(vt, operands<FP8>(powers(x, scale, m[b], l[b])), acc[b]);
         }
     };
-
     // Pages are known two tiles ahead, a tile is asked for one ahead.
     int t0 = it.begin + wave * TILE;
     if (t0 < it.end) {
         Tile x;
-        Pages next = read_pages(t0);
+        Entries next = entries_at(t0);
         load(x, next, t0);
-        if (t0 + STEP < it.end) next = read_pages(t0 + STEP);
+        if (t0 + STEP < it.end) next = entries_at(t0 + STEP);
         for (;;) {
             const bool more = t0 + STEP < it.end;
             if constexpr (AHEAD) {
                 Tile y;
                 if (more) {
                     load(y, next, t0 + STEP);
-                    if (t0 + 2 * STEP < it.end) next = read_pages(t0 + 2 * STEP);
+                    if (t0 + 2 * STEP < it.end) next = entries_at(t0 + 2 * STEP);
                 }
                 step(x, t0);
                 x = y;
@@ -359,7 +417,7 @@ __device__ __forceinline__ void attend_item(const SharedArgs &a, const Item &it,
                 step(x, t0);
                 if (more) {
                     load(x, next, t0 + STEP);
-                    if (t0 + 2 * STEP < it.end) next = read_pages(t0 + 2 * STEP);
+                    if (t0 + 2 * STEP < it.end) next = entries_at(t0 + 2 * STEP);
                 }
             }
             if (!more) break;
@@ -411,21 +469,254 @@ __device__ __forceinline__ void attend_item(const SharedArgs &a, const Item &it,
     }
 }
 
-// Workgroups of a unit: two, of one wave per SIMD each, with up to 256 registers a lane, or one with up to 512.
-constexpr int wgs_per_unit(int D, int HB) { return HB * D <= 128 ? 2 : 1; }
-
-template <int D, bool FP8, int HB>
-__global__ __launch_bounds__(64 * WAVES, wgs_per_unit(D, HB)) void shared_kernel(SharedArgs a)
+// Columns of their own for every wave, HB blocks of 16: keys and values come to LDS once, as operands, 64 positions (a stage) at a time, those of
+// the next two stages on their way to registers meanwhile.  Of a tile of 32 two waves bring keys (KEYS), two turn values (where they have two
+// registers each at least).
+template <int D, bool FP8, int HB, bool KEYS>
+__device__ __forceinline__ void attend_columns(const SharedArgs &a, const Item &it, u32x4 *lds, uint32_t (*there)[2])
 {
-    __shared__ u32x4 lds_q[HB > 2 ? HB * (D / 32) * 64 : 1];
-    __shared__ float wave_m[WAVES][16], wave_l[WAVES][16];
-    __shared__ __attribute__((aligned(16))) float joined[WAVES][16][Shape<D>::DS + 4];
+    constexpr int QK = D / 32, W = D / 16, KB = FP8 ? D / 64 : D / 32, VR = FP8 ? W / 4 : W / 2, EL = FP8 ? 1 : 2;
+    constexpr int SUB = 2, STEP = TILE * SUB;         // tiles of a stage
+    constexpr int FRAGS = 2 * QK + W;                 // operands of a tile: of the keys, then of the values
+    constexpr int VH = VR > 1 ? VR / 2 : 1, WH = VH * (FP8 ? 4 : 2);      // registers, and elements, of a value that a wave turns
     const CacheArgs &C = a.cache;
-    Item it;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int c = lane & 15, g = lane >> 4;
+    const int slot_bytes = (int)C.slot_stride * EL, last = it.end - 1;
+    uint32_t turn;
+    const float scale = scale_of<FP8>(a, it.kv_head, turn);
+    const bool idle = !KEYS && VR == 1 && (wave & 1);
+    const int sub = wave >> 1 & 1, half = wave & 1;   // tile of a stage; which keys, or elements, of it
+    const uint8_t *base = static_cast<const uint8_t *>(KEYS ? C.k : C.v) + it.kv_head * C.head_stride * EL + (KEYS ? 16 * g : (W * c + (idle ? 0 : WH * half)) * EL);
+    // This wave's tile of a stage; past the last one, that again (as many loads in every stage: what is waited for is counted).
+    auto tile_at = [&](int t0) __attribute__((always_inline)) {
+        const int t = t0 + TILE * sub, most = it.begin + ((last - it.begin) & ~(TILE - 1));
+        return t < most ? t : most;
+    };
+    Entries next;
+    auto entries_at = [&](int t0) __attribute__((always_inline)) { next = read_entries(C, it.table, last, tile_at(t0)); };
+    struct Raw {
+        uint32_t r[8][2];                             // pieces of a key, or VH registers of eight values
+        uint32_t there;
+    };
+    Raw raw[2];                                       // of the stages after this one, by their number's last bit
+    static_assert(KB * 4 <= 16 && VH <= 2);
+    auto fetch = [&](Raw &raw, int t0) __attribute__((always_inline)) {
+        const int t = tile_at(t0);
+        const Pages pages = pages_of(C, next, EL);
+        raw.there = pages.there;
+        if constexpr (KEYS) {
+            const uint8_t *src = base + place_of(C, pages, t, t + 16 * half + c, last, slot_bytes);
+#pragma unroll
+            for (int j = 0; j < KB; ++j) {
+                const u32x4 k = *reinterpret_cast<const u32x4 *>(src + 64 * j);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) raw.r[2 * j + (r >> 1)][r & 1] = k[r];
+            }
+        } else {
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                const uint8_t *src = base + place_of(C, pages, t, t + 16 * s + 4 * g, last & ~3, slot_bytes);
+#pragma unroll
+                for (int i = 0; i < 4; ++i, src += slot_bytes) {
+                    uint32_t v[VH];
+                    load_value<VH>(src, v);
+#pragma unroll
+                    for (int r = 0; r < VH; ++r) raw.r[4 * s + i][r] = v[r];
+                }
+            }
+        }
+    };
+    auto keep = [&](Raw &raw, int buffer, int t0) __attribute__((always_inline)) {
+        const int t = t0 + TILE * sub;
+        if (t >= it.end || idle) return;
+        u32x4 *to = lds + ((buffer * SUB + sub) * FRAGS) * 64 + lane;
+        constexpr int USED = KEYS ? 2 * KB : 8;
+        if (t + TILE > it.end || raw.there != 15u) {
+            // what positions that are not seen hold must not meet a 0 or -inf: NaN and infinities would stay
+            const bool key_in = seen_at(C, raw.there, t, t + 16 * half + c, it.lo, it.end);
+#pragma unroll
+            for (int i = 0; i < USED; ++i) {
+                const bool in = KEYS ? key_in : seen_at(C, raw.there, t, t + 16 * (i >> 2) + 4 * g + (i & 3), it.lo, it.end);
+#pragma unroll
+                for (int r = 0; r < (KEYS ? 2 : VH); ++r) raw.r[i][r] = in ? raw.r[i][r] : 0u;
+            }
+        }
+        if constexpr (KEYS) {
+            if (lane == 0) there[buffer][sub] = raw.there;
+            u32x4 k[KB];
+#pragma unroll
+            for (int j = 0; j < KB; ++j) k[j] = u32x4{raw.r[2 * j][0], raw.r[2 * j][1], raw.r[2 * j + 1][0], raw.r[2 * j + 1][1]};
+#pragma unroll
+            for (int j = 0; j < QK; ++j) to[(half * QK + j) * 64] = key_piece<FP8, KB>(k, j);
+        } else {
+            uint32_t v[8][VH];
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+#pragma unroll
+                for (int r = 0; r < VH; ++r) v[i][r] = raw.r[i][r];
+            u32x4 vt[WH];
+            turn_values<FP8, VH>(v, vt);
+#pragma unroll
+            for (int e = 0; e < WH; ++e) to[(2 * QK + WH * half + e) * 64] = vt[e];
+        }
+    };
+
+    u32x4 q[HB][QK];
+    float m[HB], l[HB];
+    f32x4 acc[HB][W];
+#pragma unroll
+    for (int b = 0; b < HB; ++b) {
+        m[b] = LOWEST;
+        l[b] = 0.f;
+#pragma unroll
+        for (int s = 0; s < QK; ++s) q[b][s] = query_piece<D, FP8>(a, it, 16 * (wave * HB + b) + c, s, g, turn);
+#pragma unroll
+        for (int e = 0; e < W; ++e) acc[b][e] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+
+    // A step is a block of columns of a tile.  While its scores become weights, the matrix instructions are those of its neighbours, one by one
+    // between the vector instructions: values x weights of the block before, keys x queries of the one after.  (Of a single block the weights are added
+    // first: its reference may move.)
+    u32x4 key[2 * QK], vt[W];
+    uint32_t next_pages = 15u;                        // of the tile whose keys were read, and where it begins
+    int next_t0 = it.begin;
+    f32x4 x[2];
+    Weights<FP8> w{};
+#pragma unroll
+    for (int e = 0; e < W; ++e) vt[e] = u32x4{0, 0, 0, 0};
+    int t0 = it.begin;                                // of the present tile
+    auto operands_of = [&](int stage, int tile) __attribute__((always_inline)) { return lds + (stage * SUB + tile) * FRAGS * 64 + lane; };
+    auto read_keys = [&](int stage, int tile, int t) __attribute__((always_inline)) {
+        const u32x4 *from = operands_of(stage, tile);
+#pragma unroll
+        for (int j = 0; j < 2 * QK; ++j) key[j] = from[j * 64];
+        next_pages = there[stage][tile];
+        next_t0 = t;
+    };
+    auto begin_scores = [&]() __attribute__((always_inline)) {
+        x[0] = x[1] = f32x4{0.f, 0.f, 0.f, 0.f};
+        const uint32_t pages = __builtin_amdgcn_readfirstlane(next_pages);
+        if (next_t0 + TILE > it.end || pages != 15u) {
+            const Start start = start_of(C, pages, next_t0, g, it.lo, it.end);
+            x[0] = start.x[0];
+            x[1] = start.x[1];
+        }
+    };
+    // (stage: its number's last bit.  Past the last tile everything goes on, so that the loads in flight are always as many; those scores are not used.)
+    auto next_keys = [&](int stage, int tile) __attribute__((always_inline)) {
+        const int next_tile = t0 + TILE;
+        if (tile == SUB - 1) {
+            keep(raw[stage ^ 1], stage ^ 1, next_tile);
+            __syncthreads();
+            fetch(raw[stage ^ 1], next_tile + 2 * STEP);
+            entries_at(next_tile + 3 * STEP);
+            read_keys(stage ^ 1, 0, next_tile);
+        } else {
+            read_keys(stage, tile + 1, next_tile);
+        }
+    };
+    auto step = [&](int stage, int tile, int b) __attribute__((always_inline)) {
+        constexpr bool APART = HB > 1;
+        if (APART && b == HB - 1) next_keys(stage, tile);
+        if (!APART) add_weighted<FP8, W>(vt, w, acc[0]);
+        follow<FP8>(x, scale, m[b], l[b], acc[b]);
+        f32x4 *before = acc[b > 0 ? b - 1 : HB - 1];
+        float p[8], rest[8];
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            if (APART && i < W) before[i] = FP8 ? mfma_f16(vt[i], w.near, before[i]) : mfma_bf16(vt[i], w.near, before[i]);
+            p[i] = __builtin_amdgcn_exp2f(fmaf(x[i >> 2][i & 3], scale, -m[b]));
+            __builtin_amdgcn_sched_barrier(0);
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            if (APART && !FP8 && i < W) before[i] = mfma_bf16(vt[i], w.rest, before[i]);
+            l[b] += p[i];
+            // (see operands)
+            if (!FP8) rest[i] = fmaxf(p[i] - __uint_as_float(__float_as_uint(p[i]) & 0xFFFF0000u), 1.2e-38f);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        if (b == 0) {
+            const u32x4 *from = operands_of(stage, tile);
+#pragma unroll
+            for (int e = 0; e < W; ++e) vt[e] = from[(2 * QK + e) * 64];
+        }
+        if (!APART) next_keys(stage, tile);
+        begin_scores();
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int j = 0; j < 2 * QK; ++j) {
+            x[j & 1] = mfma_bf16(key[(j & 1) * QK + (j >> 1)], q[b + 1 < HB ? b + 1 : 0][j >> 1], x[j & 1]);
+            if (j < 4) {
+                if constexpr (FP8) {
+                    const f16x2 h = {(_Float16)p[2 * j], (_Float16)p[2 * j + 1]};
+                    w.near[j] = __builtin_bit_cast(uint32_t, h);
+                } else {
+                    w.near[j] = __builtin_amdgcn_perm(__float_as_uint(p[2 * j + 1]), __float_as_uint(p[2 * j]), 0x07060302u);
+                    w.rest[j] = pack_bf16x2(rest[2 * j], rest[2 * j + 1]);
+                }
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+    entries_at(it.begin);
+    fetch(raw[0], it.begin);
+    entries_at(it.begin + STEP);
+    fetch(raw[1], it.begin + STEP);
+    entries_at(it.begin + 2 * STEP);
+    keep(raw[0], 0, it.begin);
+    __syncthreads();
+    fetch(raw[0], it.begin + 2 * STEP);
+    entries_at(it.begin + 3 * STEP);
+    read_keys(0, 0, t0);
+    begin_scores();
+#pragma unroll
+    for (int j = 0; j < 2 * QK; ++j) x[j & 1] = mfma_bf16(key[(j & 1) * QK + (j >> 1)], q[0][j >> 1], x[j & 1]);
+    for (bool more = true; more;) {
+#pragma unroll
+        for (int tile = 0; tile < 2 * SUB; ++tile) {
+            if (!more) break;
+#pragma unroll
+            for (int b = 0; b < HB; ++b) step(tile / SUB, tile % SUB, b);
+            t0 += TILE;
+            more = t0 < it.end;
+        }
+    }
+    add_weighted<FP8, W>(vt, w, acc[HB - 1]);
+    const float v_scale = FP8 && C.v_scale ? C.v_scale[it.kv_head] : 1.f;
+#pragma unroll
+    for (int b = 0; b < HB; ++b) {
+        l[b] = across_groups(l[b], [](float x, float y) { return x + y; });
+        const int column = 16 * (wave * HB + b) + c;
+        if (column >= it.n) continue;
+        const size_t place = (size_t)it.slot + column;
+        if (g == 0) {
+            a.part_ml[2 * place] = m[b];
+            a.part_ml[2 * place + 1] = l[b];
+        }
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+#pragma unroll
+            for (int e = 0; e < W; e += 4) {
+                f32x4 x;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) x[i] = acc[b][e + i][r] * v_scale;
+                *reinterpret_cast<f32x4 *>(a.part + place * D + W * (4 * g + r) + e) = x;
+            }
+    }
+}
+
+// The item of a workgroup: true, of the shared positions; it.n < 1: none.
+__device__ __forceinline__ bool item_of(const SharedArgs &a, Item &it)
+{
+    const CacheArgs &C = a.cache;
+    it.n = 0;
     if ((int)blockIdx.x < a.prefix_wgs) {
         // The workgroups of a chunk that have different columns read the same positions: they are eight apart, on one XCD, at the same time.
         const int per = 8 * a.tiles, eight = (int)blockIdx.x / per, in = (int)blockIdx.x - eight * per, tile = in / 8, unit = 8 * eight + in - 8 * tile;
-        if (unit >= a.chunks * C.kv_heads) return;
+        if (unit >= a.chunks * C.kv_heads) return true;
         const int chunk = unit / C.kv_heads;
         it.kv_head = unit - chunk * C.kv_heads;
         it.first = tile * a.columns;
@@ -435,27 +726,55 @@ __global__ __launch_bounds__(64 * WAVES, wgs_per_unit(D, HB)) void shared_kernel
         it.end = a.shared - it.begin < a.chunk ? a.shared : it.begin + a.chunk;
         it.table = C.table + a.prefix * C.table_stride;
         it.slot = ((long long)unit * a.tiles + tile) * a.columns;
-        attend_item<D, FP8, HB>(a, it, lds_q, wave_m, wave_l, joined);
-    } else {
-        const int number = (int)blockIdx.x - a.prefix_wgs, item = number / a.own_splits, split = number - item * a.own_splits;
-        const int of_row = item / a.own_blocks, block = item - of_row * a.own_blocks, row = of_row / C.kv_heads;
-        RowInfo r = row_info(a, row);
-        r.len = __builtin_amdgcn_readfirstlane(r.len);
-        r.lo = __builtin_amdgcn_readfirstlane(r.lo);
-        r.seq = __builtin_amdgcn_readfirstlane(r.seq);
-        const OwnChunks o = own_chunks(a, r);
-        if (split >= o.n) return;
-        it.kv_head = of_row - row * C.kv_heads;
-        it.first = row * a.group + block * a.own_columns;
-        it.n = a.group - block * a.own_columns;
-        it.n = it.n < a.own_columns ? it.n : a.own_columns;
-        it.lo = r.lo;
-        it.begin = o.from + split * o.length;
-        it.end = r.len - it.begin < o.length ? r.len : it.begin + o.length;
-        it.table = C.table + r.seq * C.table_stride;
-        it.slot = (long long)a.chunks * C.kv_heads * a.tiles * a.columns + (long long)number * a.own_columns;
-        attend_item<D, FP8, 1>(a, it, lds_q, wave_m, wave_l, joined);
+        return true;
     }
+    const int number = (int)blockIdx.x - a.prefix_wgs, item = number / a.own_splits, split = number - item * a.own_splits;
+    const int of_row = item / a.own_blocks, block = item - of_row * a.own_blocks, row = of_row / C.kv_heads;
+    RowInfo r = row_info(a, row);
+    r.len = __builtin_amdgcn_readfirstlane(r.len);
+    r.lo = __builtin_amdgcn_readfirstlane(r.lo);
+    r.seq = __builtin_amdgcn_readfirstlane(r.seq);
+    const OwnChunks o = own_chunks(a, r);
+    if (split >= o.n) return false;
+    it.kv_head = of_row - row * C.kv_heads;
+    it.first = row * a.group + block * a.own_columns;
+    it.n = a.group - block * a.own_columns;
+    it.n = it.n < a.own_columns ? it.n : a.own_columns;
+    it.lo = r.lo;
+    it.begin = o.from + split * o.length;
+    it.end = r.len - it.begin < o.length ? r.len : it.begin + o.length;
+    it.table = C.table + r.seq * C.table_stride;
+    it.slot = (long long)a.chunks * C.kv_heads * a.tiles * a.columns + (long long)number * a.own_columns;
+    return false;
+}
+
+// Workgroups of a unit: two, of one wave per SIMD each, with up to 256 registers a lane, or one with up to 512.
+constexpr int wgs_per_unit(int D, int HB) { return HB * D <= 128 ? 2 : 1; }
+
+template <int D, bool FP8, int HB>
+__global__ __launch_bounds__(256, wgs_per_unit(D, HB)) void shared_kernel(SharedArgs a)
+{
+    __shared__ u32x4 lds_q[HB > 2 ? HB * (D / 32) * 64 : 1];
+    __shared__ float wave_m[4][16], wave_l[4][16];
+    __shared__ __attribute__((aligned(16))) float joined[4][16][Shape<D>::DS + 4];
+    Item it;
+    const bool of_prefix = item_of(a, it);
+    if (it.n < 1) return;
+    if (of_prefix) attend_item<D, FP8, HB, 4>(a, it, lds_q, wave_m, wave_l, joined);
+    else attend_item<D, FP8, 1, 4>(a, it, lds_q, wave_m, wave_l, joined);
+}
+
+// The shared positions of many columns, 128 HB of a workgroup of eight waves.
+template <int D, bool FP8, int HB>
+__global__ __launch_bounds__(512, 1) void shared_wide_kernel(SharedArgs a)
+{
+    __shared__ u32x4 operands[2 * 2 * (D / 8) * 64];
+    __shared__ uint32_t there[2][2];
+    Item it;
+    item_of(a, it);
+    if (it.n < 1) return;
+    if (threadIdx.x < 256) attend_columns<D, FP8, HB, true>(a, it, operands, there);
+    else attend_columns<D, FP8, HB, false>(a, it, operands, there);
 }
 
 // Joins a column's parts: a workgroup per row and head.  A group of D / 4 lanes has some of the parts, 16 bytes of a part's sums a lane, four
@@ -525,6 +844,7 @@ template <int D> __global__ __launch_bounds__(256) void shared_join_kernel(Share
 
 // How a call is cut.
 struct SharedPlan {
+    bool wide;
     int hb, columns, tiles, chunk, chunks, own_chunk, own_splits, own_blocks, own_columns;
     long long prefix_wgs, own_wgs;
     size_t part_bytes, ml_bytes;
@@ -536,27 +856,38 @@ SharedPlan shared_plan(const peqa_kv_cache *C, int rows, int heads, int max_len,
     const int group = heads / C->kv_heads;
     if (max_len < shared) shared = 0;                          // (every row ends among the shared positions, and has them by itself)
     const long long queries = (long long)rows * group;
-    const int most = 512 / C->head_dim;                        // (as many as there are registers for)
+    const int most = C->head_dim > 128 ? 2 : 4;                // (as many as there are registers for)
     p.hb = 1;
     while (p.hb < most && 16 * p.hb < queries) p.hb *= 2;
     p.columns = 16 * p.hb;
+    p.wide = C->head_dim <= 128 && queries > 64;
+    if (p.wide) {
+        p.hb = queries > 128 ? 2 : 1;
+        p.columns = 128 * p.hb;
+    }
     p.tiles = (int)((queries + p.columns - 1) / p.columns);
     p.own_columns = group < 16 ? group : 16;
     p.own_blocks = (group + p.own_columns - 1) / p.own_columns;
     const long long own = max_len > shared ? max_len - shared + TILE - 1 : 0;
     const long long items = (long long)rows * C->kv_heads * p.own_blocks, units = (long long)C->kv_heads * p.tiles;
-    // all that there is to walk, over as many workgroups as have room at once, 128 positions at least
-    const int wgs = PLAN_UNITS * wgs_per_unit(C->head_dim, p.hb);
-    const long long all = units * shared + items * own;
-    long long chunk = (all + wgs - 1) / wgs;
-    chunk = (chunk + STEP - 1) / STEP * STEP;
-    if (chunk < STEP) chunk = STEP;
+    // all that there is to walk, over as many workgroups as have room at once, 128 positions at least; with many columns by a launch each
+    auto per_workgroup = [](long long all, int wgs) {
+        const long long chunk = ((all + wgs - 1) / wgs + UNIT - 1) / UNIT * UNIT;
+        return chunk < UNIT ? (long long)UNIT : chunk;
+    };
+    long long chunk, own_chunk;
+    if (p.wide) {
+        chunk = per_workgroup(units * shared, PLAN_UNITS);
+        own_chunk = per_workgroup(items * own, 2 * PLAN_UNITS);
+    } else {
+        chunk = own_chunk = per_workgroup(units * shared + items * own, PLAN_UNITS * wgs_per_unit(C->head_dim, p.hb));
+    }
     p.chunks = (int)((shared + chunk - 1) / chunk);
     p.chunk = p.chunks > 0 ? (int)(((shared + p.chunks - 1) / p.chunks + TILE - 1) / TILE * TILE) : TILE;
     p.chunks = (shared + p.chunk - 1) / p.chunk;
-    p.own_splits = (int)((own + chunk - 1) / chunk);
+    p.own_splits = (int)((own + own_chunk - 1) / own_chunk);
     if (p.own_splits < 1) p.own_splits = 1;                    // (rows that end among the shared positions)
-    p.own_chunk = STEP;
+    p.own_chunk = UNIT;
     p.prefix_wgs = ((long long)p.chunks * C->kv_heads + 7) / 8 * 8 * p.tiles;
     p.own_wgs = items * p.own_splits;
     const size_t slots = (size_t)p.chunks * (size_t)units * (size_t)p.columns + (size_t)p.own_wgs * (size_t)p.own_columns;
@@ -567,15 +898,25 @@ SharedPlan shared_plan(const peqa_kv_cache *C, int rows, int heads, int max_len,
 
 template <int D, bool FP8> hipError_t launch_shared(const SharedArgs &a, const SharedPlan &p, hipStream_t stream)
 {
-    auto kernel = p.hb == 1 ? shared_kernel<D, FP8, 1> : shared_kernel<D, FP8, 2>;
-    if constexpr (D <= 128)
-        if (p.hb == 4) kernel = shared_kernel<D, FP8, 4>;
-    if constexpr (D <= 64)
-        if (p.hb == 8) kernel = shared_kernel<D, FP8, 8>;
-    trace_before(KID_SHARED, stream);
-    hipLaunchKernelGGL(kernel, dim3((unsigned)(p.prefix_wgs + p.own_wgs)), dim3(64 * WAVES), 0, stream, a);
-    trace_after(KID_SHARED, stream);
-    const hipError_t e = hipGetLastError();
+    auto run = [&](auto kernel, const SharedArgs &args, long long wgs, int threads) {
+        trace_before(KID_SHARED, stream);
+        hipLaunchKernelGGL(kernel, dim3((unsigned)wgs), dim3(threads), 0, stream, args);
+        trace_after(KID_SHARED, stream);
+        return hipGetLastError();
+    };
+    hipError_t e = hipSuccess;
+    if constexpr (D <= 128) {
+        if (p.wide) {
+            if (p.prefix_wgs > 0) e = run(p.hb == 1 ? shared_wide_kernel<D, FP8, 1> : shared_wide_kernel<D, FP8, 2>, a, p.prefix_wgs, 512);
+            if (e != hipSuccess) return e;
+            SharedArgs own = a;
+            own.prefix_wgs = 0;
+            e = run(shared_kernel<D, FP8, 1>, own, p.own_wgs, 256);
+        } else if (p.hb == 4) {
+            e = run(shared_kernel<D, FP8, 4>, a, p.prefix_wgs + p.own_wgs, 256);
+        }
+    }
+    if (!p.wide && p.hb < 4) e = run(p.hb == 1 ? shared_kernel<D, FP8, 1> : shared_kernel<D, FP8, 2>, a, p.prefix_wgs + p.own_wgs, 256);
     if (e != hipSuccess) return e;
     trace_before(KID_SHARED_JOIN, stream);
     hipLaunchKernelGGL(shared_join_kernel<D>, dim3((unsigned)a.rows * (unsigned)a.heads), dim3(256), 0, stream, a);

@@ -93,7 +93,8 @@ def both(torch, peqa, gen, shared, own, kv, dim, page, fp8, layout="heads"):
     (1, [1], 1, 1, 64, 8, "heads"), (1, [0, 0], 1, 1, 128, 8, "heads"), (33, [1, 5, 0], 2, 2, 64, 8, "slots"), (555, [77, 3, 40], 4, 1, 128, 16, "both"),
     (128, [128] * 17, 2, 1, 64, 32, "heads"), (100, [300, 1, 31, 32, 33], 1, 16, 128, 64, "heads"), (257, [65] * 9, 2, 8, 128, 16, "slots"),
     (1000, [20, 30], 1, 40, 64, 8, "heads"), (700, [9, 90] * 20, 1, 4, 256, 128, "heads"), (31, [1500, 2], 2, 3, 256, 16, "both"),
-    (5000, [64] * 3, 1, 12, 128, 16, "heads"), (2050, [130] * 33, 1, 8, 64, 8, "heads"), (0, [40, 1, 0], 2, 4, 128, 16, "heads")])
+    (5000, [64] * 3, 1, 12, 128, 16, "heads"), (2050, [130] * 33, 1, 8, 64, 8, "heads"), (0, [40, 1, 0], 2, 4, 128, 16, "heads"),
+    (1100, [33] * 20, 2, 8, 128, 16, "both"), (3001, [5, 600] * 20, 1, 14, 128, 8, "slots"), (130, [1, 2] * 40, 1, 1, 64, 64, "heads"), (97, [40] * 70, 3, 2, 128, 32, "heads")])
 def test_shared(env, shared, own, kv, group, dim, page, layout, fp8):
     torch, peqa = env
     gen = torch.Generator().manual_seed(shared + sum(own) + dim)
