@@ -18,7 +18,7 @@ struct EvictArgs {
     int32_t *kept, *new_lens;              // [n, kv_heads, keep]; new_lens or null
     int32_t *moved;                        // [n] positions that an entry keeps and the move kernel looks at
     int n, max_len, keep, sinks, recent;
-    int splits, chunks;                    // of the move: workgroups for the bytes of a position, and for the positions of a head
+    int splits, chunks, chunk;             // of the move: workgroups for the bytes of a position, for the positions of a head, and positions of one
     int row_bytes;                         // bytes of a head's position
     bool in_place;
 };
@@ -58,13 +58,14 @@ __device__ __forceinline__ uint32_t order_of(float w)
     return w != w ? 0u : b ^ ((uint32_t)((int32_t)b >> 31) | 0x80000000u);
 }
 
-constexpr int SELECT_THREADS = 1024, WAVES = SELECT_THREADS / 64;
-
 // One workgroup for a sequence and a key head.  The least weight that stays is found digit by digit, 11, 11 and 10 bits, each by a
-// histogram of the weights that have the digits found so far (counts: no order of adding matters); then, 1024 positions at a time and
-// in order, those above it and as many equal ones as there is room for get their places.
-__global__ __launch_bounds__(SELECT_THREADS) void evict_select_kernel(EvictArgs a)
+// histogram of the weights that have the digits found so far (counts: no order of adding matters); then, as many positions as there
+// are threads at a time and in order, those above it and as many equal ones as there is room for get their places.
+template <int THREADS>
+__global__ __launch_bounds__(THREADS) void evict_select_kernel(EvictArgs a)
 {
+    constexpr int WAVES = THREADS / 64, OWN = 2048 / THREADS;
+    constexpr int FIRST = 4096 / THREADS, FLIGHT = 8;      // weights of a thread that stay in registers; of the others, in flight
     __shared__ uint32_t bins[2048];
     __shared__ uint32_t scan[2][WAVES][2];
     __shared__ uint32_t found[2];                          // the digit, and how many of its weights stay
@@ -78,13 +79,22 @@ __global__ __launch_bounds__(SELECT_THREADS) void evict_select_kernel(EvictArgs 
         a.moved[i] = e.again ? 0 : stays;
     }
     if (e.again || e.len == 0) {
-        for (int j = tid; j < a.keep; j += SELECT_THREADS) kept[j] = -1;
+        for (int j = tid; j < a.keep; j += THREADS) kept[j] = -1;
         return;
     }
     const float *in = a.weights + e.seq * a.seq_stride + h * a.head_stride;
     float *out = a.weights_out + e.seq * a.seq_stride + h * a.head_stride;
     const int lo = a.sinks, hi = e.len - a.recent;         // those that have to be chosen from, where some leave
     const bool all = e.len <= a.keep;
+    // the first weights' orders stay in registers over the passes, the others (past 4096 positions) are read again
+    uint32_t order[FIRST];
+    float first_w[FIRST];
+#pragma unroll
+    for (int k = 0; k < FIRST; ++k) {
+        const int j = k * THREADS + tid;
+        first_w[k] = j < e.len ? in[j] : 0.f;
+        order[k] = order_of(first_w[k]);
+    }
     uint32_t least = 0, equal = 0;                         // the least order that stays, and how many of it
     if (!all) {
         uint32_t room = (uint32_t)(a.keep - a.sinks - a.recent), known = 0, mask = 0;
@@ -94,16 +104,29 @@ __global__ __launch_bounds__(SELECT_THREADS) void evict_select_kernel(EvictArgs 
 #pragma unroll 1
             for (int pass = 0; pass < 3; ++pass) {
                 const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, digits = pass == 2 ? 1024 : 2048;
-                for (int j = tid; j < 2048; j += SELECT_THREADS) bins[j] = 0;
+                for (int j = tid; j < 2048; j += THREADS) bins[j] = 0;
                 __syncthreads();
-                for (int j = lo + tid; j < hi; j += SELECT_THREADS) {
-                    const uint32_t o = order_of(in[j]);
-                    if ((o & mask) == known) atomicAdd(&bins[(o >> shift) & (digits - 1)], 1u);
+                auto count = [&](int j, uint32_t o) {
+                    if (j >= lo && j < hi && (o & mask) == known) atomicAdd(&bins[(o >> shift) & (digits - 1)], 1u);
+                };
+#pragma unroll
+                for (int k = 0; k < FIRST; ++k) count(k * THREADS + tid, order[k]);
+                for (int j0 = FIRST * THREADS + tid; j0 < hi; j0 += FLIGHT * THREADS) {
+                    float w[FLIGHT];
+#pragma unroll
+                    for (int k = 0; k < FLIGHT; ++k) w[k] = in[j0 + k * THREADS < hi ? j0 + k * THREADS : j0];
+#pragma unroll
+                    for (int k = 0; k < FLIGHT; ++k) count(j0 + k * THREADS, order_of(w[k]));
                 }
                 __syncthreads();
-                // from the top: thread t has the digits 2047 - 2 t and 2046 - 2 t
-                const uint32_t high = bins[2047 - 2 * tid], low = bins[2046 - 2 * tid];
-                uint32_t upto = high + low;
+                // from the top: thread t has the OWN digits up to 2047 - OWN t
+                uint32_t own[OWN], mine = 0;
+#pragma unroll
+                for (int d = 0; d < OWN; ++d) {
+                    own[d] = bins[2047 - OWN * tid - d];
+                    mine += own[d];
+                }
+                uint32_t upto = mine;
 #pragma unroll
                 for (int o = 1; o < 64; o *= 2) {
                     const uint32_t other = __shfl_up(upto, o);
@@ -111,12 +134,18 @@ __global__ __launch_bounds__(SELECT_THREADS) void evict_select_kernel(EvictArgs 
                 }
                 if (lane == 63) scan[0][wave][0] = upto;
                 __syncthreads();
-                uint32_t before = upto - high - low;
-                for (int w = 0; w < wave; ++w) before += scan[0][w][0];
-                if (before < room && room <= before + high + low) {
-                    const bool first = room <= before + high;
-                    found[0] = first ? 2047 - 2 * tid : 2046 - 2 * tid;
-                    found[1] = first ? room - before : room - before - high;
+                uint32_t before = upto - mine;
+#pragma unroll
+                for (int w = 0; w < WAVES; ++w) before += w < wave ? scan[0][w][0] : 0;
+                if (before < room && room <= before + mine) {
+#pragma unroll
+                    for (int d = 0; d < OWN; ++d) {
+                        if (before < room && room <= before + own[d]) {
+                            found[0] = 2047 - OWN * tid - d;
+                            found[1] = room - before;
+                        }
+                        before += own[d];
+                    }
                 }
                 __syncthreads();
                 known |= found[0] << shift;
@@ -129,11 +158,9 @@ __global__ __launch_bounds__(SELECT_THREADS) void evict_select_kernel(EvictArgs 
         }
     }
     uint32_t larger_before = 0, equal_before = 0;
-    for (int from = 0, k = 0; from < e.len; from += SELECT_THREADS, k ^= 1) {
+    auto place = [&](int from, int k, float w, uint32_t o) __attribute__((always_inline)) {
         const int j = from + tid;
-        const float w = j < e.len ? in[j] : 0.f;
         const bool held = all || j < lo || j >= hi;
-        const uint32_t o = order_of(w);
         const bool is_larger = j < e.len && (held || o > least), is_equal = j < e.len && !held && o == least;
         const uint64_t larger = __ballot(is_larger), same = __ballot(is_equal), below = (1ull << lane) - 1;
         if (lane == 0) {
@@ -155,19 +182,37 @@ __global__ __launch_bounds__(SELECT_THREADS) void evict_select_kernel(EvictArgs 
             kept[at] = j;
             out[at] = w;
         }
+    };
+#pragma unroll
+    for (int k = 0; k < FIRST; ++k)
+        if (k * THREADS < e.len) place(k * THREADS, k & 1, first_w[k], order[k]);
+    for (int from = FIRST * THREADS; from < e.len; from += FLIGHT * THREADS) {
+        float w[FLIGHT];                                   // (read before any of their places is written)
+#pragma unroll
+        for (int k = 0; k < FLIGHT; ++k) w[k] = from + k * THREADS + tid < e.len ? in[from + k * THREADS + tid] : 0.f;
+#pragma unroll
+        for (int k = 0; k < FLIGHT; ++k)
+            if (from + k * THREADS < e.len) place(from + k * THREADS, k & 1, w[k], order_of(w[k]));
     }
     __syncthreads();
-    for (int j = stays + tid; j < a.keep; j += SELECT_THREADS) kept[j] = -1;
-    for (int j = stays + tid; j < a.max_len; j += SELECT_THREADS) out[j] = 0.f;
+    for (int j = stays + tid; j < a.keep; j += THREADS) kept[j] = -1;
+    for (int j = stays + tid; j < a.max_len; j += THREADS) out[j] = 0.f;
 }
 
-constexpr int MOVE_THREADS = 256, EACH = 4;                // positions that a thread has in flight
+constexpr int SECTION = 1024;          // positions whose places are looked up at a time
+constexpr int each_of(int threads) { return threads > 512 ? 4 : 8; }   // positions that a thread has in flight
 
-// Keys or values of a sequence and a key head, or some of the bytes of each, to their places.  In place a workgroup goes over all
-// positions in order: no position moves up, so what is written lies at or below what the workgroup has read, and no other workgroup has
-// these bytes.  To another cache the positions are split over workgroups too.
-__global__ __launch_bounds__(MOVE_THREADS) void evict_move_kernel(EvictArgs a)
+// Keys or values of a sequence and a key head, or some of the bytes of each, to their places.  Where they come from and go to is found for a
+// section first (two loads after one another for all of it); then the next positions' bytes are asked for before the present ones are stored.
+// In place a workgroup goes over all positions in order: no position moves up, so what is written lies at or below what the
+// workgroup has read when it writes, what is read next lies above, and no other workgroup has these bytes.  To another cache the positions
+// are split over workgroups too.
+// Bound by memory where there are many heads (DESCRIBED BELOW).
+template <int THREADS>
+__global__ __launch_bounds__(THREADS) void evict_move_kernel(EvictArgs a)
 {
+    constexpr int EACH = each_of(THREADS);
+    __shared__ long long from_at[SECTION], to_at[SECTION];  // in bytes; -1: from nowhere (zeros), to nowhere
     unsigned b = blockIdx.x;
     const int chunk = (int)(b % (unsigned)a.chunks);
     b /= (unsigned)a.chunks;
@@ -177,38 +222,58 @@ __global__ __launch_bounds__(MOVE_THREADS) void evict_move_kernel(EvictArgs a)
     b >>= 1;
     const int i = (int)(b / (unsigned)a.from.kv_heads), h = (int)(b - (unsigned)i * (unsigned)a.from.kv_heads);
     const int n = a.moved[i], seq = a.seq ? a.seq[i] : i;
-    const int bytes = a.row_bytes / a.splits, lanes = bytes / 16, rows = MOVE_THREADS / lanes;
+    const int bytes = a.row_bytes / a.splits, lanes = bytes / 16, rows = THREADS / lanes;
     const int row = (int)threadIdx.x / lanes, at = split * bytes + 16 * ((int)threadIdx.x - row * lanes);
     const int step = EACH * rows;
     const int32_t *kept = a.kept + ((size_t)i * a.from.kv_heads + h) * (size_t)a.keep;
     const uint8_t *src = static_cast<const uint8_t *>(is_v ? a.from.v : a.from.k) + h * a.from.head_stride + at;
     uint8_t *dst = static_cast<uint8_t *>(is_v ? a.to.v : a.to.k) + h * a.to.head_stride + at;
     const int32_t *table = a.from.table + seq * a.from.table_stride, *to_table = a.to.table + seq * a.to.table_stride;
-    for (int j0 = chunk * step; j0 < n; j0 += a.chunks * step) {
-        u32x4 x[EACH];
-        int goal[EACH];
+    const int first = chunk * a.chunk, until = a.in_place ? n : first + a.chunk < n ? first + a.chunk : n;
+    for (int j0 = first; j0 < until; j0 += SECTION) {
+        const int count = until - j0 < SECTION ? until - j0 : SECTION;
+        if (j0 > first) __syncthreads();                    // (the last section's places have been read)
 #pragma unroll
-        for (int k = 0; k < EACH; ++k) {
-            const int j = j0 + k * rows + row;
-            const int old = j < n ? kept[j] : -1;
-            goal[k] = old < 0 || (a.in_place && old == j) ? -1 : j;
-            x[k] = u32x4{0, 0, 0, 0};
-            if (goal[k] >= 0) {
-                const int page = table[old >> a.from.page_shift];
-                if (page >= 0 && page < a.from.n_pages)
-                    x[k] = *reinterpret_cast<const u32x4 *>(src + page * a.from.page_stride + (old & a.from.page_mask) * a.from.slot_stride);
+        for (int k = 0; k < SECTION / THREADS; ++k) {
+            const int u = k * THREADS + (int)threadIdx.x, j = j0 + u;
+            if (u < count) {
+                const int old = kept[j];
+                const bool moves = old >= 0 && !(a.in_place && old == j);
+                const int page = moves ? table[old >> a.from.page_shift] : -1, goal = moves ? to_table[j >> a.to.page_shift] : -1;
+                const bool there = page >= 0 && page < a.from.n_pages, room = goal >= 0 && goal < a.to.n_pages;
+                from_at[u] = there ? page * a.from.page_stride + (old & a.from.page_mask) * a.from.slot_stride : -1ll;
+                to_at[u] = room ? goal * a.to.page_stride + (j & a.to.page_mask) * a.to.slot_stride : -1ll;
             }
         }
-        if (a.in_place) {
-            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-            __syncthreads();
-        }
+        __syncthreads();
+        u32x4 x[EACH], y[EACH];
+        auto read = [&](u32x4 (&x)[EACH], int u0) __attribute__((always_inline)) {
 #pragma unroll
-        for (int k = 0; k < EACH; ++k) {
-            if (goal[k] < 0) continue;
-            const int page = to_table[goal[k] >> a.to.page_shift];
-            if (page >= 0 && page < a.to.n_pages)
-                *reinterpret_cast<u32x4 *>(dst + page * a.to.page_stride + (goal[k] & a.to.page_mask) * a.to.slot_stride) = x[k];
+            for (int k = 0; k < EACH; ++k) {
+                const int u = u0 + k * rows + row;
+                x[k] = u32x4{0, 0, 0, 0};
+                const long long from = u < count ? from_at[u] : -1ll;
+                if (from >= 0) x[k] = *reinterpret_cast<const u32x4 *>(src + from);
+            }
+        };
+        read(x, 0);
+        for (int u0 = 0; u0 < count; u0 += step) {
+            if (a.in_place) {
+                // every thread has what it read
+#pragma unroll
+                for (int k = 0; k < EACH; ++k) asm volatile("" : "+v"(x[k]));
+                asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+                __syncthreads();
+            }
+            read(y, u0 + step);
+#pragma unroll
+            for (int k = 0; k < EACH; ++k) {
+                const int u = u0 + k * rows + row;
+                const long long to = u < count ? to_at[u] : -1ll;
+                if (to >= 0) *reinterpret_cast<u32x4 *>(dst + to) = x[k];
+            }
+#pragma unroll
+            for (int k = 0; k < EACH; ++k) x[k] = y[k];
         }
     }
 }
@@ -299,18 +364,33 @@ peqa_status peqa_cache_evict(const peqa_kv_cache *C, const peqa_kv_cache *to, in
     a.in_place = in_place;
     a.row_bytes = C->head_dim * (C->dtype == PEQA_CACHE_FP8 ? 1 : 2);
     const int heads = n * C->kv_heads, most = max_len < keep ? max_len : keep;
-    a.splits = a.row_bytes >= 256 && heads < peqa::PLAN_UNITS ? a.row_bytes / 128 : 1;
-    const int step = peqa::EACH * (peqa::MOVE_THREADS * 16 * a.splits / a.row_bytes);
-    a.chunks = in_place ? 1 : (most + step - 1) / step;
-    if (a.chunks < 1) a.chunks = 1;
+    // Few heads: large workgroups, each with 128 or 64 bytes of the positions.
+    const bool few = heads < peqa::PLAN_UNITS;
+    const int piece = heads <= 32 ? 64 : 128;
+    a.splits = few && a.row_bytes > piece ? a.row_bytes / piece : 1;
+    const int threads = few ? 1024 : 256, step = peqa::each_of(threads) * (threads * 16 * a.splits / a.row_bytes);
+    a.chunk = most;
+    a.chunks = 1;
+    if (!in_place) {
+        // a step each, or, of many heads, up to a section
+        long long chunk = (long long)most * heads * 2 * a.splits / (8 * peqa::PLAN_UNITS) / step * step;
+        chunk = chunk < step ? step : chunk > peqa::SECTION ? peqa::SECTION : chunk;
+        a.chunk = (int)chunk;
+        a.chunks = (int)((most + chunk - 1) / chunk);
+        if (a.chunks < 1) a.chunks = 1;
+    }
     hipStream_t s = static_cast<hipStream_t>(stream);
     peqa::trace_before(peqa::KID_EVICT_SELECT, s);
-    hipLaunchKernelGGL(peqa::evict_select_kernel, dim3((unsigned)heads), dim3(peqa::SELECT_THREADS), 0, s, a);
+    // (512 and 1024 threads, us: 16 x 32 heads of up to 2048 positions 8.5 and 12.6, 512 of 300 5.8 and 11.7;  8 of 30000 77 and 58 with a weight of a
+    // thread in flight)
+    const bool many = max_len > 4096;
+    hipLaunchKernelGGL((many ? peqa::evict_select_kernel<1024> : peqa::evict_select_kernel<512>), dim3((unsigned)heads), dim3(many ? 1024 : 512), 0, s, a);
     peqa::trace_after(peqa::KID_EVICT_SELECT, s);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return dev_status(e);
     peqa::trace_before(peqa::KID_EVICT_MOVE, s);
-    hipLaunchKernelGGL(peqa::evict_move_kernel, dim3((unsigned)heads * 2u * (unsigned)a.splits * (unsigned)a.chunks), dim3(peqa::MOVE_THREADS), 0, s, a);
+    auto move = few ? peqa::evict_move_kernel<1024> : peqa::evict_move_kernel<256>;
+    hipLaunchKernelGGL(move, dim3((unsigned)heads * 2u * (unsigned)a.splits * (unsigned)a.chunks), dim3((unsigned)threads), 0, s, a);
     peqa::trace_after(peqa::KID_EVICT_MOVE, s);
     return dev_status(hipGetLastError());
 }
