@@ -478,7 +478,10 @@ __device__ __forceinline__ void attend_columns(const SharedArgs &a, const Item &
     constexpr int QK = D / 32, W = D / 16, KB = FP8 ? D / 64 : D / 32, VR = FP8 ? W / 4 : W / 2, EL = FP8 ? 1 : 2;
     constexpr int SUB = 2, STEP = TILE * SUB;         // tiles of a stage
     constexpr int FRAGS = 2 * QK + W;                 // operands of a tile: of the keys, then of the values
-    constexpr int VH = VR > 1 ? VR / 2 : 1, WH = VH * (FP8 ? 4 : 2);      // registers, and elements, of a value that a wave turns
+    // Registers, and neighbouring elements, of a value that a lane of a wave turns; waves for it, each with a half of the elements (whole lines of
+    // memory: 150 us -> 136 of 65537 positions, 8 key heads, 256 columns, where both waves had 8 bytes of every 16).  Operand e of the values has
+    // element e / WH * D / HALVES + WH * row + e % WH.
+    constexpr int VH = VR > 1 ? VR / 2 : 1, WH = VH * (FP8 ? 4 : 2), HALVES = W / WH;
     const CacheArgs &C = a.cache;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int c = lane & 15, g = lane >> 4;
@@ -487,7 +490,7 @@ __device__ __forceinline__ void attend_columns(const SharedArgs &a, const Item &
     const float scale = scale_of<FP8>(a, it.kv_head, turn);
     const bool idle = !KEYS && VR == 1 && (wave & 1);
     const int sub = wave >> 1 & 1, half = wave & 1;   // tile of a stage; which keys, or elements, of it
-    const uint8_t *base = static_cast<const uint8_t *>(KEYS ? C.k : C.v) + it.kv_head * C.head_stride * EL + (KEYS ? 16 * g : (W * c + (idle ? 0 : WH * half)) * EL);
+    const uint8_t *base = static_cast<const uint8_t *>(KEYS ? C.k : C.v) + it.kv_head * C.head_stride * EL + (KEYS ? 16 * g : (WH * c + (idle ? 0 : half * (D / HALVES))) * EL);
     // This wave's tile of a stage; past the last one, that again (as many loads in every stage: what is waited for is counted).
     auto tile_at = [&](int t0) __attribute__((always_inline)) {
         const int t = t0 + TILE * sub, most = it.begin + ((last - it.begin) & ~(TILE - 1));
@@ -685,26 +688,37 @@ __device__ __forceinline__ void attend_columns(const SharedArgs &a, const Item &
         }
     }
     add_weighted<FP8, W>(vt, w, acc[HB - 1]);
+    // A block's sums through the wave's part of LDS, so that whole rows are stored (16 bytes a lane, each of another row: 11 us of the 24 that 128
+    // positions take, of 256 workgroups; pieces of a row change places by its column's last bits, for the banks).
     const float v_scale = FP8 && C.v_scale ? C.v_scale[it.kv_head] : 1.f;
+    constexpr int PIECES = D / 4;                     // of 16 bytes, of a column
+    f32x4 *own = reinterpret_cast<f32x4 *>(lds) + wave * 16 * PIECES;
+    __syncthreads();                                  // (the last operands have been read)
 #pragma unroll
     for (int b = 0; b < HB; ++b) {
+        const int column0 = 16 * (wave * HB + b);
         l[b] = across_groups(l[b], [](float x, float y) { return x + y; });
-        const int column = 16 * (wave * HB + b) + c;
-        if (column >= it.n) continue;
-        const size_t place = (size_t)it.slot + column;
-        if (g == 0) {
-            a.part_ml[2 * place] = m[b];
-            a.part_ml[2 * place + 1] = l[b];
+        if (g == 0 && column0 + c < it.n) {
+            a.part_ml[2 * ((size_t)it.slot + column0 + c)] = m[b];
+            a.part_ml[2 * ((size_t)it.slot + column0 + c) + 1] = l[b];
         }
 #pragma unroll
-        for (int r = 0; r < 4; ++r)
+        for (int h = 0; h < HALVES; ++h)
 #pragma unroll
-            for (int e = 0; e < W; e += 4) {
+            for (int k = 0; k < WH; ++k) {                     // four elements: of one row of the operand, or of two neighbouring ones
                 f32x4 x;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) x[i] = acc[b][e + i][r] * v_scale;
-                *reinterpret_cast<f32x4 *>(a.part + place * D + W * (4 * g + r) + e) = x;
+                for (int i = 0; i < 4; ++i) x[i] = acc[b][WH * h + i % WH][k * 4 / WH + i / WH] * v_scale;
+                own[c * PIECES + ((PIECES / HALVES * h + WH * g + k) ^ (c & 7))] = x;
             }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll
+        for (int k = 0; k < 16 * PIECES / 64; ++k) {
+            const int u = 64 * k + lane, column = u / PIECES, piece = u % PIECES;
+            const f32x4 x = own[column * PIECES + (piece ^ (column & 7))];
+            if (column0 + column < it.n) *reinterpret_cast<f32x4 *>(a.part + ((size_t)it.slot + column0 + column) * D + 4 * piece) = x;
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     }
 }
 
@@ -880,7 +894,9 @@ SharedPlan shared_plan(const peqa_kv_cache *C, int rows, int heads, int max_len,
         chunk = per_workgroup(units * shared, PLAN_UNITS);
         own_chunk = per_workgroup(items * own, 2 * PLAN_UNITS);
     } else {
-        chunk = own_chunk = per_workgroup(units * shared + items * own, PLAN_UNITS * wgs_per_unit(C->head_dim, p.hb));
+        // (rows' own positions are half of the longest's on average, and cut finer: 40 rows x 8 heads, 4096 shared and up to 2000 own 47.4 -> 41.8 us)
+        chunk = per_workgroup(units * shared + items * own / 2, PLAN_UNITS * wgs_per_unit(C->head_dim, p.hb));
+        own_chunk = chunk / 2 > UNIT ? chunk / 2 : UNIT;
     }
     p.chunks = (int)((shared + chunk - 1) / chunk);
     p.chunk = p.chunks > 0 ? (int)(((shared + p.chunks - 1) / p.chunks + TILE - 1) / TILE * TILE) : TILE;
