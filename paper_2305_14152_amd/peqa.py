@@ -556,23 +556,29 @@ def norm_rope_append(cache, q, k, v, pos, cos, sin, q_weight, k_weight, eps, q_o
         raise PeqaError(status, "peqa_norm_rope_append")
 
 
-def _side(x, shape):
-    """(pointer, row stride) of queries, keys or their gradients of this shape."""
-    assert x.shape == shape, "tensors of the same shape"
+def _sides(tensors, shape):
+    """Pointers and row strides, after one another, of queries, keys or their gradients, all of this shape."""
     T, heads, dim = shape
-    p, s = _rows(x, heads, dim)
-    return p, (s if T > 1 else heads * dim)    # (a single row may have any stride)
+    found = []
+    for x in tensors:
+        s0, s1, s2 = x.stride()
+        assert x.shape == shape and s2 == 1 and (s1 == dim or heads == 1) and _kind[x.dtype] in _BF16, _ROWS
+        found += x.data_ptr(), (s0 if T > 1 else heads * dim)    # (a single row may have any stride)
+    return found
 
 
 def norm_rope(q, k, pos, cos, sin, q_weight, k_weight, eps, q_out, k_out, interleaved=False, stream=None):
     """q, q_out [T, heads, head_dim], k, k_out [T, kv_heads, head_dim], pos [T] int32, cos, sin [positions, rot / 2] fp32 or None (no
     rotation), q_weight, k_weight [head_dim] fp32 or None (ones)."""
-    T, heads, dim = q.shape
-    assert k.dim() == 3 and k.shape[0] == T and k.shape[2] == dim, "q [T, heads, head_dim] and k [T, kv_heads, head_dim]"
+    T, heads, dim = q_shape = q.shape
+    k_shape = k.shape
+    assert len(k_shape) == 3 and k_shape[0] == T and k_shape[2] == dim, "q [T, heads, head_dim] and k [T, kv_heads, head_dim]"
+    kv_heads = k_shape[1]
     n_pos, rot = _angles(cos, sin)
+    qp, qs, qo, qos = _sides((q, q_out), q_shape)
+    kp, ks, ko, kos = _sides((k, k_out), k_shape)
     status = (_lib or lib()).peqa_norm_rope(T, _index(pos, T), _floats(cos), _floats(sin), n_pos, rot, interleaved, _floats(q_weight, dim),
-                                            _floats(k_weight, dim), eps, dim, heads, k.shape[1], *_side(q, q.shape), *_side(k, k.shape),
-                                            *_side(q_out, q.shape), *_side(k_out, k.shape), _stream(stream))
+                                            _floats(k_weight, dim), eps, dim, heads, kv_heads, qp, qs, kp, ks, qo, qos, ko, kos, _stream(stream))
     if status:
         raise PeqaError(status, "peqa_norm_rope")
 
@@ -585,12 +591,15 @@ def norm_rope_bwd(q, k, pos, cos, sin, q_weight, k_weight, eps, d_q_out, d_k_out
                   interleaved=False, stream=None):
     """The inputs of norm_rope, the gradients of its outputs, and those that it gives: dq as q, dk as k, d_q_weight, d_k_weight [head_dim] fp32
     or None."""
-    T, heads, dim = q.shape
-    assert k.dim() == 3 and k.shape[0] == T and k.shape[2] == dim, "q [T, heads, head_dim] and k [T, kv_heads, head_dim]"
+    T, heads, dim = q_shape = q.shape
+    k_shape = k.shape
+    assert len(k_shape) == 3 and k_shape[0] == T and k_shape[2] == dim, "q [T, heads, head_dim] and k [T, kv_heads, head_dim]"
+    kv_heads = k_shape[1]
     n_pos, rot = _angles(cos, sin)
+    qp, qs, gq, gqs, dqp, dqs = _sides((q, d_q_out, dq), q_shape)
+    kp, ks, gk, gks, dkp, dks = _sides((k, d_k_out, dk), k_shape)
     status = (_lib or lib()).peqa_norm_rope_bwd(T, _index(pos, T), _floats(cos), _floats(sin), n_pos, rot, interleaved, _floats(q_weight, dim),
-                                                _floats(k_weight, dim), eps, dim, heads, k.shape[1], *_side(q, q.shape), *_side(k, k.shape),
-                                                *_side(d_q_out, q.shape), *_side(d_k_out, k.shape), *_side(dq, q.shape), *_side(dk, k.shape),
+                                                _floats(k_weight, dim), eps, dim, heads, kv_heads, qp, qs, kp, ks, gq, gqs, gk, gks, dqp, dqs, dkp, dks,
                                                 _floats(d_q_weight, dim), _floats(d_k_weight, dim), _room(workspace, workspace_bytes_),
                                                 workspace_bytes_, _stream(stream))
     if status:
