@@ -507,8 +507,8 @@ peqa_status peqa_paged_attention(const peqa_kv_cache *C, int32_t rows, int32_t h
  *   max_len: the host's bound of lens, shared positions included;  shared, max_len at most n_blocks * page_size (PEQA_ERR_SHAPE)
  *   prefix: 0 .. n_seqs - 1;  the other arguments as in peqa_paged_attention
  *   workspace: peqa_shared_attention_workspace_bytes(C, rows, heads, max_len, shared).
- * Products and sums are fp32; weights are rounded to two bf16 parts (16 bits) against bf16 values, to fp16 (11 bits; of weights under 2^-28
- * of the row's largest to 2^-39 of it) against 8-bit ones.  The same call gives the same bits.
+ * Products and sums are fp32; weights are rounded to two bf16 parts (16 bits) against bf16 values, to fp16 (11 bits; of weights under 2^-20
+ * of the row's largest to 2^-31 of it) against 8-bit ones.  The same call gives the same bits.
  */
 size_t peqa_shared_attention_workspace_bytes(const peqa_kv_cache *C, int32_t rows, int32_t heads, int32_t max_len, int32_t shared);
 peqa_status peqa_shared_attention(const peqa_kv_cache *C, int32_t rows, int32_t heads, const uint16_t *q, int64_t q_stride,
@@ -546,9 +546,10 @@ peqa_status peqa_paged_attention_weights(const peqa_kv_cache *C, int32_t rows, i
  *   any page size; its pages of these places are none that C's sequences have.  NULL, or one with C's own pools and table: in place.  In
  *   place a sequence's pages are its own: what another sequence shares with it would change.
  *   lens [n] int32, cut to max_len (as in the attention);  1 <= keep,  0 <= sinks, recent,  sinks + recent <= keep (PEQA_ERR_PARAM)
- *   weights, weights_out as in peqa_paged_attention_weights; places behind what stays, up to max_len, become 0
+ *   weights, weights_out as in peqa_paged_attention_weights; places behind what stays, up to max_len, become 0 (those of
+ *   a sequence without positions are left as they are)
  *   kept [n, kv_heads, keep] int32 out or NULL: the position that each place's was, -1 behind what stays
- *   new_lens [n] int32 out or NULL: min(lens[i], keep); not lens itself (the layers of a model have the same lens)
+ *   new_lens [n] int32 out or NULL: min(lens[i], keep); not lens itself, nor in part (the layers of a model have the same lens)
  * A sequence outside [0, n_seqs) has none; one that an earlier entry has is left out (kept -1, that entry's length).  What lies on a page that is
  * not there arrives as zeros; nothing is stored to one.  Weights are compared as they are: every choice is exact.
  *   workspace: peqa_cache_evict_workspace_bytes(C, n, max_len, keep).

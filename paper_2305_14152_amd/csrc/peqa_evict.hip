@@ -280,10 +280,23 @@ __global__ __launch_bounds__(THREADS) void evict_move_kernel(EvictArgs a)
 
 struct EvictPlan {
     size_t kept_bytes, moved_bytes;
+    bool few;                              // heads: large workgroups of the move, each with `splits` of a position's bytes
+    int splits, chunks, chunk;             // of the move, to another cache (in place a head is one chunk)
 };
-EvictPlan evict_plan(const peqa_kv_cache *C, int n, int keep)
+EvictPlan evict_plan(const peqa_kv_cache *C, int n, int max_len, int keep)
 {
     EvictPlan p{};
+    const int heads = n * C->kv_heads, most = max_len < keep ? max_len : keep;
+    const int row_bytes = C->head_dim * (C->dtype == PEQA_CACHE_FP8 ? 1 : 2), piece = heads <= 32 ? 64 : 128;
+    p.few = heads < PLAN_UNITS;
+    p.splits = p.few && row_bytes > piece ? row_bytes / piece : 1;
+    // a step each, or, of many heads, up to a section
+    const int threads = p.few ? 1024 : 256, step = each_of(threads) * (threads * 16 * p.splits / row_bytes);
+    long long chunk = (long long)most * heads * 2 * p.splits / (8 * PLAN_UNITS) / step * step;
+    chunk = chunk < step ? step : chunk > SECTION ? SECTION : chunk;
+    p.chunk = (int)chunk;
+    p.chunks = (int)((most + chunk - 1) / chunk);
+    if (p.chunks < 1) p.chunks = 1;
     p.kept_bytes = round256((size_t)n * (size_t)C->kv_heads * (size_t)keep * sizeof(int32_t));
     p.moved_bytes = round256((size_t)n * sizeof(int32_t));
     return p;
@@ -295,7 +308,9 @@ peqa_status check_evict(const peqa_kv_cache *C, int32_t n, int32_t max_len, int3
     if (st != PEQA_OK) return st;
     if (n < 1 || max_len < 0 || (int64_t)max_len > (int64_t)C->n_blocks * C->page_size) return PEQA_ERR_SHAPE;
     if (keep < 1 || keep > (1 << 30)) return PEQA_ERR_PARAM;
-    if ((int64_t)n * C->kv_heads > (1 << 20)) return PEQA_ERR_SHAPE;          // workgroups of a launch
+    if ((int64_t)n * C->kv_heads > (1 << 20)) return PEQA_ERR_SHAPE;          // workgroups of a launch, here and of the move
+    const EvictPlan p = evict_plan(C, n, max_len, keep);
+    if ((int64_t)n * C->kv_heads * 2 * p.splits * p.chunks > (1 << 23)) return PEQA_ERR_SHAPE;
     return PEQA_OK;
 }
 
@@ -318,7 +333,7 @@ extern "C" {
 size_t peqa_cache_evict_workspace_bytes(const peqa_kv_cache *C, int32_t n, int32_t max_len, int32_t keep)
 {
     if (peqa::check_evict(C, n, max_len, keep) != PEQA_OK) return 0;
-    const peqa::EvictPlan p = peqa::evict_plan(C, n, keep);
+    const peqa::EvictPlan p = peqa::evict_plan(C, n, max_len, keep);
     return p.kept_bytes + p.moved_bytes;
 }
 
@@ -343,12 +358,13 @@ peqa_status peqa_cache_evict(const peqa_kv_cache *C, const peqa_kv_cache *to, in
     if (!lens || !weights || !weights_out) return PEQA_ERR_NULL;
     if (!seq && n > C->n_seqs) return PEQA_ERR_SHAPE;
     if (sinks < 0 || recent < 0 || (int64_t)sinks + recent > keep) return PEQA_ERR_PARAM;
-    if (new_lens == lens) return PEQA_ERR_PARAM;           // (the heads' workgroups read it)
     if (weights_head_stride < max_len || weights_seq_stride < max_len) return PEQA_ERR_SHAPE;
     if ((reinterpret_cast<uintptr_t>(lens) | reinterpret_cast<uintptr_t>(seq) | reinterpret_cast<uintptr_t>(weights) |
          reinterpret_cast<uintptr_t>(weights_out) | reinterpret_cast<uintptr_t>(kept) | reinterpret_cast<uintptr_t>(new_lens)) & 3)
         return PEQA_ERR_ALIGN;
-    const peqa::EvictPlan p = peqa::evict_plan(C, n, keep);
+    const intptr_t behind = (intptr_t)new_lens - (intptr_t)lens;
+    if (new_lens && behind < n * 4ll && -behind < n * 4ll) return PEQA_ERR_PARAM;             // (the heads' workgroups read lens)
+    const peqa::EvictPlan p = peqa::evict_plan(C, n, max_len, keep);
     if (!workspace || workspace_bytes < p.kept_bytes + p.moved_bytes) return PEQA_ERR_WORKSPACE;
     if (!aligned16(workspace)) return PEQA_ERR_ALIGN;
     char *w = static_cast<char *>(workspace);
@@ -363,22 +379,10 @@ peqa_status peqa_cache_evict(const peqa_kv_cache *C, const peqa_kv_cache *to, in
     a.n = n; a.max_len = max_len; a.keep = keep; a.sinks = sinks; a.recent = recent;
     a.in_place = in_place;
     a.row_bytes = C->head_dim * (C->dtype == PEQA_CACHE_FP8 ? 1 : 2);
-    const int heads = n * C->kv_heads, most = max_len < keep ? max_len : keep;
-    // Few heads: large workgroups, each with 128 or 64 bytes of the positions.
-    const bool few = heads < peqa::PLAN_UNITS;
-    const int piece = heads <= 32 ? 64 : 128;
-    a.splits = few && a.row_bytes > piece ? a.row_bytes / piece : 1;
-    const int threads = few ? 1024 : 256, step = peqa::each_of(threads) * (threads * 16 * a.splits / a.row_bytes);
-    a.chunk = most;
-    a.chunks = 1;
-    if (!in_place) {
-        // a step each, or, of many heads, up to a section
-        long long chunk = (long long)most * heads * 2 * a.splits / (8 * peqa::PLAN_UNITS) / step * step;
-        chunk = chunk < step ? step : chunk > peqa::SECTION ? peqa::SECTION : chunk;
-        a.chunk = (int)chunk;
-        a.chunks = (int)((most + chunk - 1) / chunk);
-        if (a.chunks < 1) a.chunks = 1;
-    }
+    const int heads = n * C->kv_heads;
+    a.splits = p.splits;
+    a.chunk = in_place ? max_len : p.chunk;
+    a.chunks = in_place ? 1 : p.chunks;
     hipStream_t s = static_cast<hipStream_t>(stream);
     peqa::trace_before(peqa::KID_EVICT_SELECT, s);
     // (512 and 1024 threads, us: 16 x 32 heads of up to 2048 positions 8.5 and 12.6, 512 of 300 5.8 and 11.7;  8 of 30000 77 and 58 with a weight of a
@@ -389,8 +393,8 @@ peqa_status peqa_cache_evict(const peqa_kv_cache *C, const peqa_kv_cache *to, in
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return dev_status(e);
     peqa::trace_before(peqa::KID_EVICT_MOVE, s);
-    auto move = few ? peqa::evict_move_kernel<1024> : peqa::evict_move_kernel<256>;
-    hipLaunchKernelGGL(move, dim3((unsigned)heads * 2u * (unsigned)a.splits * (unsigned)a.chunks), dim3((unsigned)threads), 0, s, a);
+    auto move = p.few ? peqa::evict_move_kernel<1024> : peqa::evict_move_kernel<256>;
+    hipLaunchKernelGGL(move, dim3((unsigned)heads * 2u * (unsigned)a.splits * (unsigned)a.chunks), dim3(p.few ? 1024 : 256), 0, s, a);
     peqa::trace_after(peqa::KID_EVICT_MOVE, s);
     return dev_status(hipGetLastError());
 }

@@ -235,7 +235,8 @@ template <bool FP8> __device__ __forceinline__ float scale_of(const SharedArgs &
 {
     const float scale = a.scale * (FP8 && a.cache.k_scale ? a.cache.k_scale[kv_head] : 1.f);
     turn = scale < 0.f ? 0x80008000u : 0u;
-    return fmaxf(fabsf(scale), 1e-36f);
+    const float size = fabsf(scale);
+    return size < 1e-36f ? 1e-36f : size;                      // (NaN stays)
 }
 
 // A piece of the query of a column: 16 bytes of step s of the scores' product, whose elements the keys' pieces decide.

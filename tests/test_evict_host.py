@@ -57,6 +57,12 @@ def test_eviction_refusals_and_sizes(peqa):
     assert need >= 4 * (3 * 2 * 30 + 3) and call(room=need - 1) == peqa.PEQA_ERR_WORKSPACE
     assert peqa.cache_evict_workspace_bytes(C, 0, 64, 30) == 0 and peqa.cache_evict_workspace_bytes(C, 3, 65, 30) == 0
     assert peqa.cache_evict_workspace_bytes(C, 3, 64, 0) == 0
+    # lengths that the call would read and write; more workgroups than a launch has
+    for behind in (4, -8):
+        assert call(new=GOOD + behind) == peqa.PEQA_ERR_PARAM
+    long = cache(peqa, n_blocks=1 << 16, table_stride=1 << 16, n_seqs=1 << 20, kv_heads=1, head_stride=0)
+    many = dict(C=long, n=1 << 20, seq=GOOD, most=1 << 20, hs=1 << 20, ss=1 << 20, keep=1 << 20, kept=None, new=None, room=1 << 50)
+    assert call(**many) == peqa.PEQA_ERR_SHAPE and peqa.cache_evict_workspace_bytes(long, 1 << 20, 1 << 20, 1 << 20) == 0
 
 
 def test_binding(peqa):

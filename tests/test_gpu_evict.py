@@ -267,3 +267,51 @@ def test_evict_replayed(env):
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(got, want)), i
         assert all(torch.equal(a, b) for a, b in zip([weights, *cache.tensors[:2]], ends)), i
+
+
+@pytest.mark.parametrize("fp8", [False, True])
+def test_far_places(env, fp8):
+    """Pages past 2^31 elements of a pool: appended to, attended to and evicted as in a small pool, on two streams at once."""
+    torch, peqa = env
+    gen = torch.Generator().manual_seed(12)
+    page, dim, kv, heads, keep = 256, 128, 2, 4, 200
+    dtype, bits = (torch.float8_e4m3fn, torch.uint8) if fp8 else (torch.bfloat16, torch.int16)
+    near, far = [0, 1, 2, 3], [1, 39990, 39999, 2]
+    pools = [[torch.zeros((n, kv, page, dim), dtype=dtype, device="cuda") for _ in range(4)] for n in (4, 40000)]
+    for which in range(2):
+        data = torch.randn((4, kv, page, dim), generator=gen).to(dtype).cuda()
+        pools[0][which].view(bits).copy_(data.view(bits))
+        for a, b in zip(near, far):
+            pools[1][which].view(bits)[b] = data.view(bits)[a]
+    scales = [torch.full((kv,), 0.5, device="cuda") for _ in range(2)] if fp8 else [None, None]
+    lens = torch.tensor([400, 511], dtype=torch.int32, device="cuda")
+    q, k, v = (torch.randn((2, n, dim), generator=gen).to(torch.bfloat16).cuda() for n in (heads, kv, kv))
+    weights = torch.rand((2, kv, 512), generator=gen).cuda()
+    start, results = torch.cuda.Event(), []
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    caches = []
+    for pool, pages in zip(pools, (near, far)):
+        table = torch.tensor(pages, dtype=torch.int32, device="cuda").view(2, 2)
+        caches.append([peqa.kv_cache(pool[i], pool[i + 1], table, *scales) for i in (0, 2)])
+    torch.cuda.synchronize()
+    start.record()
+    for stream, (cache, to) in zip(streams, caches):
+        with torch.cuda.stream(stream):
+            stream.wait_event(start)
+            qo, out, w = torch.empty_like(q), torch.empty_like(q), weights.clone()
+            kept, left = torch.empty((2, kv, keep), dtype=torch.int32, device="cuda"), torch.empty(2, dtype=torch.int32, device="cuda")
+            peqa.norm_rope_append(cache, q, k, v, lens, None, None, None, None, 1e-6, qo, place=lens)
+            r1, r2 = peqa.paged_attention_weights_workspace_bytes(cache, heads, 2, 512), peqa.cache_evict_workspace_bytes(cache, 2, 512, keep)
+            w1, w2 = (torch.empty(n, dtype=torch.uint8, device="cuda") for n in (r1, r2))
+            peqa.paged_attention_weights(cache, qo, lens, 512, 0.1, out, w, w, w1, r1)
+            elsewhere = torch.zeros_like(w)
+            peqa.cache_evict(cache, lens, 512, w, elsewhere, keep, 3, 20, kept, left, w2, r2, to=to)
+            peqa.cache_evict(cache, lens, 512, w, w, keep, 3, 20, kept, left, w2, r2)
+            results.append([qo, out, w, elsewhere, kept, left])
+    torch.cuda.synchronize()
+    for a, b in zip(*results):
+        assert torch.equal(a, b)
+    assert torch.equal(results[0][2], results[0][3]) and results[0][5].tolist() == [keep] * 2
+    for small, big in zip(*pools):
+        for a, b in zip(near, far):
+            assert torch.equal(small.view(bits)[a], big.view(bits)[b])
