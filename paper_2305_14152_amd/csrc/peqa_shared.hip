@@ -32,7 +32,7 @@ struct SharedArgs {
     int max_len, prefix, shared;
     int columns, tiles;        // of the shared positions' workgroups: columns of one, and how many have all
     int chunk, chunks;         // positions of one, and how many have the shared ones
-    int prefix_wgs;
+    int prefix_wgs, own_items;
     int own_chunk, own_splits; // positions of a row's own at least, and workgroups of a row and a block of heads
     int own_blocks, own_columns;   // blocks of a key head's heads, and heads in one
 };
@@ -282,7 +282,7 @@ template <int D> struct Shape {
 
 // All columns in every wave, which take the tiles in turn.
 template <int D, bool FP8, int HB, int WAVES>
-__device__ __forceinline__ void attend_item(const SharedArgs &a, const Item &it, u32x4 *lds_q, float (*wave_m)[16], float (*wave_l)[16],
+__device__ __forceinline__ void attend_item(const SharedArgs &a, const Item &it, int tid, u32x4 *lds_q, float (*wave_m)[16], float (*wave_l)[16],
                                             float (*joined)[16][Shape<D>::DS + 4])
 {
     constexpr int STEP = TILE * WAVES;                // positions of a workgroup's step
@@ -295,7 +295,7 @@ __device__ __forceinline__ void attend_item(const SharedArgs &a, const Item &it,
     constexpr bool QUERIES_IN_LDS = HB > 2;
     constexpr bool AHEAD = HB * D < 512 || (FP8 && D <= 128);       // registers for two tiles
     const CacheArgs &C = a.cache;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int c = lane & 15, g = lane >> 4;
     const int slot_bytes = (int)C.slot_stride * EL;
 
@@ -446,7 +446,7 @@ __device__ __forceinline__ void attend_item(const SharedArgs &a, const Item &it,
                     *reinterpret_cast<f32x4 *>(&joined[wave][c][W * (4 * g + r) + e]) = x;
                 }
             __syncthreads();
-            for (int u = threadIdx.x; u < 16 * DS / 4; u += 64 * WAVES) {
+            for (int u = tid; u < 16 * DS / 4; u += 64 * WAVES) {
                 const int col = u / (DS / 4), at = 4 * (u % (DS / 4));
                 if (16 * b + col >= it.n) break;
                 float top = LOWEST, total = 0.f;
@@ -723,8 +723,8 @@ __device__ __forceinline__ void attend_columns(const SharedArgs &a, const Item &
     }
 }
 
-// The item of a workgroup: true, of the shared positions; it.n < 1: none.
-__device__ __forceinline__ bool item_of(const SharedArgs &a, Item &it)
+// The item of a workgroup: true, of the shared positions; it.n < 1: none.  Of rows' own positions a workgroup has EACH items, this is one of them.
+template <int EACH> __device__ __forceinline__ bool item_of(const SharedArgs &a, int of_wg, Item &it)
 {
     const CacheArgs &C = a.cache;
     it.n = 0;
@@ -743,7 +743,8 @@ __device__ __forceinline__ bool item_of(const SharedArgs &a, Item &it)
         it.slot = ((long long)unit * a.tiles + tile) * a.columns;
         return true;
     }
-    const int number = (int)blockIdx.x - a.prefix_wgs, item = number / a.own_splits, split = number - item * a.own_splits;
+    const int number = ((int)blockIdx.x - a.prefix_wgs) * EACH + of_wg, item = number / a.own_splits, split = number - item * a.own_splits;
+    if (number >= a.own_items) return false;
     const int of_row = item / a.own_blocks, block = item - of_row * a.own_blocks, row = of_row / C.kv_heads;
     RowInfo r = row_info(a, row);
     r.len = __builtin_amdgcn_readfirstlane(r.len);
@@ -773,23 +774,34 @@ __global__ __launch_bounds__(256, wgs_per_unit(D, HB)) void shared_kernel(Shared
     __shared__ float wave_m[4][16], wave_l[4][16];
     __shared__ __attribute__((aligned(16))) float joined[4][16][Shape<D>::DS + 4];
     Item it;
-    const bool of_prefix = item_of(a, it);
+    const bool of_prefix = item_of<1>(a, 0, it);
     if (it.n < 1) return;
-    if (of_prefix) attend_item<D, FP8, HB, 4>(a, it, lds_q, wave_m, wave_l, joined);
-    else attend_item<D, FP8, 1, 4>(a, it, lds_q, wave_m, wave_l, joined);
+    if (of_prefix) attend_item<D, FP8, HB, 4>(a, it, threadIdx.x, lds_q, wave_m, wave_l, joined);
+    else attend_item<D, FP8, 1, 4>(a, it, threadIdx.x, lds_q, wave_m, wave_l, joined);
 }
 
-// The shared positions of many columns, 128 HB of a workgroup of eight waves.
+// The shared positions of many columns, 128 HB of a workgroup of eight waves; behind those two items of rows' own positions a workgroup, by four
+// waves each (one by eight: 200 rows x 32 heads of up to 300 own positions 152 us for 144).
 template <int D, bool FP8, int HB>
 __global__ __launch_bounds__(512, 1) void shared_wide_kernel(SharedArgs a)
 {
-    __shared__ u32x4 operands[2 * 2 * (D / 8) * 64];
+    __shared__ union {
+        u32x4 operands[2 * 2 * (D / 8) * 64];
+        float joined[2][4][16][D + 4];
+    } lds;
     __shared__ uint32_t there[2][2];
+    __shared__ float wave_m[2][4][16], wave_l[2][4][16];
     Item it;
-    item_of(a, it);
+    const int half = __builtin_amdgcn_readfirstlane(threadIdx.x >> 8);
+    if (!item_of<2>(a, half, it)) {
+        // (one barrier in either)
+        if (it.n > 0) attend_item<D, FP8, 1, 4>(a, it, threadIdx.x & 255, nullptr, wave_m[half], wave_l[half], lds.joined[half]);
+        else __syncthreads();
+        return;
+    }
     if (it.n < 1) return;
-    if (threadIdx.x < 256) attend_columns<D, FP8, HB, true>(a, it, operands, there);
-    else attend_columns<D, FP8, HB, false>(a, it, operands, there);
+    if (half == 0) attend_columns<D, FP8, HB, true>(a, it, lds.operands, there);
+    else attend_columns<D, FP8, HB, false>(a, it, lds.operands, there);
 }
 
 // Joins a column's parts: a workgroup per row and head.  A group of D / 4 lanes has some of the parts, 16 bytes of a part's sums a lane, four
@@ -861,7 +873,7 @@ template <int D> __global__ __launch_bounds__(256) void shared_join_kernel(Share
 struct SharedPlan {
     bool wide;
     int hb, columns, tiles, chunk, chunks, own_chunk, own_splits, own_blocks, own_columns;
-    long long prefix_wgs, own_wgs;
+    long long prefix_wgs, own_items;
     size_t part_bytes, ml_bytes;
 };
 
@@ -885,17 +897,20 @@ SharedPlan shared_plan(const peqa_kv_cache *C, int rows, int heads, int max_len,
     p.own_blocks = (group + p.own_columns - 1) / p.own_columns;
     const long long own = max_len > shared ? max_len - shared + TILE - 1 : 0;
     const long long items = (long long)rows * C->kv_heads * p.own_blocks, units = (long long)C->kv_heads * p.tiles;
-    // all that there is to walk, over as many workgroups as have room at once, 128 positions at least; with many columns by a launch each
+    // all that there is to walk, over as many workgroups as have room at once, 128 positions at least; rows' own positions are half of the longest's on average
     auto per_workgroup = [](long long all, int wgs) {
         const long long chunk = ((all + wgs - 1) / wgs + UNIT - 1) / UNIT * UNIT;
         return chunk < UNIT ? (long long)UNIT : chunk;
     };
     long long chunk, own_chunk;
     if (p.wide) {
-        chunk = per_workgroup(units * shared, PLAN_UNITS);
+        // Many columns of a position are two of a row's own: then the units that the shared positions leave read the rows' own meanwhile, matrix
+        // instructions beside loads (64 rows x 8 key heads x 8, 8192 shared and up to 1024 own: 65 us, 79 with the shared ones on all units; with three
+        // or four for two 80, rows' own cut finer 67 to 72).
+        chunk = per_workgroup(units * shared + items * own / 4, PLAN_UNITS);
         own_chunk = per_workgroup(items * own, 2 * PLAN_UNITS);
     } else {
-        // (rows' own positions are half of the longest's on average, and cut finer: 40 rows x 8 heads, 4096 shared and up to 2000 own 47.4 -> 41.8 us)
+        // (rows' own cut finer: 40 rows x 8 heads, 4096 shared and up to 2000 own 47.4 -> 41.8 us)
         chunk = per_workgroup(units * shared + items * own / 2, PLAN_UNITS * wgs_per_unit(C->head_dim, p.hb));
         own_chunk = chunk / 2 > UNIT ? chunk / 2 : UNIT;
     }
@@ -906,8 +921,8 @@ SharedPlan shared_plan(const peqa_kv_cache *C, int rows, int heads, int max_len,
     if (p.own_splits < 1) p.own_splits = 1;                    // (rows that end among the shared positions)
     p.own_chunk = UNIT;
     p.prefix_wgs = ((long long)p.chunks * C->kv_heads + 7) / 8 * 8 * p.tiles;
-    p.own_wgs = items * p.own_splits;
-    const size_t slots = (size_t)p.chunks * (size_t)units * (size_t)p.columns + (size_t)p.own_wgs * (size_t)p.own_columns;
+    p.own_items = items * p.own_splits;
+    const size_t slots = (size_t)p.chunks * (size_t)units * (size_t)p.columns + (size_t)p.own_items * (size_t)p.own_columns;
     p.part_bytes = round256(slots * (size_t)C->head_dim * sizeof(float));
     p.ml_bytes = round256(slots * 2 * sizeof(float));
     return p;
@@ -924,16 +939,12 @@ template <int D, bool FP8> hipError_t launch_shared(const SharedArgs &a, const S
     hipError_t e = hipSuccess;
     if constexpr (D <= 128) {
         if (p.wide) {
-            if (p.prefix_wgs > 0) e = run(p.hb == 1 ? shared_wide_kernel<D, FP8, 1> : shared_wide_kernel<D, FP8, 2>, a, p.prefix_wgs, 512);
-            if (e != hipSuccess) return e;
-            SharedArgs own = a;
-            own.prefix_wgs = 0;
-            e = run(shared_kernel<D, FP8, 1>, own, p.own_wgs, 256);
+            e = run(p.hb == 1 ? shared_wide_kernel<D, FP8, 1> : shared_wide_kernel<D, FP8, 2>, a, p.prefix_wgs + (p.own_items + 1) / 2, 512);
         } else if (p.hb == 4) {
-            e = run(shared_kernel<D, FP8, 4>, a, p.prefix_wgs + p.own_wgs, 256);
+            e = run(shared_kernel<D, FP8, 4>, a, p.prefix_wgs + p.own_items, 256);
         }
     }
-    if (!p.wide && p.hb < 4) e = run(p.hb == 1 ? shared_kernel<D, FP8, 1> : shared_kernel<D, FP8, 2>, a, p.prefix_wgs + p.own_wgs, 256);
+    if (!p.wide && p.hb < 4) e = run(p.hb == 1 ? shared_kernel<D, FP8, 1> : shared_kernel<D, FP8, 2>, a, p.prefix_wgs + p.own_items, 256);
     if (e != hipSuccess) return e;
     trace_before(KID_SHARED_JOIN, stream);
     hipLaunchKernelGGL(shared_join_kernel<D>, dim3((unsigned)a.rows * (unsigned)a.heads), dim3(256), 0, stream, a);
@@ -950,7 +961,7 @@ peqa_status check_shared(const peqa_kv_cache *C, int32_t rows, int32_t heads, in
     if (max_len > room || shared > room) return PEQA_ERR_SHAPE;
     if ((int64_t)rows * heads > (1 << 23)) return PEQA_ERR_SHAPE;             // workgroups of a launch
     const SharedPlan p = shared_plan(C, rows, heads, max_len, shared);
-    if (p.prefix_wgs + p.own_wgs > (1 << 23)) return PEQA_ERR_SHAPE;
+    if (p.prefix_wgs + p.own_items > (1 << 23)) return PEQA_ERR_SHAPE;
     return PEQA_OK;
 }
 
@@ -991,7 +1002,7 @@ peqa_status peqa_shared_attention(const peqa_kv_cache *C, int32_t rows, int32_t 
     a.rows = rows; a.heads = heads; a.group = heads / C->kv_heads;
     a.max_len = max_len; a.prefix = prefix; a.shared = shared;
     a.columns = p.columns; a.tiles = p.tiles; a.chunk = p.chunk; a.chunks = p.chunks;
-    a.prefix_wgs = (int)p.prefix_wgs;
+    a.prefix_wgs = (int)p.prefix_wgs; a.own_items = (int)p.own_items;
     a.own_chunk = p.own_chunk; a.own_splits = p.own_splits; a.own_blocks = p.own_blocks; a.own_columns = p.own_columns;
     hipStream_t s = static_cast<hipStream_t>(stream);
     const bool fp8 = C->dtype == PEQA_CACHE_FP8;
