@@ -54,7 +54,9 @@ struct AttendArgs {
     float *part_ml;            // [slots, per_wg, 2] reference (the maximum, or 14 below it; of powers of two) and sum
     ItemParts *parts;          // [rows * items of a row], or [shares]: of the item that ends in a share and began before it
     float *scores;             // [rows, heads, score_stride] of powers of two, for the positions' weights; or null
-    long long q_stride, out_stride, score_stride;
+    const float *weights;      // of an item's positions, where the workgroup that has all of it adds what they were given
+    float *weights_out;        // (null: attend_weights_kernel does)
+    long long q_stride, out_stride, score_stride, weights_seq_stride, weights_head_stride;
     float scale;               // times log2 e
     int rows, heads, group;    // heads per key head
     int max_len, window;
@@ -168,6 +170,24 @@ struct Piece {
     bool first, last, alone;                               // of its segment; alone: the segment is the whole item
 };
 
+// What four positions were given by a head: of those in [lo, end); lse of powers of two.
+__device__ __forceinline__ void add_given(f32x4 &sum, const float *scores, float lse, int pos, int lo, int end)
+{
+    if (lse == -__builtin_inff()) return;                  // (a row without positions)
+    const f32x4 x = *reinterpret_cast<const f32x4 *>(scores + pos);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) sum[k] += pos + k >= lo && pos + k < end ? __builtin_amdgcn_exp2f(x[k] - lse) : 0.f;
+}
+__device__ __forceinline__ void store_given(const float *weights, float *weights_out, f32x4 sum, int pos, int end)
+{
+    if (pos + 4 <= end) {
+        if (weights) sum += *reinterpret_cast<const f32x4 *>(weights + pos);
+        *reinterpret_cast<f32x4 *>(weights_out + pos) = sum;
+    } else {
+        for (int k = 0; k < end - pos; ++k) weights_out[pos + k] = (weights ? weights[pos + k] : 0.f) + sum[k];
+    }
+}
+
 // The sum of lanes c and c + 8 of every 16, in both.
 __device__ __forceinline__ float add_halves(float v)
 {
@@ -204,6 +224,7 @@ __global__ __launch_bounds__(64 * WAVES, wgs_per_unit(D, FP8)) void attend_kerne
     __shared__ int scan[WAVES + 6];
     __shared__ float wave_m[WAVES][HB][16], wave_l[WAVES][HB][16];
     __shared__ __attribute__((aligned(16))) float joined[WAVES][8][DS + 4];
+    __shared__ float head_lse[SCORES ? COLS * HB : 1];
 
     const CacheArgs &C = a.cache;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -562,8 +583,11 @@ __global__ __launch_bounds__(64 * WAVES, wgs_per_unit(D, FP8)) void attend_kerne
                             const float by = any ? v_scale / total : 0.f;
                             uint16_t *o = a.out + cur.row * a.out_stride + (long long)head * D + 128 * s + at;
                             *reinterpret_cast<u32x2 *>(o) = u32x2{pack_bf16x2(x[0] * by, x[1] * by), pack_bf16x2(x[2] * by, x[3] * by)};
-                            if (a.lse && at == 0 && s == 0)
-                                a.lse[(size_t)cur.row * a.heads + head] = any ? (top + __builtin_amdgcn_logf(total)) * LN2 : -__builtin_inff();
+                            if (at == 0 && s == 0) {
+                                const float lse = any ? top + __builtin_amdgcn_logf(total) : -__builtin_inff();
+                                if constexpr (SCORES) head_lse[b * COLS + 8 * half + col] = lse;
+                                if (a.lse) a.lse[(size_t)cur.row * a.heads + head] = lse * LN2;
+                            }
                         } else {
                             const size_t place = (size_t)cur.slot * a.per_wg + b * COLS + 8 * half + col;
                             *reinterpret_cast<f32x4 *>(a.part + place * D + 128 * s + at) = x;
@@ -573,6 +597,20 @@ __global__ __launch_bounds__(64 * WAVES, wgs_per_unit(D, FP8)) void attend_kerne
                             }
                         }
                     }
+                }
+            }
+        }
+        if constexpr (SCORES) {
+            if (a.weights_out) {
+                // (the item, of one piece or several, is this workgroup's only one and has all heads of its key head)
+                __syncthreads();
+                const long long at = cur.seq * a.weights_seq_stride + cur.kv_head * a.weights_head_stride;
+                for (int pos = 4 * tid; pos < cur.end; pos += 256 * WAVES) {
+                    f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+                    if (pos + 4 > cur.lo)
+                        for (int i = 0; i < a.group; ++i)
+                            add_given(sum, a.scores + ((size_t)cur.row * a.heads + (size_t)cur.kv_head * a.group + i) * a.score_stride, head_lse[i], pos, cur.lo, cur.end);
+                    store_given(a.weights ? a.weights + at : nullptr, a.weights_out + at, sum, pos, cur.end);
                 }
             }
         }
@@ -742,8 +780,11 @@ template <bool SCORES> hipError_t launch_attend(const peqa_kv_cache *C, const At
 }
 
 // What the positions were given: weights_out = weights + the sum over a row's heads of a key head, and over the rows of a sequence, of
-// 2^(score - log2 of the sum of powers).  A workgroup has 1024 positions of a key head, four a thread, of the first row with its sequence, and
-// adds the others' after one another, so that no sum depends on an order of workgroups.
+// 2^(score - log2 of the sum of powers), of the scores that the attention left: a score is known long before its row's sum is, and 4 bytes written
+// and read again for a head and a position are less than reading its keys again (where 8 heads share 256 bytes of a key, an eighth).  A workgroup has
+// 1024 positions of a key head, four a thread, of the first row with its sequence, and adds the others' after one another, so that no sum
+// depends on an order of workgroups.  Bound by memory: 32 rows of up to 8192, 64 heads, 8 key heads  10 us for 33 MB of scores, which are
+// still cached in part; the attention that writes them takes 124 us for 109.
 struct WeightArgs {
     const int32_t *lens, *seq;
     const float *scores, *lse, *weights;
@@ -778,11 +819,7 @@ __global__ __launch_bounds__(256) void attend_weights_kernel(WeightArgs a)
         if (pos >= len || pos + 4 <= lo) return;
         for (int i = 0; i < a.group; ++i) {
             const size_t head = (size_t)r * a.heads + (size_t)h * a.group + i;
-            const float lse = a.lse[head] * LOG2E;
-            if (lse == -__builtin_inff()) continue;        // (a row without positions)
-            const f32x4 x = *reinterpret_cast<const f32x4 *>(a.scores + head * a.score_stride + pos);
-#pragma unroll
-            for (int k = 0; k < 4; ++k) sum[k] += pos + k >= lo && pos + k < len ? __builtin_amdgcn_exp2f(x[k] - lse) : 0.f;
+            add_given(sum, a.scores + head * a.score_stride, a.lse[head] * LOG2E, pos, lo, len);
         }
     };
     add_row(row);
@@ -797,13 +834,8 @@ __global__ __launch_bounds__(256) void attend_weights_kernel(WeightArgs a)
         }
     }
     if (pos >= longest) return;
-    const size_t at = (size_t)(seq * a.seq_stride + h * a.head_stride) + pos;
-    if (pos + 4 <= longest) {
-        if (a.weights) sum += *reinterpret_cast<const f32x4 *>(a.weights + at);
-        *reinterpret_cast<f32x4 *>(a.weights_out + at) = sum;
-    } else {
-        for (int k = 0; k < longest - pos; ++k) a.weights_out[at + k] = (a.weights ? a.weights[at + k] : 0.f) + sum[k];
-    }
+    const long long at = seq * a.seq_stride + h * a.head_stride;
+    store_given(a.weights ? a.weights + at : nullptr, a.weights_out + at, sum, pos, longest);
 }
 
 }  // namespace
@@ -997,9 +1029,16 @@ peqa_status peqa_paged_attention_weights(const peqa_kv_cache *C, int32_t rows, i
     if (st != PEQA_OK) return st;
     a.scores = reinterpret_cast<float *>(w + r.parts);
     a.score_stride = r.stride;
+    // An item that one workgroup has is finished there, without a launch of its own (1 row x 32, 1, of 333  10.5 us, 12.4 with; 16 x 32, 1, of 500
+    // 26.1, 28.5;  64 x 8, 8, up to 1000 (8 bits)  24.4, 26.6;  128 x 8, 8, up to 400  35.1, 34.7); rows of one sequence add to the same sums.
+    const bool within = !seq && p.blocks == 1 && p.splits == 1 && p.shares == 0;
+    if (within) {
+        a.weights = weights; a.weights_out = weights_out;
+        a.weights_seq_stride = weights_seq_stride; a.weights_head_stride = weights_head_stride;
+    }
     hipStream_t s = static_cast<hipStream_t>(stream);
     const hipError_t e = peqa::launch_attend<true>(C, a, p, s);
-    if (e != hipSuccess || chunks == 0) return dev_status(e);
+    if (e != hipSuccess || chunks == 0 || within) return dev_status(e);
     peqa::WeightArgs g{};
     g.lens = lens; g.seq = seq; g.scores = a.scores; g.lse = lse; g.weights = weights; g.weights_out = weights_out;
     g.score_stride = r.stride; g.seq_stride = weights_seq_stride; g.head_stride = weights_head_stride;
