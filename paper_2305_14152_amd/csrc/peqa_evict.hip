@@ -280,22 +280,26 @@ __global__ __launch_bounds__(THREADS) void evict_move_kernel(EvictArgs a)
 
 struct EvictPlan {
     size_t kept_bytes, moved_bytes;
-    bool few;                              // heads: large workgroups of the move, each with `splits` of a position's bytes
-    int splits, chunks, chunk;             // of the move, to another cache (in place a head is one chunk)
+    bool few;                              // heads in place: large workgroups of the move, `splits` for a position's bytes
+    int splits, chunks, chunk;             // of the move
 };
-EvictPlan evict_plan(const peqa_kv_cache *C, int n, int max_len, int keep)
+EvictPlan evict_plan(const peqa_kv_cache *C, int n, int max_len, int keep, bool in_place)
 {
     EvictPlan p{};
     const int heads = n * C->kv_heads, most = max_len < keep ? max_len : keep;
-    const int row_bytes = C->head_dim * (C->dtype == PEQA_CACHE_FP8 ? 1 : 2), piece = heads <= 32 ? 64 : 128;
-    p.few = heads < PLAN_UNITS;
-    p.splits = p.few && row_bytes > piece ? row_bytes / piece : 1;
-    // a step each, or, of many heads, up to a section
+    const int row_bytes = C->head_dim * (C->dtype == PEQA_CACHE_FP8 ? 1 : 2);
+    // In place a head's positions are one workgroup's, or its lines': of few heads 16 waves that have 128 bytes of each, which keep more in flight.
+    // (us, and as of many heads: 1 x 8 heads, 1501 -> 1001 positions 14.6, 23.5;  5 x 8, 3000 -> 2000 22, 45;  2 x 8 of 256 elements, 6000 -> 4000
+    // 39, 138;  25 x 8, 2000 -> 1000 30.6, 31.7;  40 x 8 43.9, 44.2;  64 x 8 of 64 bytes 30.9, 27.6.  Pieces of 64 bytes 14.7, 23.5, 39.3, 41.7.  To
+    // another cache 2 x 8 of 256 elements 46.7, 41.9;  4 x 8 20.2, 18.6.)
+    p.few = in_place && heads < PLAN_UNITS;
+    p.splits = p.few && row_bytes > 128 ? row_bytes / 128 : 1;
+    // to another cache a step each, or, of many heads, up to a section
     const int threads = p.few ? 1024 : 256, step = each_of(threads) * (threads * 16 * p.splits / row_bytes);
-    long long chunk = (long long)most * heads * 2 * p.splits / (8 * PLAN_UNITS) / step * step;
+    long long chunk = in_place ? SECTION : (long long)most * heads * 2 * p.splits / (8 * PLAN_UNITS) / step * step;
     chunk = chunk < step ? step : chunk > SECTION ? SECTION : chunk;
     p.chunk = (int)chunk;
-    p.chunks = (int)((most + chunk - 1) / chunk);
+    p.chunks = in_place ? 1 : (int)((most + chunk - 1) / chunk);
     if (p.chunks < 1) p.chunks = 1;
     p.kept_bytes = round256((size_t)n * (size_t)C->kv_heads * (size_t)keep * sizeof(int32_t));
     p.moved_bytes = round256((size_t)n * sizeof(int32_t));
@@ -309,7 +313,7 @@ peqa_status check_evict(const peqa_kv_cache *C, int32_t n, int32_t max_len, int3
     if (n < 1 || max_len < 0 || (int64_t)max_len > (int64_t)C->n_blocks * C->page_size) return PEQA_ERR_SHAPE;
     if (keep < 1 || keep > (1 << 30)) return PEQA_ERR_PARAM;
     if ((int64_t)n * C->kv_heads > (1 << 20)) return PEQA_ERR_SHAPE;          // workgroups of a launch, here and of the move
-    const EvictPlan p = evict_plan(C, n, max_len, keep);
+    const EvictPlan p = evict_plan(C, n, max_len, keep, false);
     if ((int64_t)n * C->kv_heads * 2 * p.splits * p.chunks > (1 << 23)) return PEQA_ERR_SHAPE;
     return PEQA_OK;
 }
@@ -333,7 +337,7 @@ extern "C" {
 size_t peqa_cache_evict_workspace_bytes(const peqa_kv_cache *C, int32_t n, int32_t max_len, int32_t keep)
 {
     if (peqa::check_evict(C, n, max_len, keep) != PEQA_OK) return 0;
-    const peqa::EvictPlan p = peqa::evict_plan(C, n, max_len, keep);
+    const peqa::EvictPlan p = peqa::evict_plan(C, n, max_len, keep, true);
     return p.kept_bytes + p.moved_bytes;
 }
 
@@ -364,7 +368,7 @@ peqa_status peqa_cache_evict(const peqa_kv_cache *C, const peqa_kv_cache *to, in
         return PEQA_ERR_ALIGN;
     const intptr_t behind = (intptr_t)new_lens - (intptr_t)lens;
     if (new_lens && behind < n * 4ll && -behind < n * 4ll) return PEQA_ERR_PARAM;             // (the heads' workgroups read lens)
-    const peqa::EvictPlan p = peqa::evict_plan(C, n, max_len, keep);
+    const peqa::EvictPlan p = peqa::evict_plan(C, n, max_len, keep, in_place);
     if (!workspace || workspace_bytes < p.kept_bytes + p.moved_bytes) return PEQA_ERR_WORKSPACE;
     if (!aligned16(workspace)) return PEQA_ERR_ALIGN;
     char *w = static_cast<char *>(workspace);
@@ -381,8 +385,8 @@ peqa_status peqa_cache_evict(const peqa_kv_cache *C, const peqa_kv_cache *to, in
     a.row_bytes = C->head_dim * (C->dtype == PEQA_CACHE_FP8 ? 1 : 2);
     const int heads = n * C->kv_heads;
     a.splits = p.splits;
-    a.chunk = in_place ? max_len : p.chunk;
-    a.chunks = in_place ? 1 : p.chunks;
+    a.chunk = p.chunk;
+    a.chunks = p.chunks;
     hipStream_t s = static_cast<hipStream_t>(stream);
     peqa::trace_before(peqa::KID_EVICT_SELECT, s);
     // (512 and 1024 threads, us: 16 x 32 heads of up to 2048 positions 8.5 and 12.6, 512 of 300 5.8 and 11.7;  8 of 30000 77 and 58 with a weight of a

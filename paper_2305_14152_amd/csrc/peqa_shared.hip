@@ -887,9 +887,15 @@ SharedPlan shared_plan(const peqa_kv_cache *C, int rows, int heads, int max_len,
     p.hb = 1;
     while (p.hb < most && 16 * p.hb < queries) p.hb *= 2;
     p.columns = 16 * p.hb;
+    // (up to 64 columns all in every wave / each wave its own, us: 8 key heads x 32, 40000 positions 39.8 / 57.6;  4 x 64 28.5 / 33.9, 8 bits 27.0 / 29.5;
+    // 4 x 80 36.3 / 34.4;  4 x 128 37.3 / 35.5, 8 bits 36.0 / 31.4, heads of 64 29.6 / 27.9;  4 x 160 72 / 50;  8 x 256 81 / 72.5;  8192 positions
+    // 4 x 80 18.8 / 18.7, 4 x 128 19.6 / 19.8)
     p.wide = C->head_dim <= 128 && queries > 64;
     if (p.wide) {
-        p.hb = queries > 128 ? 2 : 1;
+        // 256 columns halve what comes through LDS for each, 128 the parts, which count where few positions are walked; neither leaves columns
+        // empty that the other does not (us, 256 / 128: 8 key heads x 512, 8192 shared and up to 1024 own 73 / 87.5;  8 x 256, 30000 72.5 / 76.6;
+        // 4 x 160, 40000 50 / 54;  8 x 256, 8192 (8 bits) 29.0 / 27.9;  4 x 160, 8192 25.8 / 22.8;  4 x 320, 30000 68 / 58)
+        p.hb = (queries + 127) / 128 % 2 == 0 && (queries + 255) / 256 * C->kv_heads * shared >= 2 * UNIT * PLAN_UNITS ? 2 : 1;
         p.columns = 128 * p.hb;
     }
     p.tiles = (int)((queries + p.columns - 1) / p.columns);
