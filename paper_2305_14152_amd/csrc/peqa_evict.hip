@@ -66,9 +66,9 @@ __global__ __launch_bounds__(THREADS) void evict_select_kernel(EvictArgs a)
 {
     constexpr int WAVES = THREADS / 64, OWN = 2048 / THREADS;
     constexpr int FIRST = 4096 / THREADS, FLIGHT = 8;      // weights of a thread that stay in registers; of the others, in flight
-    __shared__ uint32_t bins[2048];
+    __shared__ __attribute__((aligned(16))) uint32_t bins[3][2048];       // of a pass each
     __shared__ uint32_t scan[2][WAVES][2];
-    __shared__ uint32_t found[2];                          // the digit, and how many of its weights stay
+    __shared__ uint32_t found[3][2];                       // the digit, and how many of its weights stay
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int i = (int)(blockIdx.x / (unsigned)a.from.kv_heads), h = (int)blockIdx.x - i * a.from.kv_heads;
     const Entry e = entry_of(a, i);
@@ -82,6 +82,7 @@ __global__ __launch_bounds__(THREADS) void evict_select_kernel(EvictArgs a)
         for (int j = tid; j < a.keep; j += THREADS) kept[j] = -1;
         return;
     }
+    for (int j = tid; j < 3 * 512; j += THREADS) reinterpret_cast<u32x4 *>(bins)[j] = u32x4{0, 0, 0, 0};
     const float *in = a.weights + e.seq * a.seq_stride + h * a.head_stride;
     float *out = a.weights_out + e.seq * a.seq_stride + h * a.head_stride;
     const int lo = a.sinks, hi = e.len - a.recent;         // those that have to be chosen from, where some leave
@@ -97,6 +98,7 @@ __global__ __launch_bounds__(THREADS) void evict_select_kernel(EvictArgs a)
     }
     uint32_t least = 0, equal = 0;                         // the least order that stays, and how many of it
     if (!all) {
+        __syncthreads();                                   // (the bins are empty)
         uint32_t room = (uint32_t)(a.keep - a.sinks - a.recent), known = 0, mask = 0;
         if (room == 0) {
             least = 0xFFFFFFFFu;                           // (of NaN only, which no weight has)
@@ -104,10 +106,8 @@ __global__ __launch_bounds__(THREADS) void evict_select_kernel(EvictArgs a)
 #pragma unroll 1
             for (int pass = 0; pass < 3; ++pass) {
                 const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, digits = pass == 2 ? 1024 : 2048;
-                for (int j = tid; j < 2048; j += THREADS) bins[j] = 0;
-                __syncthreads();
                 auto count = [&](int j, uint32_t o) {
-                    if (j >= lo && j < hi && (o & mask) == known) atomicAdd(&bins[(o >> shift) & (digits - 1)], 1u);
+                    if (j >= lo && j < hi && (o & mask) == known) atomicAdd(&bins[pass][(o >> shift) & (digits - 1)], 1u);
                 };
 #pragma unroll
                 for (int k = 0; k < FIRST; ++k) count(k * THREADS + tid, order[k]);
@@ -123,7 +123,7 @@ __global__ __launch_bounds__(THREADS) void evict_select_kernel(EvictArgs a)
                 uint32_t own[OWN], mine = 0;
 #pragma unroll
                 for (int d = 0; d < OWN; ++d) {
-                    own[d] = bins[2047 - OWN * tid - d];
+                    own[d] = bins[pass][2047 - OWN * tid - d];
                     mine += own[d];
                 }
                 uint32_t upto = mine;
@@ -141,17 +141,16 @@ __global__ __launch_bounds__(THREADS) void evict_select_kernel(EvictArgs a)
 #pragma unroll
                     for (int d = 0; d < OWN; ++d) {
                         if (before < room && room <= before + own[d]) {
-                            found[0] = 2047 - OWN * tid - d;
-                            found[1] = room - before;
+                            found[pass][0] = 2047 - OWN * tid - d;
+                            found[pass][1] = room - before;
                         }
                         before += own[d];
                     }
                 }
                 __syncthreads();
-                known |= found[0] << shift;
+                known |= found[pass][0] << shift;
                 mask |= (uint32_t)(digits - 1) << shift;
-                room = found[1];
-                __syncthreads();
+                room = found[pass][1];
             }
             least = known;
             equal = room;
@@ -221,15 +220,23 @@ __global__ __launch_bounds__(THREADS) void evict_move_kernel(EvictArgs a)
     const bool is_v = b & 1;
     b >>= 1;
     const int i = (int)(b / (unsigned)a.from.kv_heads), h = (int)(b - (unsigned)i * (unsigned)a.from.kv_heads);
+    const int32_t *kept = a.kept + ((size_t)i * a.from.kv_heads + h) * (size_t)a.keep;
+    const int first = chunk * a.chunk;
+    // (the first section's, asked for before it is known how many there are)
+    int32_t old_at[SECTION / THREADS];
+#pragma unroll
+    for (int k = 0; k < SECTION / THREADS; ++k) {
+        const int j = first + k * THREADS + (int)threadIdx.x;
+        old_at[k] = j < a.keep ? kept[j] : -1;
+    }
     const int n = a.moved[i], seq = a.seq ? a.seq[i] : i;
     const int bytes = a.row_bytes / a.splits, lanes = bytes / 16, rows = THREADS / lanes;
     const int row = (int)threadIdx.x / lanes, at = split * bytes + 16 * ((int)threadIdx.x - row * lanes);
     const int step = EACH * rows;
-    const int32_t *kept = a.kept + ((size_t)i * a.from.kv_heads + h) * (size_t)a.keep;
     const uint8_t *src = static_cast<const uint8_t *>(is_v ? a.from.v : a.from.k) + h * a.from.head_stride + at;
     uint8_t *dst = static_cast<uint8_t *>(is_v ? a.to.v : a.to.k) + h * a.to.head_stride + at;
     const int32_t *table = a.from.table + seq * a.from.table_stride, *to_table = a.to.table + seq * a.to.table_stride;
-    const int first = chunk * a.chunk, until = a.in_place ? n : first + a.chunk < n ? first + a.chunk : n;
+    const int until = a.in_place ? n : first + a.chunk < n ? first + a.chunk : n;
     for (int j0 = first; j0 < until; j0 += SECTION) {
         const int count = until - j0 < SECTION ? until - j0 : SECTION;
         if (j0 > first) __syncthreads();                    // (the last section's places have been read)
@@ -237,7 +244,7 @@ __global__ __launch_bounds__(THREADS) void evict_move_kernel(EvictArgs a)
         for (int k = 0; k < SECTION / THREADS; ++k) {
             const int u = k * THREADS + (int)threadIdx.x, j = j0 + u;
             if (u < count) {
-                const int old = kept[j];
+                const int old = j0 == first ? old_at[k] : kept[j];
                 const bool moves = old >= 0 && !(a.in_place && old == j);
                 const int page = moves ? table[old >> a.from.page_shift] : -1, goal = moves ? to_table[j >> a.to.page_shift] : -1;
                 const bool there = page >= 0 && page < a.from.n_pages, room = goal >= 0 && goal < a.to.n_pages;
