@@ -1,11 +1,20 @@
 // Attention of single query tokens whose sequences begin with the same positions (peqa_shared_attention): those are read once for all rows.
 //
 // For a key head the queries of all rows and of the heads that share it are the columns of one product with the shared positions; what
-// a row has of its own is a product with its heads alone.  Both are cut into chunks of positions, a workgroup each, in one launch, and every
-// column's parts (running maximum, sum, weighted values) are joined by a second one.  A workgroup has up to 64 columns (heads of 128) in blocks of 16, its four
-// waves take tiles of 32 positions in turn and have all columns of each, so that a key or a value that is loaded is used for every column
-// without passing through LDS; the products and their operands are those of the paged attention (scores as keys x queries, whose result is the
-// weights' operand of values^T x weights as it stands; values are turned 8 x 8 in registers).
+// a row has of its own is a product with its heads alone:
+//   x[j][c] = scale <k_j, q_c>;   m_c = max_j x[j][c];   l_c = sum_j e^(x[j][c] - m_c);   o_c = sum_j e^(x[j][c] - m_c) v_j
+// Both are cut into chunks of positions, a workgroup each, in one launch, and every column's parts (m, l, o) are joined by a second one: with
+// M = max m, out = sum e^(m - M) o / sum e^(m - M) l.  The products and their operands are those of the paged attention (scores as keys x
+// queries, whose result is the weights' operand of values^T x weights as it stands; values are turned 8 x 8 in registers).
+//
+// Up to 64 columns (32 of heads of 256) are in every wave: four waves take tiles of 32 positions in turn, and a key or a value that is loaded is used
+// for every column without passing through LDS.  More have waves of their own, 16 or 32 each of eight, and keys and values come to LDS once,
+// as operands, for all of them.
+//
+// Bound by memory where columns are few: 3 rows x 32 heads behind 555 positions 5.4 us and the join 3, launches and loads after one another;  16
+// rows x 32 heads behind 2048 with up to 512 of their own 20 us, 4.9 TB/s of the cache.  Where they are many the matrix instructions (16 cycles)
+// and the vector instructions of the softmax, about as long again, share a SIMD's time and hardly overlap: of 65537 positions of 8 bits, 8 key
+// heads, 256 columns, 97 us, the matrix units are busy for 35 % and vector instructions are issued for half (0.71 PFLOP/s).
 #include "peqa_attend.h"
 #include "peqa_cache.h"
 #include "peqa_host.h"
