@@ -12,9 +12,10 @@
 // as operands, for all of them.
 //
 // Bound by memory where columns are few: 3 rows x 32 heads behind 555 positions 5.4 us and the join 3, launches and loads after one another;  16
-// rows x 32 heads behind 2048 with up to 512 of their own 20 us, 4.9 TB/s of the cache.  Where they are many the matrix instructions (16 cycles)
-// and the vector instructions of the softmax, about as long again, share a SIMD's time and hardly overlap: of 65537 positions of 8 bits, 8 key
-// heads, 256 columns, 97 us, the matrix units are busy for 35 % and vector instructions are issued for half (0.71 PFLOP/s).
+// rows x 32 heads behind 2048 with up to 512 of their own 20 us, 4.9 TB/s of the cache.  Where they are many, by three things that overlap in part and
+// are about 1000 cycles each for a tile of 32 positions and 256 columns, of the 2800 that it takes: matrix instructions, vector instructions of the softmax and
+// of the operands, and the operands' way out of LDS, 16 KB for each of eight waves.  65537 positions of 8 bits, 8 key heads, 256 columns
+// 93 us, 0.74 PFLOP/s; more columns a wave than 32, which would halve the last, do not fit its registers.
 #include "peqa_attend.h"
 #include "peqa_cache.h"
 #include "peqa_host.h"
@@ -500,7 +501,10 @@ __device__ __forceinline__ void attend_columns(const SharedArgs &a, const Item &
     const float scale = scale_of<FP8>(a, it.kv_head, turn);
     const bool idle = !KEYS && VR == 1 && (wave & 1);
     const int sub = wave >> 1 & 1, half = wave & 1;   // tile of a stage; which keys, or elements, of it
-    const uint8_t *base = static_cast<const uint8_t *>(KEYS ? C.k : C.v) + it.kv_head * C.head_stride * EL + (KEYS ? 16 * g : (WH * c + (idle ? 0 : half * (D / HALVES))) * EL);
+    const uint8_t *pool = static_cast<const uint8_t *>(KEYS ? C.k : C.v) + it.kv_head * C.head_stride * EL;
+    const int in_head = KEYS ? 16 * g : (WH * c + (idle ? 0 : half * (D / HALVES))) * EL;
+    const uint8_t *base = pool + in_head;
+    const uint32_t lane_at = (uint32_t)((KEYS ? 16 * half + c : 4 * g) * slot_bytes + in_head);       // in a page of 32 positions or more
     // This wave's tile of a stage; past the last one, that again (as many loads in every stage: what is waited for is counted).
     auto tile_at = [&](int t0) __attribute__((always_inline)) {
         const int t = t0 + TILE * sub, most = it.begin + ((last - it.begin) & ~(TILE - 1));
@@ -518,7 +522,28 @@ __device__ __forceinline__ void attend_columns(const SharedArgs &a, const Item &
         const int t = tile_at(t0);
         const Pages pages = pages_of(C, next, EL);
         raw.there = pages.there;
-        if constexpr (KEYS) {
+        if (C.page_shift >= 5 && t + TILE <= it.end) {
+            // of one page, all of it: what differs between lanes stays as it is
+            const uint8_t *src = pool + pages.at[0] + (uint32_t)((t & C.page_mask) * slot_bytes);
+            if constexpr (KEYS) {
+#pragma unroll
+                for (int j = 0; j < KB; ++j) {
+                    const u32x4 k = *reinterpret_cast<const u32x4 *>(src + 64 * j + lane_at);
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) raw.r[2 * j + (r >> 1)][r & 1] = k[r];
+                }
+            } else {
+#pragma unroll
+                for (int s = 0; s < 2; ++s)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        uint32_t v[VH];
+                        load_value<VH>(src + (uint32_t)((16 * s + i) * slot_bytes) + lane_at, v);
+#pragma unroll
+                        for (int r = 0; r < VH; ++r) raw.r[4 * s + i][r] = v[r];
+                    }
+            }
+        } else if constexpr (KEYS) {
             const uint8_t *src = base + place_of(C, pages, t, t + 16 * half + c, last, slot_bytes);
 #pragma unroll
             for (int j = 0; j < KB; ++j) {
@@ -588,16 +613,13 @@ __device__ __forceinline__ void attend_columns(const SharedArgs &a, const Item &
         for (int e = 0; e < W; ++e) acc[b][e] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
 
-    // A step is a block of columns of a tile.  While its scores become weights, the matrix instructions are those of its neighbours, one by one
-    // between the vector instructions: values x weights of the block before, keys x queries of the one after.  (Of a single block the weights are added
-    // first: its reference may move.)
+    // A step is a block of columns of a tile; the next one's scores are begun while this one's become weights.  (A block's values x weights held back
+    // until the next one's exponentials, each matrix instruction between vector instructions: 96.0 us for 93.5 of 65537 positions of 8 bits, 71.0
+    // for 71.4 of 30000 of bf16.)
     u32x4 key[2 * QK], vt[W];
     uint32_t next_pages = 15u;                        // of the tile whose keys were read, and where it begins
     int next_t0 = it.begin;
     f32x4 x[2];
-    Weights<FP8> w{};
-#pragma unroll
-    for (int e = 0; e < W; ++e) vt[e] = u32x4{0, 0, 0, 0};
     int t0 = it.begin;                                // of the present tile
     auto operands_of = [&](int stage, int tile) __attribute__((always_inline)) { return lds + (stage * SUB + tile) * FRAGS * 64 + lane; };
     auto read_keys = [&](int stage, int tile, int t) __attribute__((always_inline)) {
@@ -607,13 +629,13 @@ __device__ __forceinline__ void attend_columns(const SharedArgs &a, const Item &
         next_pages = there[stage][tile];
         next_t0 = t;
     };
-    auto begin_scores = [&]() __attribute__((always_inline)) {
-        x[0] = x[1] = f32x4{0.f, 0.f, 0.f, 0.f};
+    // Scores of positions that are not seen (their keys are zeros in LDS) become -inf.
+    auto hide = [&]() __attribute__((always_inline)) {
         const uint32_t pages = __builtin_amdgcn_readfirstlane(next_pages);
         if (next_t0 + TILE > it.end || pages != 15u) {
             const Start start = start_of(C, pages, next_t0, g, it.lo, it.end);
-            x[0] = start.x[0];
-            x[1] = start.x[1];
+            x[0] += start.x[0];
+            x[1] += start.x[1];
         }
     };
     // (stage: its number's last bit.  Past the last tile everything goes on, so that the loads in flight are always as many; those scores are not used.)
@@ -630,49 +652,19 @@ __device__ __forceinline__ void attend_columns(const SharedArgs &a, const Item &
         }
     };
     auto step = [&](int stage, int tile, int b) __attribute__((always_inline)) {
-        constexpr bool APART = HB > 1;
-        if (APART && b == HB - 1) next_keys(stage, tile);
-        if (!APART) add_weighted<FP8, W>(vt, w, acc[0]);
-        follow<FP8>(x, scale, m[b], l[b], acc[b]);
-        f32x4 *before = acc[b > 0 ? b - 1 : HB - 1];
-        float p[8], rest[8];
-        __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            if (APART && i < W) before[i] = FP8 ? mfma_f16(vt[i], w.near, before[i]) : mfma_bf16(vt[i], w.near, before[i]);
-            p[i] = __builtin_amdgcn_exp2f(fmaf(x[i >> 2][i & 3], scale, -m[b]));
-            __builtin_amdgcn_sched_barrier(0);
-        }
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            if (APART && !FP8 && i < W) before[i] = mfma_bf16(vt[i], w.rest, before[i]);
-            l[b] += p[i];
-            // (see operands)
-            if (!FP8) rest[i] = fmaxf(p[i] - __uint_as_float(__float_as_uint(p[i]) & 0xFFFF0000u), 1.2e-38f);
-            __builtin_amdgcn_sched_barrier(0);
-        }
+        hide();
         if (b == 0) {
             const u32x4 *from = operands_of(stage, tile);
 #pragma unroll
-            for (int e = 0; e < W; ++e) vt[e] = from[(2 * QK + e) * 64];
+            for (int k = 0; k < W; ++k) vt[k] = from[(2 * QK + k) * 64];
         }
-        if (!APART) next_keys(stage, tile);
-        begin_scores();
-        __builtin_amdgcn_sched_barrier(0);
+        if (b == HB - 1) next_keys(stage, tile);
+        follow<FP8>(x, scale, m[b], l[b], acc[b]);
+        const Eights e = powers(x, scale, m[b], l[b]);
+        x[0] = x[1] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int j = 0; j < 2 * QK; ++j) {
-            x[j & 1] = mfma_bf16(key[(j & 1) * QK + (j >> 1)], q[b + 1 < HB ? b + 1 : 0][j >> 1], x[j & 1]);
-            if (j < 4) {
-                if constexpr (FP8) {
-                    const f16x2 h = {(_Float16)p[2 * j], (_Float16)p[2 * j + 1]};
-                    w.near[j] = __builtin_bit_cast(uint32_t, h);
-                } else {
-                    w.near[j] = __builtin_amdgcn_perm(__float_as_uint(p[2 * j + 1]), __float_as_uint(p[2 * j]), 0x07060302u);
-                    w.rest[j] = pack_bf16x2(rest[2 * j], rest[2 * j + 1]);
-                }
-            }
-            __builtin_amdgcn_sched_barrier(0);
-        }
+        for (int j = 0; j < 2 * QK; ++j) x[j & 1] = mfma_bf16(key[(j & 1) * QK + (j >> 1)], q[b + 1 < HB ? b + 1 : 0][j >> 1], x[j & 1]);
+        add_weighted<FP8, W>(vt, operands<FP8>(e), acc[b]);
     };
     entries_at(it.begin);
     fetch(raw[0], it.begin);
@@ -684,7 +676,7 @@ __device__ __forceinline__ void attend_columns(const SharedArgs &a, const Item &
     fetch(raw[0], it.begin + 2 * STEP);
     entries_at(it.begin + 3 * STEP);
     read_keys(0, 0, t0);
-    begin_scores();
+    x[0] = x[1] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int j = 0; j < 2 * QK; ++j) x[j & 1] = mfma_bf16(key[(j & 1) * QK + (j >> 1)], q[0][j >> 1], x[j & 1]);
     for (bool more = true; more;) {
@@ -697,7 +689,6 @@ __device__ __forceinline__ void attend_columns(const SharedArgs &a, const Item &
             more = t0 < it.end;
         }
     }
-    add_weighted<FP8, W>(vt, w, acc[HB - 1]);
     // A block's sums through the wave's part of LDS, so that whole rows are stored (16 bytes a lane, each of another row: 11 us of the 24 that 128
     // positions take, of 256 workgroups; pieces of a row change places by its column's last bits, for the banks).
     const float v_scale = FP8 && C.v_scale ? C.v_scale[it.kv_head] : 1.f;
