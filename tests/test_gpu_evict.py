@@ -315,3 +315,32 @@ def test_far_places(env, fp8):
     for small, big in zip(*pools):
         for a, b in zip(near, far):
             assert torch.equal(small.view(bits)[a], big.view(bits)[b])
+
+
+def test_in_place_by_name(env):
+    """The cache itself as the one that positions go to, and another descriptor of the same pools: in place.  Its own spare pages: elsewhere."""
+    torch, peqa = env
+    gen = torch.Generator().manual_seed(13)
+    lens, results = [300, 77, 450], []
+    for name in ("none", "itself", "alike", "spare"):
+        gen.manual_seed(13)
+        cache = make_cache(torch, peqa, gen, [450] * 6, 2, 64, 16)
+        table = cache.tensors[2]
+        spare = table[3:].clone()
+        table[3:] = -1
+        goal = table if name != "spare" else torch.cat((spare, table[3:]))
+        to = None if name == "none" else cache if name == "itself" else peqa.kv_cache(*cache.tensors[:2], goal)
+        weights = torch.rand((6, 2, 452), generator=gen).cuda()
+        kept = torch.empty((3, 2, 100), dtype=torch.int32, device="cuda")
+        room = peqa.cache_evict_workspace_bytes(cache, 3, 450, 100)
+        ws = torch.empty(room, dtype=torch.uint8, device="cuda")
+        before = [cache.tensors[w][table[:3].long()].clone() for w in (0, 1)]
+        peqa.cache_evict(cache, torch.tensor(lens, dtype=torch.int32, device="cuda"), 450, weights, weights, 100, 4, 30, kept, None, ws, room, to=to)
+        at = goal[:3].long()
+        rows = [cache.tensors[w][at].permute(0, 2, 1, 3, 4).flatten(2, 3)[s, :, :min(100, lens[s])] for w in (0, 1) for s in range(3)]
+        results.append([kept, weights] + rows)
+        if name == "spare":
+            assert all(torch.equal(cache.tensors[w][table[:3].long()].view(torch.int16), before[w].view(torch.int16)) for w in (0, 1))
+    for other in results[1:]:
+        for a, b in zip(results[0], other):
+            assert torch.equal(a, b)
