@@ -804,15 +804,19 @@ __global__ __launch_bounds__(512, 1) void shared_wide_kernel(SharedArgs a)
     else attend_columns<D, FP8, HB, false>(a, it, lds.operands, there);
 }
 
-// Joins a column's parts: a workgroup per row and head.  A group of D / 4 lanes has some of the parts, 16 bytes of a part's sums a lane, four
-// parts in flight; the groups' results meet in LDS.
-template <int D> __global__ __launch_bounds__(256) void shared_join_kernel(SharedArgs a)
+// Joins a column's parts: a workgroup, or a wave of one (EACH = 4), per row and head.  A group of D / 4 lanes has some of the parts, 16 bytes of a
+// part's sums a lane, four or eight parts in flight; the groups' results meet in LDS.
+template <int D, int EACH> __global__ __launch_bounds__(256) void shared_join_kernel(SharedArgs a)
 {
-    constexpr int LANES = D / 4, GROUPS = 256 / LANES, FLIGHT = 4;
-    __shared__ float group_m[GROUPS], group_l[GROUPS];
-    __shared__ f32x4 sums[GROUPS][LANES];
+    constexpr int LANES = D / 4, GROUPS = 256 / EACH / LANES, FLIGHT = EACH > 1 ? 8 : 4;
+    __shared__ float all_m[EACH][GROUPS], all_l[EACH][GROUPS];
+    __shared__ f32x4 all_sums[EACH][GROUPS][LANES];
     const CacheArgs &C = a.cache;
-    const int row = (int)(blockIdx.x / (unsigned)a.heads), head = (int)(blockIdx.x - (unsigned)row * (unsigned)a.heads);
+    const int of_wg = EACH > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : 0, tid = EACH > 1 ? threadIdx.x & 63 : threadIdx.x;
+    auto &group_m = all_m[of_wg], &group_l = all_l[of_wg];
+    auto &sums = all_sums[of_wg];
+    const unsigned number = blockIdx.x * EACH + of_wg, items = (unsigned)a.rows * (unsigned)a.heads, item = number < items ? number : items - 1;   // (the last again)
+    const int row = (int)(item / (unsigned)a.heads), head = (int)(item - (unsigned)row * (unsigned)a.heads);
     const int kv_head = head / a.group, of_group = head - kv_head * a.group;
     const RowInfo r = row_info(a, row);
     const int shared = r.follows ? a.chunks : 0, n = shared + own_chunks(a, r).n;
@@ -820,7 +824,7 @@ template <int D> __global__ __launch_bounds__(256) void shared_join_kernel(Share
     const long long own0 = (long long)a.chunks * C.kv_heads * a.tiles * a.columns +
                            ((long long)(row * C.kv_heads + kv_head) * a.own_blocks + block) * a.own_splits * a.own_columns + (of_group - block * a.own_columns);
     const long long shared0 = ((long long)kv_head * a.tiles + tile) * a.columns + (query - tile * a.columns);
-    const int at = threadIdx.x % LANES, group = threadIdx.x / LANES;
+    const int at = tid % LANES, group = tid / LANES;
     float m = LOWEST, l = 0.f;
     f32x4 sum = {0.f, 0.f, 0.f, 0.f};
     for (int s0 = group; s0 < n; s0 += FLIGHT * GROUPS) {
@@ -851,7 +855,7 @@ template <int D> __global__ __launch_bounds__(256) void shared_join_kernel(Share
     sums[group][at] = sum;
     if (at == 0) { group_m[group] = m; group_l[group] = l; }
     __syncthreads();
-    if (threadIdx.x >= LANES) return;
+    if (tid >= LANES) return;
     float top = LOWEST, total = 0.f;
 #pragma unroll
     for (int k = 0; k < GROUPS; ++k) top = fmaxf(top, group_m[k]);
@@ -872,7 +876,7 @@ template <int D> __global__ __launch_bounds__(256) void shared_join_kernel(Share
 // How a call is cut.
 struct SharedPlan {
     bool wide;
-    int hb, columns, tiles, chunk, chunks, own_chunk, own_splits, own_blocks, own_columns;
+    int hb, columns, tiles, chunk, chunks, own_chunk, own_splits, own_blocks, own_columns, join_each;
     long long prefix_wgs, own_items;
     size_t part_bytes, ml_bytes;
 };
@@ -928,6 +932,9 @@ SharedPlan shared_plan(const peqa_kv_cache *C, int rows, int heads, int max_len,
     p.own_chunk = UNIT;
     p.prefix_wgs = ((long long)p.chunks * C->kv_heads + 7) / 8 * 8 * p.tiles;
     p.own_items = items * p.own_splits;
+    // A wave a column where columns are many and its parts all in flight at once (us, and by four waves: 64 rows x 64 heads of 10 parts 70.4, 74.5;  100 x 32
+    // of 64 elements 21.1, 22.6;  200 x 32 133, 136;  but 32 x 64 of 33 parts 96.2, 95.0, 8 x 64 of 64 38.2, 36.5)
+    p.join_each = (long long)rows * heads >= 4 * PLAN_UNITS && p.chunks + p.own_splits <= 2048 / C->head_dim ? 4 : 1;
     const size_t slots = (size_t)p.chunks * (size_t)units * (size_t)p.columns + (size_t)p.own_items * (size_t)p.own_columns;
     p.part_bytes = round256(slots * (size_t)C->head_dim * sizeof(float));
     p.ml_bytes = round256(slots * 2 * sizeof(float));
@@ -953,7 +960,9 @@ template <int D, bool FP8> hipError_t launch_shared(const SharedArgs &a, const S
     if (!p.wide && p.hb < 4) e = run(p.hb == 1 ? shared_kernel<D, FP8, 1> : shared_kernel<D, FP8, 2>, a, p.prefix_wgs + p.own_items, 256);
     if (e != hipSuccess) return e;
     trace_before(KID_SHARED_JOIN, stream);
-    hipLaunchKernelGGL(shared_join_kernel<D>, dim3((unsigned)a.rows * (unsigned)a.heads), dim3(256), 0, stream, a);
+    const unsigned items = (unsigned)a.rows * (unsigned)a.heads;
+    if (p.join_each > 1) hipLaunchKernelGGL((shared_join_kernel<D, 4>), dim3((items + 3) / 4), dim3(256), 0, stream, a);
+    else hipLaunchKernelGGL((shared_join_kernel<D, 1>), dim3(items), dim3(256), 0, stream, a);
     trace_after(KID_SHARED_JOIN, stream);
     return hipGetLastError();
 }
