@@ -170,13 +170,28 @@ struct Piece {
     bool first, last, alone;                               // of its segment; alone: the segment is the whole item
 };
 
-// What four positions were given by a head: of those in [lo, end); lse of powers of two.
-__device__ __forceinline__ void add_given(f32x4 &sum, const float *scores, float lse, int pos, int lo, int end)
+// What four positions were given by a row's heads of a key head, FLIGHT heads in flight, added in their order: of those in [lo, end); lse of powers
+// of two, -inf of a row that saw no position.
+template <int FLIGHT, typename Lse>
+__device__ __forceinline__ void add_given(f32x4 &sum, const float *scores, long long stride, int heads, Lse lse_of, int pos, int lo, int end)
 {
-    if (lse == -__builtin_inff()) return;                  // (a row without positions)
-    const f32x4 x = *reinterpret_cast<const f32x4 *>(scores + pos);
+    for (int i0 = 0; i0 < heads; i0 += FLIGHT) {
+        f32x4 x[FLIGHT];
+        float lse[FLIGHT];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) sum[k] += pos + k >= lo && pos + k < end ? __builtin_amdgcn_exp2f(x[k] - lse) : 0.f;
+        for (int i = 0; i < FLIGHT; ++i) {
+            const int at = i0 + i < heads ? i0 + i : i0;
+            x[i] = *reinterpret_cast<const f32x4 *>(scores + at * stride + pos);
+            lse[i] = lse_of(at);
+        }
+#pragma unroll
+        for (int i = 0; i < FLIGHT; ++i) {
+            if (i0 + i >= heads) continue;
+            const bool any = lse[i] != -__builtin_inff();
+#pragma unroll
+            for (int k = 0; k < 4; ++k) sum[k] += any && pos + k >= lo && pos + k < end ? __builtin_amdgcn_exp2f(x[i][k] - lse[i]) : 0.f;
+        }
+    }
 }
 __device__ __forceinline__ void store_given(const float *weights, float *weights_out, f32x4 sum, int pos, int end)
 {
@@ -608,8 +623,8 @@ __global__ __launch_bounds__(64 * WAVES, wgs_per_unit(D, FP8)) void attend_kerne
                 for (int pos = 4 * tid; pos < cur.end; pos += 256 * WAVES) {
                     f32x4 sum = {0.f, 0.f, 0.f, 0.f};
                     if (pos + 4 > cur.lo)
-                        for (int i = 0; i < a.group; ++i)
-                            add_given(sum, a.scores + ((size_t)cur.row * a.heads + (size_t)cur.kv_head * a.group + i) * a.score_stride, head_lse[i], pos, cur.lo, cur.end);
+                        add_given<4>(sum, a.scores + ((size_t)cur.row * a.heads + (size_t)cur.kv_head * a.group) * a.score_stride, a.score_stride, a.group,
+                                  [&](int i) { return head_lse[i]; }, pos, cur.lo, cur.end);
                     store_given(a.weights ? a.weights + at : nullptr, a.weights_out + at, sum, pos, cur.end);
                 }
             }
@@ -783,7 +798,7 @@ template <bool SCORES> hipError_t launch_attend(const peqa_kv_cache *C, const At
 // 2^(score - log2 of the sum of powers), of the scores that the attention left: a score is known long before its row's sum is, and 4 bytes written
 // and read again for a head and a position are less than reading its keys again (where 8 heads share 256 bytes of a key, an eighth).  A workgroup has
 // 1024 positions of a key head, four a thread, of the first row with its sequence, and adds the others' after one another, so that no sum
-// depends on an order of workgroups.  Bound by memory: 32 rows of up to 8192, 64 heads, 8 key heads  10 us for 33 MB of scores, which are
+// depends on an order of workgroups.  Bound by memory: 32 rows of up to 8192, 64 heads, 8 key heads  11 us for 33 MB of scores, which are
 // still cached in part; the attention that writes them takes 124 us for 109.
 struct WeightArgs {
     const int32_t *lens, *seq;
@@ -794,7 +809,7 @@ struct WeightArgs {
 };
 constexpr int WEIGHT_POSITIONS = 1024;
 
-__global__ __launch_bounds__(256) void attend_weights_kernel(WeightArgs a)
+template <int FLIGHT> __global__ __launch_bounds__(256) void attend_weights_kernel(WeightArgs a)
 {
     unsigned b = blockIdx.x;
     const int chunk = (int)(b % (unsigned)a.chunks);
@@ -817,10 +832,8 @@ __global__ __launch_bounds__(256) void attend_weights_kernel(WeightArgs a)
         if (len > longest) longest = len;
         const int lo = a.window > 0 && len > a.window ? len - a.window : 0;
         if (pos >= len || pos + 4 <= lo) return;
-        for (int i = 0; i < a.group; ++i) {
-            const size_t head = (size_t)r * a.heads + (size_t)h * a.group + i;
-            add_given(sum, a.scores + head * a.score_stride, a.lse[head] * LOG2E, pos, lo, len);
-        }
+        const size_t head = (size_t)r * a.heads + (size_t)h * a.group;
+        add_given<FLIGHT>(sum, a.scores + head * a.score_stride, a.score_stride, a.group, [&](int i) { return a.lse[head + i] * LOG2E; }, pos, lo, len);
     };
     add_row(row);
     if (a.seq) {
@@ -1030,7 +1043,7 @@ peqa_status peqa_paged_attention_weights(const peqa_kv_cache *C, int32_t rows, i
     a.scores = reinterpret_cast<float *>(w + r.parts);
     a.score_stride = r.stride;
     // An item that one workgroup has is finished there, without a launch of its own (1 row x 32, 1, of 333  10.5 us, 12.4 with; 16 x 32, 1, of 500
-    // 26.1, 28.5;  64 x 8, 8, up to 1000 (8 bits)  24.4, 26.6;  128 x 8, 8, up to 400  35.1, 34.7); rows of one sequence add to the same sums.
+    // 26.1, 28.5;  64 x 8, 8, up to 1000 (8 bits)  23.0, 26.8;  128 x 8, 8, up to 400  32.5, 34.8); rows of one sequence add to the same sums.
     const bool within = !seq && p.blocks == 1 && p.splits == 1 && p.shares == 0;
     if (within) {
         a.weights = weights; a.weights_out = weights_out;
@@ -1045,7 +1058,11 @@ peqa_status peqa_paged_attention_weights(const peqa_kv_cache *C, int32_t rows, i
     g.rows = rows; g.heads = heads; g.kv_heads = C->kv_heads; g.group = a.group; g.n_seqs = C->n_seqs;
     g.max_len = max_len; g.window = window; g.chunks = (int)chunks;
     peqa::trace_before(peqa::KID_ATTEND_WEIGHTS, s);
-    hipLaunchKernelGGL(peqa::attend_weights_kernel, dim3((unsigned)(chunks * rows * C->kv_heads)), dim3(256), 0, s, g);
+    // Few workgroups have more in flight each (both calls, us, four heads / two: 1 row of 30000, 8 key heads x 8 32.4, 33.7;  16 rows of up to 4096
+    // 37.1, 38.2;  32 of up to 8192 145.4, 142.9)
+    const long long wgs = chunks * rows * C->kv_heads;
+    auto kernel = wgs <= 4 * peqa::PLAN_UNITS ? peqa::attend_weights_kernel<4> : peqa::attend_weights_kernel<2>;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)wgs), dim3(256), 0, s, g);
     peqa::trace_after(peqa::KID_ATTEND_WEIGHTS, s);
     return dev_status(hipGetLastError());
 }
