@@ -622,9 +622,12 @@ __global__ __launch_bounds__(64 * WAVES, wgs_per_unit(D, FP8)) void attend_kerne
                 const long long at = cur.seq * a.weights_seq_stride + cur.kv_head * a.weights_head_stride;
                 for (int pos = 4 * tid; pos < cur.end; pos += 256 * WAVES) {
                     f32x4 sum = {0.f, 0.f, 0.f, 0.f};
-                    if (pos + 4 > cur.lo)
-                        add_given<4>(sum, a.scores + ((size_t)cur.row * a.heads + (size_t)cur.kv_head * a.group) * a.score_stride, a.score_stride, a.group,
-                                  [&](int i) { return head_lse[i]; }, pos, cur.lo, cur.end);
+                    const float *scores = a.scores + ((size_t)cur.row * a.heads + (size_t)cur.kv_head * a.group) * a.score_stride;
+                    auto lse_of = [&](int i) { return head_lse[i]; };
+                    if (pos + 4 > cur.lo) {
+                        if (a.group > 1) add_given<4>(sum, scores, a.score_stride, a.group, lse_of, pos, cur.lo, cur.end);
+                        else add_given<1>(sum, scores, a.score_stride, 1, lse_of, pos, cur.lo, cur.end);
+                    }
                     store_given(a.weights ? a.weights + at : nullptr, a.weights_out + at, sum, pos, cur.end);
                 }
             }
@@ -1061,7 +1064,7 @@ peqa_status peqa_paged_attention_weights(const peqa_kv_cache *C, int32_t rows, i
     // Few workgroups have more in flight each (both calls, us, four heads / two: 1 row of 30000, 8 key heads x 8 32.4, 33.7;  16 rows of up to 4096
     // 37.1, 38.2;  32 of up to 8192 145.4, 142.9)
     const long long wgs = chunks * rows * C->kv_heads;
-    auto kernel = wgs <= 4 * peqa::PLAN_UNITS ? peqa::attend_weights_kernel<4> : peqa::attend_weights_kernel<2>;
+    auto kernel = a.group == 1 ? peqa::attend_weights_kernel<1> : wgs <= 4 * peqa::PLAN_UNITS ? peqa::attend_weights_kernel<4> : peqa::attend_weights_kernel<2>;
     hipLaunchKernelGGL(kernel, dim3((unsigned)wgs), dim3(256), 0, s, g);
     peqa::trace_after(peqa::KID_ATTEND_WEIGHTS, s);
     return dev_status(hipGetLastError());
