@@ -43,6 +43,14 @@ struct ItemParts {
     int row, item, n, first, next, step;
 };
 
+// What the scores of a row and a head are weighted with: 2^(score - reference) / total (0 of a row that saw no position).  The logarithm of the sum would be one
+// number, but rounded to 2^-24 of itself: 2^-11 of every weight where scores are around 10^4.
+struct RowSum {
+    float reference, total;
+};
+constexpr int SUM_ROOM = 4;              // floats for it in front of a row's and a head's scores
+__device__ __forceinline__ RowSum &sum_of(const float *scores) { return *reinterpret_cast<RowSum *>(const_cast<float *>(scores) - SUM_ROOM); }
+
 struct AttendArgs {
     CacheArgs cache;
     const uint16_t *q;
@@ -53,7 +61,7 @@ struct AttendArgs {
     float *part;               // [slots, per_wg, head_dim] weighted sums, relative to the reference
     float *part_ml;            // [slots, per_wg, 2] reference (the maximum, or 14 below it; of powers of two) and sum
     ItemParts *parts;          // [rows * items of a row], or [shares]: of the item that ends in a share and began before it
-    float *scores;             // [rows, heads, score_stride] of powers of two, for the positions' weights; or null
+    float *scores;             // [rows, heads, score_stride] of powers of two, for the positions' weights, a RowSum in front of each; or null
     const float *weights;      // of an item's positions, where the workgroup that has all of it adds what they were given
     float *weights_out;        // (null: attend_weights_kernel does)
     long long q_stride, out_stride, score_stride, weights_seq_stride, weights_head_stride;
@@ -170,26 +178,26 @@ struct Piece {
     bool first, last, alone;                               // of its segment; alone: the segment is the whole item
 };
 
-// What four positions were given by a row's heads of a key head, FLIGHT heads in flight, added in their order: of those in [lo, end); lse of powers
-// of two, -inf of a row that saw no position.
-template <int FLIGHT, typename Lse>
-__device__ __forceinline__ void add_given(f32x4 &sum, const float *scores, long long stride, int heads, Lse lse_of, int pos, int lo, int end)
+// What four positions were given by a row's heads of a key head, FLIGHT heads in flight, added in their order: of those in [lo, end).  (Scores of positions that
+// are not seen are -inf, references finite.)
+template <int FLIGHT>
+__device__ __forceinline__ void add_given(f32x4 &sum, const float *scores, long long stride, int heads, int pos, int lo, int end)
 {
     for (int i0 = 0; i0 < heads; i0 += FLIGHT) {
         f32x4 x[FLIGHT];
-        float lse[FLIGHT];
+        RowSum of[FLIGHT];
 #pragma unroll
         for (int i = 0; i < FLIGHT; ++i) {
             const int at = i0 + i < heads ? i0 + i : i0;
             x[i] = *reinterpret_cast<const f32x4 *>(scores + at * stride + pos);
-            lse[i] = lse_of(at);
+            of[i] = sum_of(scores + at * stride);
         }
 #pragma unroll
         for (int i = 0; i < FLIGHT; ++i) {
             if (i0 + i >= heads) continue;
-            const bool any = lse[i] != -__builtin_inff();
+            const float by = of[i].total != 0.f ? __builtin_amdgcn_rcpf(of[i].total) : 0.f;
 #pragma unroll
-            for (int k = 0; k < 4; ++k) sum[k] += any && pos + k >= lo && pos + k < end ? __builtin_amdgcn_exp2f(x[i][k] - lse[i]) : 0.f;
+            for (int k = 0; k < 4; ++k) sum[k] += pos + k >= lo && pos + k < end ? __builtin_amdgcn_exp2f(x[i][k] - of[i].reference) * by : 0.f;
         }
     }
 }
@@ -239,7 +247,6 @@ __global__ __launch_bounds__(64 * WAVES, wgs_per_unit(D, FP8)) void attend_kerne
     __shared__ int scan[WAVES + 6];
     __shared__ float wave_m[WAVES][HB][16], wave_l[WAVES][HB][16];
     __shared__ __attribute__((aligned(16))) float joined[WAVES][8][DS + 4];
-    __shared__ float head_lse[SCORES ? COLS * HB : 1];
 
     const CacheArgs &C = a.cache;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -600,7 +607,7 @@ __global__ __launch_bounds__(64 * WAVES, wgs_per_unit(D, FP8)) void attend_kerne
                             *reinterpret_cast<u32x2 *>(o) = u32x2{pack_bf16x2(x[0] * by, x[1] * by), pack_bf16x2(x[2] * by, x[3] * by)};
                             if (at == 0 && s == 0) {
                                 const float lse = any ? top + __builtin_amdgcn_logf(total) : -__builtin_inff();
-                                if constexpr (SCORES) head_lse[b * COLS + 8 * half + col] = lse;
+                                if constexpr (SCORES) sum_of(a.scores + ((size_t)cur.row * a.heads + head) * a.score_stride) = RowSum{top, total};
                                 if (a.lse) a.lse[(size_t)cur.row * a.heads + head] = lse * LN2;
                             }
                         } else {
@@ -623,10 +630,9 @@ __global__ __launch_bounds__(64 * WAVES, wgs_per_unit(D, FP8)) void attend_kerne
                 for (int pos = 4 * tid; pos < cur.end; pos += 256 * WAVES) {
                     f32x4 sum = {0.f, 0.f, 0.f, 0.f};
                     const float *scores = a.scores + ((size_t)cur.row * a.heads + (size_t)cur.kv_head * a.group) * a.score_stride;
-                    auto lse_of = [&](int i) { return head_lse[i]; };
                     if (pos + 4 > cur.lo) {
-                        if (a.group > 1) add_given<4>(sum, scores, a.score_stride, a.group, lse_of, pos, cur.lo, cur.end);
-                        else add_given<1>(sum, scores, a.score_stride, 1, lse_of, pos, cur.lo, cur.end);
+                        if (a.group > 1) add_given<4>(sum, scores, a.score_stride, a.group, pos, cur.lo, cur.end);
+                        else add_given<1>(sum, scores, a.score_stride, 1, pos, cur.lo, cur.end);
                     }
                     store_given(a.weights ? a.weights + at : nullptr, a.weights_out + at, sum, pos, cur.end);
                 }
@@ -756,6 +762,7 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a)
     uint16_t *o = a.out + item.row * a.out_stride + (long long)head * D + 4 * at;
     *reinterpret_cast<u32x2 *>(o) = u32x2{pack_bf16x2(sum[0] * by, sum[1] * by), pack_bf16x2(sum[2] * by, sum[3] * by)};
     if (a.lse && at == 0) a.lse[(size_t)item.row * a.heads + head] = any ? (top + __builtin_amdgcn_logf(total)) * LN2 : -__builtin_inff();
+    if (a.scores && at == 0) sum_of(a.scores + ((size_t)item.row * a.heads + head) * a.score_stride) = RowSum{top, total};
 }
 
 template <int D, bool FP8, bool SCORES>
@@ -805,7 +812,7 @@ template <bool SCORES> hipError_t launch_attend(const peqa_kv_cache *C, const At
 // still cached in part; the attention that writes them takes 124 us for 109.
 struct WeightArgs {
     const int32_t *lens, *seq;
-    const float *scores, *lse, *weights;
+    const float *scores, *weights;
     float *weights_out;
     long long score_stride, seq_stride, head_stride;
     int rows, heads, kv_heads, group, n_seqs, max_len, window, chunks;
@@ -836,7 +843,7 @@ template <int FLIGHT> __global__ __launch_bounds__(256) void attend_weights_kern
         const int lo = a.window > 0 && len > a.window ? len - a.window : 0;
         if (pos >= len || pos + 4 <= lo) return;
         const size_t head = (size_t)r * a.heads + (size_t)h * a.group;
-        add_given<FLIGHT>(sum, a.scores + head * a.score_stride, a.score_stride, a.group, [&](int i) { return a.lse[head + i] * LOG2E; }, pos, lo, len);
+        add_given<FLIGHT>(sum, a.scores + head * a.score_stride, a.score_stride, a.group, pos, lo, len);
     };
     add_row(row);
     if (a.seq) {
@@ -973,19 +980,18 @@ peqa_status attend_args(const peqa_kv_cache *C, int32_t rows, int32_t heads, con
     return PEQA_OK;
 }
 
-// Room of a call that says what the positions were given, behind the parts' own: scores, and what the rows' sums were.
+// Room of a call that says what the positions were given, behind the parts' own: scores, and what the rows' sums were in front of them.
 struct ScoreRoom {
-    size_t parts, scores, lse;
+    size_t parts, scores;
     long long stride;
 };
 ScoreRoom score_room(const peqa_kv_cache *C, int rows, int heads, int max_len, int window)
 {
     const AttendPlan p = attend_plan(C, rows, heads, max_len, window);
     ScoreRoom r{};
-    r.stride = ((long long)max_len + 3) & ~3ll;
+    r.stride = (((long long)max_len + 3) & ~3ll) + SUM_ROOM;
     r.parts = p.part_bytes + p.ml_bytes + p.parts_bytes;
     r.scores = round256((size_t)rows * (size_t)heads * (size_t)r.stride * sizeof(float));
-    r.lse = round256((size_t)rows * (size_t)heads * sizeof(float));
     return r;
 }
 
@@ -1018,7 +1024,7 @@ size_t peqa_paged_attention_weights_workspace_bytes(const peqa_kv_cache *C, int3
 {
     if (peqa::check_attend(C, rows, heads, max_len, window) != PEQA_OK) return 0;
     const peqa::ScoreRoom r = peqa::score_room(C, rows, heads, max_len, window);
-    return r.parts + r.scores + r.lse;
+    return r.parts + r.scores;
 }
 
 peqa_status peqa_paged_attention_weights(const peqa_kv_cache *C, int32_t rows, int32_t heads, const uint16_t *q, int64_t q_stride,
@@ -1035,15 +1041,14 @@ peqa_status peqa_paged_attention_weights(const peqa_kv_cache *C, int32_t rows, i
     const peqa::ScoreRoom r = peqa::score_room(C, rows, heads, max_len, window);
     const long long chunks = ((long long)max_len + peqa::WEIGHT_POSITIONS - 1) / peqa::WEIGHT_POSITIONS;
     if (chunks * rows * C->kv_heads > (1 << 23)) return PEQA_ERR_SHAPE;       // workgroups of a launch
-    if (!workspace || workspace_bytes < r.parts + r.scores + r.lse) return PEQA_ERR_WORKSPACE;
+    if (!workspace || workspace_bytes < r.parts + r.scores) return PEQA_ERR_WORKSPACE;
     if (!aligned16(workspace)) return PEQA_ERR_ALIGN;
     char *w = static_cast<char *>(workspace);
-    if (!lse) lse = reinterpret_cast<float *>(w + r.parts + r.scores);
     peqa::AttendArgs a{};
     peqa::AttendPlan p{};
     st = peqa::attend_args(C, rows, heads, q, q_stride, lens, seq, max_len, window, scale, out, out_stride, lse, workspace, workspace_bytes, a, p);
     if (st != PEQA_OK) return st;
-    a.scores = reinterpret_cast<float *>(w + r.parts);
+    a.scores = reinterpret_cast<float *>(w + r.parts) + peqa::SUM_ROOM;
     a.score_stride = r.stride;
     // An item that one workgroup has is finished there, without a launch of its own (1 row x 32, 1, of 333  10.5 us, 12.4 with; 16 x 32, 1, of 500
     // 26.1, 28.5;  64 x 8, 8, up to 1000 (8 bits)  23.0, 26.8;  128 x 8, 8, up to 400  32.5, 34.8); rows of one sequence add to the same sums.
@@ -1056,7 +1061,7 @@ peqa_status peqa_paged_attention_weights(const peqa_kv_cache *C, int32_t rows, i
     const hipError_t e = peqa::launch_attend<true>(C, a, p, s);
     if (e != hipSuccess || chunks == 0 || within) return dev_status(e);
     peqa::WeightArgs g{};
-    g.lens = lens; g.seq = seq; g.scores = a.scores; g.lse = lse; g.weights = weights; g.weights_out = weights_out;
+    g.lens = lens; g.seq = seq; g.scores = a.scores; g.weights = weights; g.weights_out = weights_out;
     g.score_stride = r.stride; g.seq_stride = weights_seq_stride; g.head_stride = weights_head_stride;
     g.rows = rows; g.heads = heads; g.kv_heads = C->kv_heads; g.group = a.group; g.n_seqs = C->n_seqs;
     g.max_len = max_len; g.window = window; g.chunks = (int)chunks;
