@@ -5,8 +5,8 @@
 Every layer is: normalisation, one stacked PEQA linear for queries, keys and values, peqa_rope_append into the layer's paged
 cache, peqa_paged_attention, PEQA linears for the output projection and the MLP.  peqa_token_logprobs gives the next words (the
 largest alternative) and, for the text as a whole, its perplexity; peqa_token_logprobs_bwd the loss's gradient with respect
-to the logits.  With --norms the heads of queries and keys are normalised (peqa_norm_rope_append), with --keep the cache is cut to that many
-positions a head, those that were looked at most (peqa_paged_attention_weights, peqa_cache_evict), and several answers to one prompt read it
+to the logits.  With --norms the heads of queries and keys are normalised (peqa_norm_rope_append), with --keep beside it the cache is cut to that
+many positions a head, those that were looked at most (peqa_paged_attention_weights, peqa_cache_evict), and several answers to one prompt read it
 once (peqa_shared_attention).  Weights are random: the numbers mean nothing, the calls are those of a program with a checkpoint.
 """
 import argparse
@@ -93,7 +93,8 @@ class Decoder:
             if self.norms is not None:
                 peqa.norm_rope_append(cache, q, k, v, pos, self.cos, self.sin, *self.norms[n], 1e-6, q_out, place=place, seq=seq)
             else:
-                assert place is None
+                if place is not None:
+                    raise ValueError("tokens at places of their own: of decoders with norms only")
                 peqa.rope_append(cache, q, k, v, pos, self.cos, self.sin, q_out, seq=seq)
             if prefix is not None:
                 peqa.shared_attention(cache, q_out, lens, longest, *prefix, D ** -0.5, out, ws, room, seq=seq)
@@ -133,7 +134,10 @@ def int32(v):
 
 def generate(model, prompts, steps, top=5, keep=0, slack=32):
     """Reads the prompts (a list of lists of words) and writes `steps` words after each; texts, and every written word's alternatives.  keep: the
-    cache is cut to so many positions whenever it has `slack` more (0: it is not; a prompt longer than that is read whole first)."""
+    cache is cut to so many positions whenever it has `slack` more (0: it is not; a prompt longer than that is read whole first; of a decoder with
+    norms)."""
+    if keep and model.norms is None:
+        raise ValueError("a cache is cut of decoders with norms only: peqa_rope_append stores a token at the place of its position")
     lens = [len(p) for p in prompts]
     given = None
     if keep:
@@ -194,6 +198,8 @@ def main():
     ap.add_argument("--norms", action="store_true", help="heads of queries and keys normalised")
     ap.add_argument("--keep", type=int, default=0, help="positions a head that the cache is cut to (with --norms)")
     a = ap.parse_args()
+    if a.keep and not a.norms:
+        ap.error("--keep needs --norms")
     model = Decoder(layers=a.layers, dim=a.dim, mlp=-(-a.dim * 11 // 4 // 128) * 128, heads=a.dim // 128, kv_heads=max(1, a.dim // 512), fp8=a.fp8,
                     norms=a.norms)
     gen = torch.Generator().manual_seed(1)

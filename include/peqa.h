@@ -540,8 +540,9 @@ peqa_status peqa_paged_attention_weights(const peqa_kv_cache *C, int32_t rows, i
  * Eviction.  Of each of n sequences (entry i: sequence seq[i], lens[i] positions long; seq NULL: sequence i) and each key head by itself: where
  * there are more than `keep` positions, the first `sinks`, the last `recent` and, of those between, the keep - sinks - recent with the
  * largest weights stay (equal ones: the lowest positions; NaN is less than everything), in order, at places 0 .. keep - 1: keys, values and
- * weights.  Every head then has its own positions at a sequence's places, so that a token's place is no longer its position
- * (peqa_norm_rope_append).  Shorter sequences keep everything.
+ * weights.  Every head then has its own positions at a sequence's places, so that a token's place is no longer its position: the tokens that follow are
+ * stored by peqa_norm_rope_append, which takes both.  (peqa_rope_append does not: a decoder without head norms cannot go on behind an eviction, unless
+ * nothing is rotated and `pos` is the place.)  Shorter sequences keep everything.
  *   to: the cache that keys and values go to, at the same sequences' places: of as many sequences, the same heads, head_dim, dtype and scales,
  *   any page size; its pages of these places are none that C's sequences have.  NULL, or one with C's own pools and table: in place.  In
  *   place a sequence's pages are its own: what another sequence shares with it would change.
