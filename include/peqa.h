@@ -522,8 +522,8 @@ peqa_status peqa_shared_attention(const peqa_kv_cache *C, int32_t rows, int32_t 
  *   weights_out[s, h, j] = weights[s, h, j] + sum over the sequence's rows and the heads i of h of exp(x_j - lse[r, i])
  * (0 of positions outside the window and of pages that are not there; nothing else of weights_out is written).  out and lse are
  * peqa_paged_attention's, bit for bit.
- *   weights [n_seqs, kv_heads, max_len or more] fp32, sequences and heads strides apart (multiples of 4, at least max_len; 16-byte aligned), or
- *   NULL: zeros;  weights_out the same, may be weights itself
+ *   weights [n_seqs, kv_heads, max_len or more] fp32, sequences and heads strides apart (multiples of 4; 16-byte aligned; either of them the outer
+ *   one, and max_len of one never over those of another: PEQA_ERR_SHAPE), or NULL: zeros;  weights_out the same, may be weights itself
  *   workspace: peqa_paged_attention_weights_workspace_bytes(C, rows, heads, max_len, window): 4 bytes a row, head and position beside
  *   the attention's own.
  * Sums are fp32 in a fixed order: rows of one sequence after one another.

@@ -1036,8 +1036,8 @@ peqa_status peqa_paged_attention_weights(const peqa_kv_cache *C, int32_t rows, i
     peqa_status st = peqa::check_attend(C, rows, heads, max_len, window);
     if (st != PEQA_OK) return st;
     if (!weights_out) return PEQA_ERR_NULL;
-    if (weights_head_stride < max_len || weights_seq_stride < max_len) return PEQA_ERR_SHAPE;
     if (!aligned16(weights) || !aligned16(weights_out) || weights_head_stride % 4 || weights_seq_stride % 4) return PEQA_ERR_ALIGN;
+    if (!peqa::weights_apart(C, max_len, weights_seq_stride, weights_head_stride)) return PEQA_ERR_SHAPE;
     const peqa::ScoreRoom r = peqa::score_room(C, rows, heads, max_len, window);
     const long long chunks = ((long long)max_len + peqa::WEIGHT_POSITIONS - 1) / peqa::WEIGHT_POSITIONS;
     if (chunks * rows * C->kv_heads > (1 << 23)) return PEQA_ERR_SHAPE;       // workgroups of a launch

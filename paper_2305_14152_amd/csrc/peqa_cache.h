@@ -29,4 +29,14 @@ inline CacheArgs cache_args(const peqa_kv_cache *C)
     return a;
 }
 
+// Whether positions' weights [n_seqs, kv_heads, max_len], strides apart, are all places of their own: every sequence's heads together, or every head's sequences.
+inline bool weights_apart(const peqa_kv_cache *C, long long max_len, long long seq_stride, long long head_stride)
+{
+    if (seq_stride < max_len || head_stride < max_len) return false;
+    if (C->n_seqs == 1 || C->kv_heads == 1) return true;
+    // (n stretches of max_len, `stride` apart, before the next one that is `outer` further: without a product that could overflow)
+    auto within = [&](long long n, long long stride, long long outer) { return stride <= (outer - max_len) / (n - 1); };
+    return within(C->kv_heads, head_stride, seq_stride) || within(C->n_seqs, seq_stride, head_stride);
+}
+
 }  // namespace peqa

@@ -375,7 +375,7 @@ peqa_status peqa_cache_evict(const peqa_kv_cache *C, const peqa_kv_cache *to, in
     if (!lens || !weights || !weights_out) return PEQA_ERR_NULL;
     if (!seq && n > C->n_seqs) return PEQA_ERR_SHAPE;
     if (sinks < 0 || recent < 0 || (int64_t)sinks + recent > keep) return PEQA_ERR_PARAM;
-    if (weights_head_stride < max_len || weights_seq_stride < max_len) return PEQA_ERR_SHAPE;
+    if (!peqa::weights_apart(C, max_len, weights_seq_stride, weights_head_stride)) return PEQA_ERR_SHAPE;
     if ((reinterpret_cast<uintptr_t>(lens) | reinterpret_cast<uintptr_t>(seq) | reinterpret_cast<uintptr_t>(weights) |
          reinterpret_cast<uintptr_t>(weights_out) | reinterpret_cast<uintptr_t>(kept) | reinterpret_cast<uintptr_t>(new_lens)) & 3)
         return PEQA_ERR_ALIGN;
