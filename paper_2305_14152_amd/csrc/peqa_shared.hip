@@ -24,6 +24,15 @@ using namespace peqa::host;
 
 namespace peqa {
 
+// How a call is cut.
+struct SharedPlan {
+    bool wide;
+    int hb, columns, tiles, chunk, chunks, own_chunk, own_splits, own_blocks, own_columns, join_each;
+    long long prefix_wgs, own_items;
+    size_t part_bytes, ml_bytes;
+};
+SharedPlan shared_plan(const peqa_kv_cache *C, int rows, int heads, int max_len, int shared);
+
 namespace {
 
 constexpr int TILE = 32;       // positions of a wave's step
@@ -892,13 +901,7 @@ template <int D, int EACH> __global__ __launch_bounds__(256) void shared_join_ke
     if (a.lse && at == 0) a.lse[(size_t)row * a.heads + head] = any ? (top + __builtin_amdgcn_logf(total)) * LN2 : -__builtin_inff();
 }
 
-// How a call is cut.
-struct SharedPlan {
-    bool wide;
-    int hb, columns, tiles, chunk, chunks, own_chunk, own_splits, own_blocks, own_columns, join_each;
-    long long prefix_wgs, own_items;
-    size_t part_bytes, ml_bytes;
-};
+}  // namespace
 
 SharedPlan shared_plan(const peqa_kv_cache *C, int rows, int heads, int max_len, int shared)
 {
@@ -959,6 +962,8 @@ SharedPlan shared_plan(const peqa_kv_cache *C, int rows, int heads, int max_len,
     p.ml_bytes = round256(slots * 2 * sizeof(float));
     return p;
 }
+
+namespace {
 
 template <int D, bool FP8> hipError_t launch_shared(const SharedArgs &a, const SharedPlan &p, hipStream_t stream)
 {
