@@ -31,7 +31,7 @@ struct AppendArgs {
 // of what is not rotated, 16 neighbours.  Every element is loaded and stored once, 16 bytes at a time; the tables' rows (4 rot bytes
 // a token) are shared by the token's heads.  Bound by memory for prompts (5555 tokens, 32 + 2 x 8 heads of 256, 8-bit cache: 48.8 us, 5.2 TB/s)
 // and by three loads after one another, position, page and tables, for single tokens (16 of 32 + 2 x 32 heads of 128: 3.4 us).  With norms 5003
-// tokens, 40 + 2 x 8 heads of 128, half rotated in neighbouring pairs, 8-bit cache: 32.7 us, 4.1 TB/s; 16 tokens of 32 + 2 x 8 heads 3.8 us.
+// tokens, 40 + 2 x 8 heads of 128, half rotated in neighbouring pairs, 8-bit cache: 32.5 us, 4.1 TB/s; 16 tokens of 32 + 2 x 8 heads 3.4 us.
 template <bool FP8, bool INTERLEAVED, bool NORM>
 __global__ __launch_bounds__(256) void rope_append_kernel(AppendArgs a)
 {

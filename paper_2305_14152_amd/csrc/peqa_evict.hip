@@ -62,7 +62,7 @@ __device__ __forceinline__ uint32_t order_of(float w)
 // histogram of the weights that have the digits found so far (counts: no order of adding matters); then, as many positions as there
 // are threads at a time and in order, those above it and as many equal ones as there is room for get their places.  A sort would move every weight
 // log n times for an order among those that stay that nobody asks for.  Bound by the latency of its barriers, three for a digit and one for
-// as many positions as there are threads: 8 heads of 1501 positions 6.7 us, 512 of up to 2048 10 us, 8 of 30000 47.
+// as many positions as there are threads: 8 heads of 1501 positions 7.0 us, 512 of up to 2048 10 us, 8 of 30000 47.
 template <int THREADS>
 __global__ __launch_bounds__(THREADS) void evict_select_kernel(EvictArgs a)
 {
@@ -210,8 +210,8 @@ constexpr int each_of(int threads) { return threads > 512 ? 4 : 8; }
 // In place a workgroup goes over all positions in order: no position moves up, so what is written lies at or below what the
 // workgroup has read when it writes, what is read next lies above, and no other workgroup has these bytes.  To another cache the positions
 // are split over workgroups too.
-// Bound by memory where there are many heads: 16 sequences x 32 heads of up to 2048 positions to 1024 53 us, 4.5 TB/s of what moves; by what
-// a workgroup has in flight between two barriers where there are few: 8 heads of 1501 to 1001 6.1 us, of 30000 to 20000 95
+// Bound by memory where there are many heads: 16 sequences x 32 heads of up to 2048 positions to 1024 53.8 us, 4.5 TB/s of what moves; by what
+// a workgroup has in flight between two barriers where there are few: 8 heads of 1501 to 1001 6.2 us, of 30000 to 20000 95
 // (32 workgroups, 55 GB/s of what moves each: a place must not be written before all that was there is read).
 template <int THREADS>
 __global__ __launch_bounds__(THREADS) void evict_move_kernel(EvictArgs a)

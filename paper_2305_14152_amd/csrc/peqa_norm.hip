@@ -57,7 +57,7 @@ template <bool INTERLEAVED> __device__ __forceinline__ Places places(const NormA
 
 // A unit of 16 elements a thread, as in the cache's append kernel: a head's sum of squares is two to four lane exchanges, and everything is read
 // and written once.  Products and sums are fp32; the output is rounded to bf16 once, the type of its readers.  Bound by
-// memory: 2048 tokens of 2 x 32 heads of 128 14.2 us, 4.7 TB/s; 129 of 10 heads of 256 3.2 us, a launch and three loads after one another.
+// memory: 2048 tokens of 2 x 32 heads of 128 14.7 us, 4.6 TB/s; 129 of 10 heads of 256 3.4 us, a launch and three loads after one another.
 template <bool INTERLEAVED>
 __global__ __launch_bounds__(256) void norm_rope_kernel(NormArgs a)
 {
@@ -89,7 +89,7 @@ __global__ __launch_bounds__(256) void norm_rope_kernel(NormArgs a)
 // The same units.  TRAINED: a workgroup goes over several items, so that a thread adds up the weights' gradients of the elements it always
 // has, its heads meet in LDS and few rows of sums are left for norm_weights_kernel, all in a fixed order (atomics would change the bits from
 // call to call).  x is normalised again from its bf16 rather than kept: that is 4 bytes an element less than storing z, and r costs a few
-// lane exchanges.  Bound by memory: 2048 tokens of 2 x 32 heads of 128 19.5 us, 5.2 TB/s.
+// lane exchanges.  Bound by memory: 2048 tokens of 2 x 32 heads of 128 20.0 us, 5.0 TB/s.
 template <bool INTERLEAVED, bool TRAINED>
 __global__ __launch_bounds__(256) void norm_rope_bwd_kernel(NormArgs a)
 {

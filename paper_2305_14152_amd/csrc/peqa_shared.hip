@@ -11,11 +11,14 @@
 // for every column without passing through LDS.  More have waves of their own, 16 or 32 each of eight, and keys and values come to LDS once,
 // as operands, for all of them.
 //
-// Bound by memory where columns are few: 3 rows x 32 heads behind 555 positions 5.4 us and the join 3, launches and loads after one another;  16
-// rows x 32 heads behind 2048 with up to 512 of their own 20 us, 4.9 TB/s of the cache.  Where they are many, by three things that overlap in part and
+// Bound by memory where columns are few: 3 rows x 32 heads behind 555 positions 5.2 us and the join 3.5, launches and loads after one another;  16
+// rows x 32 heads behind 2048 with up to 512 of their own 20.4 us, 4.8 TB/s of the cache.  Where they are many, by three things that overlap in part and
 // are about 1000 cycles each for a tile of 32 positions and 256 columns, of the 2800 that it takes: matrix instructions, vector instructions of the softmax and
 // of the operands, and the operands' way out of LDS, 16 KB for each of eight waves.  65537 positions of 8 bits, 8 key heads, 256 columns
-// 93 us, 0.74 PFLOP/s; more columns a wave than 32, which would halve the last, do not fit its registers.
+// 94.5 us, 0.73 PFLOP/s; more columns a wave than 32, which would halve the last, do not fit its registers.  Heads of 256 have no such form: every 32
+// columns walk the shared positions anew (32 rows x 4 key heads x 8 behind 8000: 52 us, 8 bits 38).  A row that ends among the shared positions
+// has them to itself, in as many workgroups as the rows' own positions are given: one where those are few (32 rows x 64 heads behind 65536 with 333 of
+// their own, one of them 65535 long: 672 us for 146, 8 bits 360 for 100).
 #include "peqa_attend.h"
 #include "peqa_cache.h"
 #include "peqa_host.h"
@@ -179,7 +182,9 @@ template <bool FP8, int VR> __device__ __forceinline__ void turn_values(const ui
         }
 }
 
-// Weights of 8 positions and a column as operands: bf16 in two parts, fp16 in one.
+// Weights of 8 positions and a column as operands: bf16 in two parts, fp16 in one.  (A second fp16 part, 22 bits for 11, is as many matrix instructions again as
+// the values have: 65537 positions of 8 bits, 256 columns 118.3 us for 93.9, 8192 of heads of 64 31.5 for 26.5, 40000 and 64 columns 29.4 for 27.5.  Values of
+// 8 bits are off by 2^-4 themselves, and a weight's 2^-12 is of any sign.)
 template <bool FP8> struct Weights {
     u32x4 near, rest;
 };
@@ -237,7 +242,7 @@ __device__ __forceinline__ Eights powers(const f32x4 (&x)[2], float scale, float
     return e;
 }
 // As operands.  Two bf16 parts have 16 bits: the first is cut, so that the second is not negative, and not 0: an infinite value then gives
-// infinities of one sign.
+// infinities of one sign, and a finite one of 10^34 counts for 10^-4 at least.
 template <bool FP8> __device__ __forceinline__ Weights<FP8> operands(const Eights &e)
 {
     const auto &p = e.p;
